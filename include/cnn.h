@@ -449,6 +449,134 @@ int cnn_closed_form(const cnn_problem* prob, double P, double M, int capacity_mo
  */
 int cnn_hbm_bytes(const cnn_plan_t* plan, int64_t xcds, int64_t l2_bytes, double terms[3]);
 
+/*
+ * ---- Routed contractions: the Ker depends on the row ----------------------
+ *
+ * A router gives each of Nt rows Kt of Ng Kers (experts); the rows are put in
+ * the order of their Kers, multiplied group by group, and returned to where
+ * they came from.  All of it stays on the device: group sizes are device
+ * integers, read by the kernels, and no call waits for them.
+ *
+ * As above: dense row-major device buffers owned by the caller, arguments
+ * checked before any HIP call, asynchronous on `stream`, nothing allocated,
+ * capturable into a HIP graph.  `dtype` gives the operands' type and the
+ * result's (CNN_BF16: bf16 operands, fp32 result); integers are int32, weights
+ * and their gradients fp32.  Buffers may start at any element (fp32 at 4
+ * bytes); 16-byte aligned rows are fastest.  Nt = 0 or Np = 0 is a call without
+ * rows (tensors without elements may be NULL).  Results must not overlap any
+ * other argument (CNN_E_ALIAS).  Every sum has a fixed order: results do not
+ * vary from call to call.
+ *
+ * Grouped order: place p of [Offsets[g], Offsets[g+1]) belongs to group g;
+ * Offsets[0] = 0, non-decreasing, Offsets[Ng] <= Np.  Places from Offsets[Ng]
+ * on belong to no group: their results are zeros.  Rows[p] is the source row
+ * of place p; a row outside [0, Nt) reads as zeros.  Offsets that are no such
+ * order leave the result unspecified, but whatever these integers are, no
+ * kernel reads or writes outside the buffers.
+ */
+
+/* What the router's weights are a softmax over. */
+typedef enum cnn_over {
+  CNN_OVER_ALL = 0,    /* all allowed experts: a row's weights add up to at most 1 */
+  CNN_OVER_CHOSEN = 1  /* the row's chosen experts: they add up to 1               */
+} cnn_over;
+
+/*
+ * Routing.  For each row t of Logits[Nt][Ng] (Ng <= 1024) the Kt (<= 16, <=
+ * Ng) largest allowed logits, in descending order, ties to the lowest expert:
+ * Choice[t][j] is the j-th's expert and Gates[t][j] its weight,
+ * exp(l - max) / sum of exp(l' - max) over `over`.  -inf and NaN are not
+ * allowed: a row with fewer than Kt allowed experts has Choice -1 and Gates 0
+ * in the places left, one with none in all.  +inf takes the whole weight,
+ * shared equally among its kind.  The type's lowest value is an ordinary one.
+ *
+ * Offsets[Ng + 1], Rows[Nt Kt] and Slots[Nt][Kt] put the (row, choice) pairs in
+ * the order of their experts, rows in order within one: Slots[t][j] is the
+ * pair's place (-1: not chosen), Rows[Slots[t][j]] = t, Rows is -1 from
+ * Offsets[Ng] on.  dtype is the logits' (CNN_F32, else bf16).  workspace:
+ * cnn_route_ws bytes (0 for few rows), 16-byte aligned, as in cnn_fwd_plan_ws.
+ * Errors: CNN_E_NULL, CNN_E_SHAPE (also: workspace too small or misaligned),
+ * CNN_E_DTYPE, CNN_E_OVERFLOW (also: Ng or Kt above its limit), CNN_E_ALIAS,
+ * CNN_E_UNSUPPORTED (`over`), CNN_E_HIP.
+ */
+int cnn_route(const void* Logits, int32_t* Choice, float* Gates, int32_t* Offsets, int32_t* Rows,
+              int32_t* Slots, int64_t Nt, int64_t Ng, int64_t Kt, int dtype, int over,
+              void* workspace, int64_t ws_bytes, void* stream);
+
+/* Bytes of cnn_route's workspace (host only). */
+int cnn_route_ws(int64_t Nt, int64_t Ng, int64_t Kt, int64_t* ws_bytes);
+
+/*
+ * The router's gradient: dLogits from dGates, with Choice and Gates as
+ * cnn_route gave them.  With p the softmax over `over` (zero outside it),
+ * dLogits[t][e] = p[e] ([e chosen] dGates[e] - sum_j Gates[j] dGates[j]); zero
+ * for experts that are not allowed and for rows without a choice.
+ */
+int cnn_route_bwd(const void* Logits, const int32_t* Choice, const float* Gates,
+                  const float* dGates, void* dLogits, int64_t Nt, int64_t Ng, int64_t Kt,
+                  int dtype, int over, void* stream);
+
+/*
+ * The return to the rows: Out[t] = sum_j Gates[t][j] In[Slots[t][j]] in the
+ * order of j, fp32 sums; places outside [0, Np) add nothing.  Gates NULL: ones
+ * (the gradient of a gather: dIn of cnn_group_bwd_in summed for each row).
+ */
+int cnn_combine(const void* In, const int32_t* Slots, const float* Gates, void* Out, int64_t Nt,
+                int64_t Kt, int64_t Np, int64_t Nk, int dtype, void* stream);
+
+/*
+ * Its gradient: for each pair with a place p = Slots[t][j],
+ * dIn[p] = Gates[t][j] dOut[t] and dGates[t][j] = sum_k dOut[t][k] In[p][k] (0
+ * without a place).  Rows names the places without a pair (Rows[p] < 0), whose
+ * dIn is zero.  A place must belong to one pair, as cnn_route makes them.
+ * Gates may be NULL (ones), dGates may be NULL (not wanted).  dOut and In have
+ * the operands' type, dIn the result's.
+ */
+int cnn_combine_bwd(const void* dOut, const void* In, const int32_t* Slots, const int32_t* Rows,
+                    const float* Gates, void* dIn, float* dGates, int64_t Nt, int64_t Kt,
+                    int64_t Np, int64_t Nk, int dtype, void* stream);
+
+/*
+ * The groups' products:
+ *   Out[p][k] = sum_c In[Rows[p]][c] Ker[g][k][c],   p in group g
+ * In[Nt][Nc], Ker[Ng][Nk][Nc], Out[Np][Nk].  Rows NULL: In is in grouped order
+ * already (Nt = Np).  Ng <= 65535.
+ */
+int cnn_group_fwd(const void* In, const void* Ker, void* Out, const int32_t* Offsets,
+                  const int32_t* Rows, int64_t Nt, int64_t Np, int64_t Ng, int64_t Nc, int64_t Nk,
+                  int dtype, void* stream);
+
+/* Its gradient in In, in grouped order: dIn[p][c] = sum_k dOut[p][k] Ker[g][k][c]. */
+int cnn_group_bwd_in(const void* dOut, const void* Ker, void* dIn, const int32_t* Offsets,
+                     int64_t Np, int64_t Ng, int64_t Nc, int64_t Nk, int dtype, void* stream);
+
+/*
+ * Its gradient in Ker: dKer[g][k][c] = sum over p in group g of
+ * dOut[p][k] In[Rows[p]][c]; zero for a group without rows.
+ */
+int cnn_group_bwd_ker(const void* dOut, const void* In, void* dKer, const int32_t* Offsets,
+                      const int32_t* Rows, int64_t Nt, int64_t Np, int64_t Ng, int64_t Nc,
+                      int64_t Nk, int dtype, void* stream);
+
+/*
+ * A shared projection with a low-rank adapter for each row:
+ *   Out[t][k] = sum_c In[t][c] Ker[k][c]
+ *             + Scales[a] sum_r (sum_c In[t][c] A[a][r][c]) B[a][k][r],  a = Ids[t]
+ * In[Nt][Nc], Ker[Nk][Nc], A[Na][Nl][Nc], B[Na][Nk][Nl], Scales[Na] (NULL:
+ * ones), Na <= 1024, Nl <= 4096.  A row whose Ids is outside [0, Na) has no
+ * adapter.  Adapters of smaller rank are stored with zeros up to Nl.  The inner
+ * sum is kept to fp32 (bf16 Out: to 2^-16 of itself).  For calls that serve;
+ * gradients are those of cnn_group_* with the adapters as groups.  workspace:
+ * cnn_adapt_ws bytes, 16-byte aligned.  Errors as cnn_route.
+ */
+int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
+                  const int32_t* Ids, const float* Scales, void* Out, int64_t Nt, int64_t Nc,
+                  int64_t Nk, int64_t Na, int64_t Nl, int dtype, void* workspace,
+                  int64_t ws_bytes, void* stream);
+
+/* Bytes of cnn_adapt_fwd's workspace (host only). */
+int cnn_adapt_ws(int64_t Nt, int64_t Nc, int64_t Nk, int64_t Na, int64_t Nl, int64_t* ws_bytes);
+
 /* Budget of HIP device `device` (CU count, LDS per CU, accumulator regs). */
 int cnn_device_budget(int device, cnn_budget* budget);
 

@@ -36,7 +36,10 @@ EXPORTS = ["cnn_fwd", "cnn_plan", "cnn_plan_candidates", "cnn_variants", "cnn_pl
            "cnn_plan_lookup", "cnn_plan_tiles", "cnn_fwd_plan", "cnn_fwd_plan_ws",
            "cnn_fwd_plan_static", "cnn_eq1_cost",
            "cnn_slab_cost", "cnn_closed_form", "cnn_hbm_bytes", "cnn_device_budget",
-           "cnn_strerror", "cnn_last_error", "cnn_abi_version"]
+           "cnn_strerror", "cnn_last_error", "cnn_abi_version",
+           "cnn_route", "cnn_route_ws", "cnn_route_bwd", "cnn_combine", "cnn_combine_bwd",
+           "cnn_group_fwd", "cnn_group_bwd_in", "cnn_group_bwd_ker", "cnn_adapt_fwd",
+           "cnn_adapt_ws"]
 
 i64 = ctypes.c_int64
 
@@ -134,6 +137,20 @@ def lib():
               "cnn_eq1_cost", "cnn_slab_cost", "cnn_closed_form", "cnn_hbm_bytes", "cnn_device_budget",
               "cnn_abi_version"):
         getattr(L, f).restype = ctypes.c_int
+    # the routed contractions (called through routed.py)
+    lp, ci = ctypes.POINTER(i64), ctypes.c_int
+    for f, args in (("cnn_route", [vp] * 6 + [i64] * 3 + [ci, ci, vp, i64, vp]),
+                    ("cnn_route_ws", [i64] * 3 + [lp]),
+                    ("cnn_route_bwd", [vp] * 5 + [i64] * 3 + [ci, ci, vp]),
+                    ("cnn_combine", [vp] * 4 + [i64] * 4 + [ci, vp]),
+                    ("cnn_combine_bwd", [vp] * 7 + [i64] * 4 + [ci, vp]),
+                    ("cnn_group_fwd", [vp] * 5 + [i64] * 5 + [ci, vp]),
+                    ("cnn_group_bwd_in", [vp] * 4 + [i64] * 4 + [ci, vp]),
+                    ("cnn_group_bwd_ker", [vp] * 5 + [i64] * 5 + [ci, vp]),
+                    ("cnn_adapt_fwd", [vp] * 7 + [i64] * 5 + [ci, vp, i64, vp]),
+                    ("cnn_adapt_ws", [i64] * 5 + [lp])):
+        getattr(L, f).argtypes = args
+        getattr(L, f).restype = ci
     _lib = L
     return L
 

@@ -1,0 +1,551 @@
+// The tile kernel of the grouped products (bf16 and fp32 MFMA, gfx950).
+//
+// One workgroup computes TM x TN results D[n][m] = sum_k X[m, k] Y[n, k] of
+// one group.  m is the result's last index, so the MFMA's row operand is X
+// and a lane ends up with four consecutive results of one row n.  Either
+// operand may lie with k last (KC: rows of the tile, 128 bytes of k a stage)
+// or with the tile's own index last (MC: rows of k, read from LDS by the
+// transposing LDS read in bf16):
+//   forward       X = Ker[g] (KC), Y = gathered In rows (KC)
+//   gradient, In  X = Ker[g] (MC), Y = dOut rows (KC)
+//   gradient, Ker X = gathered In rows (MC), Y = dOut rows (MC), k = the rows
+//   adapted       X = Ker, Y = In rows in the order of their adapters, one
+//                 group, then the low-rank part
+// Group sizes are read on the device, so the caller never waits for them: a
+// workgroup finds its tile by adding up the groups' tile counts (a wave scans
+// 64 groups at a time), and the launch has as many workgroups as the worst
+// split of the rows into groups needs.  Rows past the last group are a last
+// group without products: their results are zeros.
+//
+// LDS: each operand's stage is 8 units of 16 bytes per tile row (KC) or the
+// same number laid out by k (MC).  Units are permuted within their row so
+// that the 16 lanes of a read meet all 64 banks once.
+#pragma once
+
+#include "common.h"
+#include "routed.h"
+
+namespace cnnlib {
+namespace group {
+
+enum Mode { kFwd = 0, kBwdIn = 1, kBwdKer = 2, kAdapt = 3 };
+
+#define LDS_AS(T, p) ((__attribute__((address_space(3))) T*)(p))
+#define GLB_AS(T, p) ((__attribute__((address_space(1))) T*)(p))
+
+// 16 zero bytes that copies of what lies outside a tensor read instead.
+static __device__ __attribute__((aligned(16))) uint32_t zero_unit[4] = {0, 0, 0, 0};
+
+__device__ __forceinline__ void copy16_lds(const void* src, void* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(GLB_AS(void, const_cast<void*>(src)), LDS_AS(void, lds), 16, 0, 0);
+#else
+  (void)src;
+  (void)lds;
+#endif
+}
+
+// `valid` (at most 16 / sizeof(T)) elements at any element alignment, the rest zeros.
+template <typename T> __device__ __forceinline__ u32x4_t load_unit(const T* p, int valid) {
+  constexpr int CE = 16 / (int)sizeof(T);
+  u32x4_t v = {0u, 0u, 0u, 0u};
+  if (valid >= CE) {
+    __builtin_memcpy(&v, p, 16);
+  } else if (valid > 0) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < CE; ++i)
+        if (i < valid) v[i] = __builtin_bit_cast(uint32_t, p[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < CE; ++i)
+        if (i < valid) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    }
+  }
+  return v;
+}
+
+// Where unit `c` (16 bytes) of row `r` of an operand's stage lies.  KC: 8
+// units a row, 16 rows of one unit column hit 16 distinct 16-byte columns.
+// MC: R * sizeof(T) / 16 units a row of k; bf16 keeps pairs of units (the 32
+// bytes a transposing read takes from a row) together and spreads the 8 rows
+// that half a wave reads at once, fp32 keeps 64 bytes and spreads the four
+// rows a wave reads at once.
+template <typename T, bool KC, int R> __device__ __forceinline__ int unit_at(int r, int c) {
+  if constexpr (KC) return r * 8 + (c ^ ((r >> 1) & 7));
+  constexpr int U = R * (int)sizeof(T) / 16;
+  if constexpr (sizeof(T) == 2) {
+    const int g = U >= 16 ? (r & 3) | ((r >> 1) & 4) : ((r >> 1) & 1) | ((r >> 2) & 2);
+    return r * U + (c ^ (g << 1));
+  } else {
+    return r * U + (c ^ (((r >> 2) & 3) << 2));
+  }
+}
+
+// Stages one operand: R tile rows by TK values of k, 8 R units by NT threads.
+template <typename T, bool KC, int R, int NT, bool DMA, bool GATHER> struct Stager {
+  static constexpr int CE = 16 / (int)sizeof(T);
+  static constexpr int TK = 128 / (int)sizeof(T);
+  static constexpr int NU = 8 * R / NT;  // units a thread copies per stage
+  static constexpr int U = KC ? 8 : R / CE;
+  static_assert(8 * R % NT == 0, "whole rounds");
+
+  const T* p[NU];   // the unit's first element at k = 0
+  int lim[NU];      // KC: elements of k from the unit's first; MC: elements of the tile index
+  int krow[NU];     // MC: row of k within a stage
+  u32x4_t reg[DMA ? 1 : NU];
+
+  // base: the tensor at its first k; rows [i0, i0 + n) of the tile index are
+  // valid; ld: elements from row to row; K: extent of k (KC).
+  // index: for a gathered KC operand, the source row of each tile row.
+  __device__ __forceinline__ void init(int tid, const T* base, int64_t ld, int64_t i0, int n, int K,
+                                       const int32_t* index, int nsrc) {
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      const int u = j * NT + tid;
+      const int r = u / U, pos = u % U;
+      const int c = unit_at<T, KC, R>(r, pos) - r * U;  // the permutation is its own inverse
+      if constexpr (KC) {
+        int64_t row = i0 + r;
+        bool ok = r < n;
+        if constexpr (GATHER) {
+          if (ok && index) {
+            row = index[row];
+            ok = row >= 0 && row < nsrc;
+          }
+        }
+        p[j] = base + (ok ? row * ld : 0) + c * CE;
+        lim[j] = ok ? K - c * CE : 0;
+        krow[j] = 0;
+      } else {
+        p[j] = base + i0 + c * CE;
+        lim[j] = n - c * CE;
+        krow[j] = r;
+      }
+    }
+  }
+
+  // Source and valid elements of unit j of the stage at k0.  MC: `index` as
+  // in init for the rows of k; nk rows of k in all.
+  __device__ __forceinline__ const T* at(int j, int k0, int64_t ld, int nk, const int32_t* index,
+                                         int nsrc, int* valid) const {
+    if constexpr (KC) {
+      *valid = lim[j] - k0;
+      return p[j] + k0;
+    } else {
+      const int k = k0 + krow[j];
+      int64_t row = k;
+      bool ok = k < nk;
+      if constexpr (GATHER) {
+        if (ok && index) {
+          row = index[k];
+          ok = row >= 0 && row < nsrc;
+        }
+      }
+      *valid = ok ? lim[j] : 0;
+      return p[j] + (ok ? row * ld : 0);
+    }
+  }
+
+  __device__ __forceinline__ void issue(int tid, u32x4_t* lds, int k0, int64_t ld, int nk,
+                                        const int32_t* index, int nsrc) {
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      int valid;
+      const T* src = at(j, k0, ld, nk, index, nsrc, &valid);
+      if constexpr (DMA) {
+        // whole units only: a unit that starts inside a row ends inside it
+        const void* from = valid > 0 ? (const void*)src : (const void*)zero_unit;
+        copy16_lds(from, lds + j * NT + (__builtin_amdgcn_readfirstlane(tid) & ~63));
+      } else {
+        reg[j] = load_unit(src, valid);
+      }
+    }
+  }
+  __device__ __forceinline__ void commit(int tid, u32x4_t* lds) {
+    if constexpr (!DMA) {
+#pragma unroll
+      for (int j = 0; j < NU; ++j) lds[j * NT + tid] = reg[j];
+    }
+  }
+};
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ u32x2_t read_tr(const bf16_t* p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         LDS_AS(s16x4_t, const_cast<bf16_t*>(p))));
+#else
+  (void)p;
+  return u32x2_t{0u, 0u};
+#endif
+}
+
+// The operand of 16 tile rows from i0 for the k sub-step ks.  bf16: 32 values
+// of k, lane l row l % 16 and k = 8 (l / 16) + 0..7.  fp32: 16 values of k,
+// element e of lane l is k = 4 (l / 16) + e, used by the e-th of four MFMAs.
+template <typename T, bool KC, int R>
+__device__ __forceinline__ u32x4_t read_frag(const u32x4_t* lds, int i0, int ks, int lane) {
+  const int l16 = lane & 15, G = lane >> 4;
+  if constexpr (KC) {
+    return lds[unit_at<T, true, R>(i0 + l16, 4 * ks + G)];
+  } else if constexpr (sizeof(T) == 2) {
+    // 4 rows of k by 16 columns for each 16 lanes: lane 4v + q reads row v,
+    // columns 4q .. 4q+3, and receives column l % 16 of the four rows
+    const int k = 32 * ks + 8 * G + (l16 >> 2), q = l16 & 3;
+    const bf16_t* base = reinterpret_cast<const bf16_t*>(lds);
+    const bf16_t* a = base + 8 * unit_at<T, false, R>(k, (i0 >> 3) + (q >> 1)) + 4 * (q & 1);
+    const bf16_t* b = base + 8 * unit_at<T, false, R>(k + 4, (i0 >> 3) + (q >> 1)) + 4 * (q & 1);
+    const u32x2_t lo = read_tr(a), hi = read_tr(b);
+    return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+  } else {
+    const uint32_t* base = reinterpret_cast<const uint32_t*>(lds);
+    u32x4_t v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = base[4 * unit_at<T, false, R>(16 * ks + 4 * G + e, (i0 >> 2) + (l16 >> 2)) + (l16 & 3)];
+    return v;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4_t mma(u32x4_t x, u32x4_t y, f32x4_t acc) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x),
+                                                   __builtin_bit_cast(bf16x8_t, y), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[e]), __uint_as_float(y[e]), acc,
+                                                 0, 0, 0);
+    return acc;
+  }
+}
+
+// Four consecutive results from `m` of one row, as many as lie below M.
+template <typename TO>
+__device__ __forceinline__ void store4(TO* row, int m, int M, f32x4_t v, bool whole) {
+  if (whole && m + 4 <= M) {
+    if constexpr (sizeof(TO) == 4) {
+      *reinterpret_cast<f32x4_t*>(row + m) = v;
+    } else {
+      *reinterpret_cast<u32x2_t*>(row + m) = u32x2_t{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (m + e < M) row[m + e] = from_f32<TO>(v[e]);
+  }
+}
+
+// A row tile of the groups: its group (Ng: the rows past the last), the rows
+// [n0, n1) of the group from the tile's first on, and its tile of m.
+struct RowTile {
+  int g, n0, n1, mt;
+};
+
+// Rows of group g; group Ng is the rows past the last.
+__device__ __forceinline__ void group_rows(const int32_t* off, int Ng, int Np, int g, int* lo,
+                                           int* hi) {
+  *lo = off[g];
+  *hi = g < Ng ? off[g + 1] : Np;
+}
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+// The tile of workgroup `bid` of a launch over the groups' row tiles by MT
+// tiles of m; false: none.  Row tiles are walked in bands: `band` row tiles by
+// every m tile, so that the tiles an XCD runs at a time share their rows of X
+// and Y in its L2.  Offsets that are not an order (documented as the caller's
+// duty) are found out by the wave that adds them up: no tile is then run.
+template <int TN>
+__device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, int MT, int bid,
+                                          int band, RowTile* t) {
+  const int lane = threadIdx.x & 63;
+  int nt, j0, lo_g = 0, hi_g = Np;  // row tiles of the group, tile within it, its rows
+  t->g = 0;
+  if (!off) {
+    nt = (Np + TN - 1) / TN;
+    if (bid >= nt * MT) return false;
+    j0 = xcd_remap(bid, nt * MT);
+  } else {
+    int total = 0;
+    for (int base = 0; base <= Ng; base += 64) {
+      const int g = base + lane;
+      int lo = 0, hi = 0;
+      if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
+      if (__ballot(lo < 0 || hi < lo || hi > Np || (g == 0 && lo != 0))) return false;
+      total += __shfl(wave_scan((hi - lo + TN - 1) / TN, lane), 63);
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    if (bid >= total * MT) return false;
+    const int L = xcd_remap(bid, total * MT);
+    int before = 0;
+    for (int base = 0;; base += 64) {
+      const int g = base + lane;
+      int lo = 0, hi = 0;
+      if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
+      const int n = (hi - lo + TN - 1) / TN;
+      const int incl = before + wave_scan(n, lane);
+      const uint64_t here = __ballot(L < incl * MT);
+      if (here) {
+        const int who = __ffsll((unsigned long long)here) - 1;
+        nt = __builtin_amdgcn_readfirstlane(__shfl(n, who));
+        j0 = L - (__builtin_amdgcn_readfirstlane(__shfl(incl, who)) - nt) * MT;
+        t->g = __builtin_amdgcn_readfirstlane(base + who);
+        lo_g = __builtin_amdgcn_readfirstlane(__shfl(lo, who));
+        hi_g = __builtin_amdgcn_readfirstlane(__shfl(hi, who));
+        break;
+      }
+      before = __shfl(incl, 63);
+    }
+  }
+  const int b = j0 / (band * MT), rb = min(band, nt - b * band), j = j0 - b * band * MT;
+  t->mt = j / rb;
+  t->n0 = lo_g + (b * band + j % rb) * TN;
+  t->n1 = hi_g;
+  return true;
+}
+
+// Part `part` of h as the sum of bf16 values: the leading 8 bits of what the
+// earlier parts left.  What is not finite is all in the first part.
+__device__ __forceinline__ float bf16_part(float h, int part) {
+  if (!(fabsf(h) < INFINITY)) return part == 0 ? to_f32(from_f32<bf16_t>(h)) : 0.f;
+  float v = __uint_as_float(__float_as_uint(h) & 0xffff0000u);
+  for (int i = 0; i < part; ++i) {
+    h -= v;
+    v = __uint_as_float(__float_as_uint(h) & 0xffff0000u);
+  }
+  return v;
+}
+
+// TM x TN results by WM x WN waves.  DMA: both operands by 16-byte copies to
+// LDS (16-byte aligned rows), else through registers.
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>
+__global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
+  constexpr int NT = 64 * WM * WN;
+  constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
+  constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE == kAdapt;  // gathered operands
+  constexpr int TK = 128 / (int)sizeof(T);
+  constexpr int KS = 2;  // sub-steps of a stage: 32 (bf16) or 16 (fp32) values of k
+  constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
+  constexpr int XU = 8 * TM, YU = 8 * TN;
+
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  u32x4_t* const buf0 = reinterpret_cast<u32x4_t*>(smem);
+  u32x4_t* const buf1 = buf0 + XU + YU;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  const int MT = (a.M + TM - 1) / TM;
+
+  RowTile t;
+  const T* X = reinterpret_cast<const T*>(a.X);
+  const T* Y = reinterpret_cast<const T*>(a.Y);
+  TO* D = reinterpret_cast<TO*>(a.D);
+  const int32_t* rows = a.rows;
+  int K, n_rows;  // extent of k; valid rows of n in this tile
+  if constexpr (MODE == kBwdKer) {
+    const int NTL = (a.N + TN - 1) / TN;
+    const int L = xcd_remap(blockIdx.x, gridDim.x);
+    t.g = L / (MT * NTL);
+    const int j0 = L - t.g * MT * NTL;
+    const int b = j0 / (band * MT), rb = min(band, NTL - b * band), j = j0 - b * band * MT;
+    t.mt = j / rb;
+    t.n0 = (b * band + j % rb) * TN;
+    int lo, hi;
+    group_rows(a.off, a.Ng, a.K, t.g, &lo, &hi);
+    // clamped, so that no offset leads outside the tensors
+    lo = min(max(__builtin_amdgcn_readfirstlane(lo), 0), a.K);
+    K = min(max(__builtin_amdgcn_readfirstlane(hi), lo), a.K) - lo;
+    n_rows = a.N - t.n0;
+    if (rows) rows += lo; else X += lo * a.ldx;
+    Y += lo * a.ldy;
+    D += t.g * a.dgroup + (int64_t)t.n0 * a.ldd;
+  } else {
+    if (!find_tile<TN>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return;
+    K = t.g < a.Ng ? a.K : 0;  // the rows past the last group: no products
+    n_rows = t.n1 - t.n0;
+    X += (t.g < a.Ng ? t.g : 0) * a.xgroup;
+    if constexpr (MODE != kAdapt) D += (int64_t)t.n0 * a.ldd;
+  }
+  const int m0 = t.mt * TM;
+  const int n_valid = min(n_rows, TN), m_valid = min(a.M - m0, TM);
+
+  Stager<T, XKC, TM, NT, DMA, XG> sx;
+  Stager<T, YKC, TN, NT, DMA, YG> sy;
+  sx.init(tid, X, a.ldx, m0, m_valid, K, nullptr, 0);
+  sy.init(tid, Y, a.ldy, t.n0, n_valid, K, YG ? rows : nullptr, a.Nsrc);
+  const int32_t* const xrows = XG ? rows : nullptr;
+
+  f32x4_t acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4_t xf[NI], yf[NJ];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        xf[i] = read_frag<T, XKC, TM>(buf, wm * (TM / WM) + 16 * i, ks, lane);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        yf[j] = read_frag<T, YKC, TN>(buf + XU, wn * (TN / WN) + 16 * j, ks, lane);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i], yf[j], acc[i][j]);
+    }
+  };
+
+  const int n_st = (K + TK - 1) / TK;
+  if (n_st > 0) {
+    sx.issue(tid, buf0, 0, a.ldx, K, xrows, a.Nsrc);
+    sy.issue(tid, buf0 + XU, 0, a.ldy, K, nullptr, 0);
+    sx.commit(tid, buf0);
+    sy.commit(tid, buf0 + XU);
+  }
+  for (int s = 0; s < n_st; ++s) {
+    u32x4_t* const cur = s & 1 ? buf1 : buf0;
+    u32x4_t* const nxt = s & 1 ? buf0 : buf1;
+    // this stage has landed and every wave is done with the other buffer
+    __syncthreads();
+    if (s + 1 < n_st) {
+      sx.issue(tid, nxt, (s + 1) * TK, a.ldx, K, xrows, a.Nsrc);
+      sy.issue(tid, nxt + XU, (s + 1) * TK, a.ldy, K, nullptr, 0);
+    }
+    compute(cur);
+    if (s + 1 < n_st) {
+      sx.commit(tid, nxt);
+      sy.commit(tid, nxt + XU);
+    }
+  }
+
+  if constexpr (MODE == kAdapt) {
+    // The low-rank part: for each adapter that rows of this tile name, one
+    // more run of k, added to those rows only (another adapter's infinities
+    // must not meet them, not even as products with zero).  H is fp32; in bf16 it enters as the sum of its leading
+    // two (bf16 Out) or three (fp32 Out) bf16 parts, each a run of the ranks
+    // padded to 8, so the product keeps H to 2^-16 (2^-24) of itself, below
+    // the rounding of Out.
+    constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
+    const int Nlp = (ad.Nl + 7) & ~7;
+    const T* const B = reinterpret_cast<const T*>(ad.B);
+    int id_of[NJ];  // adapter of this lane's row in each block of 16
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      id_of[j] = ad.ids[t.n0 + min(wn * (TN / WN) + 16 * j + (lane & 15), n_valid - 1)];
+    int last = -1;
+    for (;;) {
+      // the least adapter above the last one
+      int next = 0x7fffffff;
+      for (int n = lane; n < n_valid; n += 64) {
+        const int id = ad.ids[t.n0 + n];
+        if (id > last && id < ad.Na) next = min(next, id);
+      }
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) next = min(next, __shfl_xor(next, d));
+      next = __builtin_amdgcn_readfirstlane(next);
+      if (next == 0x7fffffff) break;
+      last = next;
+      const T* const Ba = B + (int64_t)next * a.M * ad.Nl;
+      for (int k0 = 0; k0 < PARTS * Nlp; k0 += TK) {
+        __syncthreads();  // every wave is done with the buffers
+        for (int u = tid; u < XU; u += NT) {
+          constexpr int CE = 16 / (int)sizeof(T);
+          const int r = u >> 3, c = unit_at<T, true, TM>(r, u & 7) - r * 8;
+          const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
+          const int valid = r < m_valid && part < PARTS ? ad.Nl - rk : 0;
+          buf0[u] = load_unit(Ba + (int64_t)(m0 + r) * ad.Nl + rk, valid);
+        }
+        for (int u = tid; u < YU; u += NT) {
+          constexpr int CE = 16 / (int)sizeof(T);
+          const int r = u >> 3, c = unit_at<T, true, TN>(r, u & 7) - r * 8;
+          const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
+          const bool ok = r < n_valid && part < PARTS;
+          float h[CE];
+#pragma unroll
+          for (int e = 0; e < CE; ++e) {
+            h[e] = 0.f;
+            if (ok && rk + e < ad.Nl)
+              h[e] = ad.H[(int64_t)(t.n0 + r) * ad.Nl + rk + e] * (ad.scales ? ad.scales[next] : 1.f);
+          }
+          u32x4_t v;
+          if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(h[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p0 = bf16_part(h[2 * e], part), p1 = bf16_part(h[2 * e + 1], part);
+              v[e] = (__float_as_uint(p0) >> 16) | (__float_as_uint(p1) & 0xffff0000u);
+            }
+          }
+          buf0[XU + u] = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          f32x4_t part[NI];
+#pragma unroll
+          for (int i = 0; i < NI; ++i) part[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4_t yf = read_frag<T, true, TN>(buf0 + XU, wn * (TN / WN) + 16 * j, ks, lane);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+              part[i] = mma<T>(read_frag<T, true, TM>(buf0, wm * (TM / WM) + 16 * i, ks, lane), yf, part[i]);
+          }
+          if (id_of[j] == next)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) acc[i][j] += part[i];
+        }
+      }
+    }
+  }
+
+  // rows whose start lets four results be stored at once
+  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
+  const int l16 = lane & 15, G = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int n = wn * (TN / WN) + 16 * j + l16;
+    if (n < n_valid) {
+      // adapted rows go back to where they came from
+      const int64_t at = MODE == kAdapt ? (int64_t)rows[t.n0 + n] : (int64_t)n;
+      TO* const row = D + at * a.ldd;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        store4(row, m0 + wm * (TM / WM) + 16 * i + 4 * G, a.M, acc[i][j], whole);
+    }
+  }
+}
+
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>
+hipError_t launch_tiles(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
+                        hipStream_t stream) {
+  auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DMA>;
+  const int lds = 2 * 8 * (TM + TN) * 16;
+  if (lds > 64 * 1024) {
+    const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
+    if (e != hipSuccess) return e;
+  }
+  const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
+  k<<<dim3((uint32_t)grid), dim3(64 * WM * WN), lds, stream>>>(a, ad, band);
+  return hipGetLastError();
+}
+
+}  // namespace group
+}  // namespace cnnlib
