@@ -328,6 +328,181 @@ __device__ __forceinline__ float bf16_part(float h, int part) {
   return v;
 }
 
+// A workgroup's tile: its operands and result from the tile's (and, for the
+// gradient of Ker, the group's) start.
+template <typename T, typename TO> struct Tile {
+  const T* X;
+  const T* Y;
+  TO* D;
+  const int32_t* rows;  // NULL, or the source rows of grouped rows n0 .. or of k = 0 ..
+  int K, m0, m_valid, n0, n_valid;
+};
+
+template <typename T, typename TO, int MODE, int TM, int TN>
+__device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T, TO>* w) {
+  const int MT = (a.M + TM - 1) / TM;
+  w->X = reinterpret_cast<const T*>(a.X);
+  w->Y = reinterpret_cast<const T*>(a.Y);
+  w->D = reinterpret_cast<TO*>(a.D);
+  w->rows = a.rows;
+  int mt;
+  if constexpr (MODE == kBwdKer) {
+    const int NTL = (a.N + TN - 1) / TN;
+    const int L = xcd_remap(blockIdx.x, gridDim.x);
+    const int g = L / (MT * NTL);
+    const int j0 = L - g * MT * NTL;
+    const int b = j0 / (band * MT), rb = min(band, NTL - b * band), j = j0 - b * band * MT;
+    mt = j / rb;
+    w->n0 = (b * band + j % rb) * TN;
+    int lo, hi;
+    group_rows(a.off, a.Ng, a.K, g, &lo, &hi);
+    // clamped, so that no offset leads outside the tensors
+    lo = min(max(__builtin_amdgcn_readfirstlane(lo), 0), a.K);
+    w->K = min(max(__builtin_amdgcn_readfirstlane(hi), lo), a.K) - lo;
+    w->n_valid = min(a.N - w->n0, TN);
+    if (a.rows) w->rows += lo; else w->X += lo * a.ldx;
+    w->Y += lo * a.ldy;
+    w->D += g * a.dgroup + (int64_t)w->n0 * a.ldd;
+  } else {
+    RowTile t;
+    if (!find_tile<TN>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return false;
+    w->K = t.g < a.Ng ? a.K : 0;  // the rows past the last group: no products
+    w->n0 = t.n0;
+    w->n_valid = min(t.n1 - t.n0, TN);
+    w->X += (t.g < a.Ng ? t.g : 0) * a.xgroup;
+    // adapted rows go back to where they came from
+    if constexpr (MODE != kAdapt) w->D += (int64_t)t.n0 * a.ldd;
+    mt = t.mt;
+  }
+  w->m0 = mt * TM;
+  w->m_valid = min(a.M - w->m0, TM);
+  return true;
+}
+
+// Results acc[i][j] of 16 values of m from xrow(i) by 16 rows from yrow(j).
+// MASK: rows whose source row is not there are stored as zeros.
+template <typename T, typename TO, int MODE, bool MASK, int NI, int NJ, typename XR, typename YR>
+__device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>& w, int lane,
+                                           f32x4_t (&acc)[NI][NJ], XR xrow, YR yrow) {
+  const int l16 = lane & 15, m0 = w.m0 + 4 * (lane >> 4);
+  // rows whose starts and ends let every four results be stored at once
+  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0 && (a.M & 3) == 0;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int n = yrow(j) + l16;
+    if (n >= w.n_valid) continue;
+    int64_t at = n;
+    bool live = true;
+    if constexpr (MASK || MODE == kAdapt) {
+      if (w.rows) {
+        const int r = w.rows[w.n0 + n];
+        if constexpr (MODE == kAdapt) at = r;
+        live = r >= 0 && r < a.Nsrc;
+      }
+    }
+    TO* const row = w.D + at * a.ldd;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int m = m0 + xrow(i);
+      f32x4_t v = acc[i][j];
+      if constexpr (MASK)
+        if (!live) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (whole) {
+        if (m < a.M) store4(row, m, a.M, v, true);
+      } else {
+        store4(row, m, a.M, v, false);
+      }
+    }
+  }
+}
+
+// The low-rank part of an adapted tile, added to acc: for each adapter that
+// rows of the tile name, one more run of k, added to those rows only (another
+// adapter's infinities must not meet them, not even as products with zero).
+// H is fp32; in bf16 it enters as the sum of its leading two (bf16 Out) or
+// three (fp32 Out) bf16 parts, each a run of the ranks padded to 8, so the
+// product keeps H to 2^-16 (2^-24) of itself, below the rounding of Out.
+// buf: 8 (TM + TN) units that no wave uses any more after a barrier.
+template <typename T, typename TO, int TM, int TN, int NT, int NI, int NJ, typename XR, typename YR>
+__device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad,
+                                         const Tile<T, TO>& w, u32x4_t* buf, int tid,
+                                         f32x4_t (&acc)[NI][NJ], XR xrow, YR yrow) {
+  constexpr int CE = 16 / (int)sizeof(T), TK = 8 * CE;
+  constexpr int XU = 8 * TM, YU = 8 * TN;
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
+  const int lane = tid & 63;
+  const int Nlp = (ad.Nl + 7) & ~7;
+  const T* const B = reinterpret_cast<const T*>(ad.B);
+  int id_of[NJ];  // adapter of this lane's row in each block of 16
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+    id_of[j] = ad.ids[w.n0 + min(yrow(j) + (lane & 15), w.n_valid - 1)];
+  int last = -1;
+  for (;;) {
+    // the least adapter above the last one
+    int next = 0x7fffffff;
+    for (int n = lane; n < w.n_valid; n += 64) {
+      const int id = ad.ids[w.n0 + n];
+      if (id > last && id < ad.Na) next = min(next, id);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) next = min(next, __shfl_xor(next, d));
+    next = __builtin_amdgcn_readfirstlane(next);
+    if (next == 0x7fffffff) break;
+    last = next;
+    const T* const Ba = B + (int64_t)next * a.M * ad.Nl;
+    const float scale = ad.scales ? ad.scales[next] : 1.f;
+    for (int k0 = 0; k0 < PARTS * Nlp; k0 += TK) {
+      __syncthreads();  // every wave is done with the buffer
+      for (int u = tid; u < XU; u += NT) {
+        const int r = u >> 3, c = unit_at<T, true, TM>(r, u & 7) - r * 8;
+        const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
+        const int valid = r < w.m_valid && part < PARTS ? ad.Nl - rk : 0;
+        buf[u] = load_unit(Ba + (int64_t)(w.m0 + r) * ad.Nl + rk, valid);
+      }
+      for (int u = tid; u < YU; u += NT) {
+        const int r = u >> 3, c = unit_at<T, true, TN>(r, u & 7) - r * 8;
+        const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
+        const bool ok = r < w.n_valid && part < PARTS;
+        float h[CE];
+#pragma unroll
+        for (int e = 0; e < CE; ++e) {
+          h[e] = 0.f;
+          if (ok && rk + e < ad.Nl) h[e] = ad.H[(int64_t)(w.n0 + r) * ad.Nl + rk + e] * scale;
+        }
+        u32x4_t v;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(h[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = bf16_part(h[2 * e], part), p1 = bf16_part(h[2 * e + 1], part);
+            v[e] = (__float_as_uint(p0) >> 16) | (__float_as_uint(p1) & 0xffff0000u);
+          }
+        }
+        buf[XU + u] = v;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        u32x4_t yf[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) yf[ks] = read_frag<T, true, TN>(buf + XU, yrow(j), ks, lane);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          f32x4_t part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
+            part = mma<T>(read_frag<T, true, TM>(buf, xrow(i), ks, lane), yf[ks], part);
+          if (id_of[j] == next) acc[i][j] += part;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // not all rows' operands at once
+      }
+    }
+  }
+}
+
 // TM x TN results by WM x WN waves.  DMA: both operands by 16-byte copies to
 // LDS (16-byte aligned rows), else through registers.
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>
@@ -346,46 +521,16 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
-  const int MT = (a.M + TM - 1) / TM;
+  auto xrow = [&](int i) { return wm * (TM / WM) + 16 * i; };
+  auto yrow = [&](int j) { return wn * (TN / WN) + 16 * j; };
 
-  RowTile t;
-  const T* X = reinterpret_cast<const T*>(a.X);
-  const T* Y = reinterpret_cast<const T*>(a.Y);
-  TO* D = reinterpret_cast<TO*>(a.D);
-  const int32_t* rows = a.rows;
-  int K, n_rows;  // extent of k; valid rows of n in this tile
-  if constexpr (MODE == kBwdKer) {
-    const int NTL = (a.N + TN - 1) / TN;
-    const int L = xcd_remap(blockIdx.x, gridDim.x);
-    t.g = L / (MT * NTL);
-    const int j0 = L - t.g * MT * NTL;
-    const int b = j0 / (band * MT), rb = min(band, NTL - b * band), j = j0 - b * band * MT;
-    t.mt = j / rb;
-    t.n0 = (b * band + j % rb) * TN;
-    int lo, hi;
-    group_rows(a.off, a.Ng, a.K, t.g, &lo, &hi);
-    // clamped, so that no offset leads outside the tensors
-    lo = min(max(__builtin_amdgcn_readfirstlane(lo), 0), a.K);
-    K = min(max(__builtin_amdgcn_readfirstlane(hi), lo), a.K) - lo;
-    n_rows = a.N - t.n0;
-    if (rows) rows += lo; else X += lo * a.ldx;
-    Y += lo * a.ldy;
-    D += t.g * a.dgroup + (int64_t)t.n0 * a.ldd;
-  } else {
-    if (!find_tile<TN>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return;
-    K = t.g < a.Ng ? a.K : 0;  // the rows past the last group: no products
-    n_rows = t.n1 - t.n0;
-    X += (t.g < a.Ng ? t.g : 0) * a.xgroup;
-    if constexpr (MODE != kAdapt) D += (int64_t)t.n0 * a.ldd;
-  }
-  const int m0 = t.mt * TM;
-  const int n_valid = min(n_rows, TN), m_valid = min(a.M - m0, TM);
-
+  Tile<T, TO> w;
+  if (!setup_tile<T, TO, MODE, TM, TN>(a, band, &w)) return;
   Stager<T, XKC, TM, NT, DMA, XG> sx;
   Stager<T, YKC, TN, NT, DMA, YG> sy;
-  sx.init(tid, X, a.ldx, m0, m_valid, K, nullptr, 0);
-  sy.init(tid, Y, a.ldy, t.n0, n_valid, K, YG ? rows : nullptr, a.Nsrc);
-  const int32_t* const xrows = XG ? rows : nullptr;
+  sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, w.K, nullptr, 0);
+  sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, w.K, YG ? w.rows : nullptr, a.Nsrc);
+  const int32_t* const xrows = XG ? w.rows : nullptr;
 
   f32x4_t acc[NI][NJ];
 #pragma unroll
@@ -398,11 +543,9 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
     for (int ks = 0; ks < KS; ++ks) {
       u32x4_t xf[NI], yf[NJ];
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
-        xf[i] = read_frag<T, XKC, TM>(buf, wm * (TM / WM) + 16 * i, ks, lane);
+      for (int i = 0; i < NI; ++i) xf[i] = read_frag<T, XKC, TM>(buf, xrow(i), ks, lane);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        yf[j] = read_frag<T, YKC, TN>(buf + XU, wn * (TN / WN) + 16 * j, ks, lane);
+      for (int j = 0; j < NJ; ++j) yf[j] = read_frag<T, YKC, TN>(buf + XU, yrow(j), ks, lane);
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -410,10 +553,10 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
     }
   };
 
-  const int n_st = (K + TK - 1) / TK;
+  const int n_st = (w.K + TK - 1) / TK;
   if (n_st > 0) {
-    sx.issue(tid, buf0, 0, a.ldx, K, xrows, a.Nsrc);
-    sy.issue(tid, buf0 + XU, 0, a.ldy, K, nullptr, 0);
+    sx.issue(tid, buf0, 0, a.ldx, w.K, xrows, a.Nsrc);
+    sy.issue(tid, buf0 + XU, 0, a.ldy, w.K, nullptr, 0);
     sx.commit(tid, buf0);
     sy.commit(tid, buf0 + XU);
   }
@@ -423,8 +566,8 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
     // this stage has landed and every wave is done with the other buffer
     __syncthreads();
     if (s + 1 < n_st) {
-      sx.issue(tid, nxt, (s + 1) * TK, a.ldx, K, xrows, a.Nsrc);
-      sy.issue(tid, nxt + XU, (s + 1) * TK, a.ldy, K, nullptr, 0);
+      sx.issue(tid, nxt, (s + 1) * TK, a.ldx, w.K, xrows, a.Nsrc);
+      sy.issue(tid, nxt + XU, (s + 1) * TK, a.ldy, w.K, nullptr, 0);
     }
     compute(cur);
     if (s + 1 < n_st) {
@@ -432,105 +575,9 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
       sy.commit(tid, nxt + XU);
     }
   }
-
-  if constexpr (MODE == kAdapt) {
-    // The low-rank part: for each adapter that rows of this tile name, one
-    // more run of k, added to those rows only (another adapter's infinities
-    // must not meet them, not even as products with zero).  H is fp32; in bf16 it enters as the sum of its leading
-    // two (bf16 Out) or three (fp32 Out) bf16 parts, each a run of the ranks
-    // padded to 8, so the product keeps H to 2^-16 (2^-24) of itself, below
-    // the rounding of Out.
-    constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
-    const int Nlp = (ad.Nl + 7) & ~7;
-    const T* const B = reinterpret_cast<const T*>(ad.B);
-    int id_of[NJ];  // adapter of this lane's row in each block of 16
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-      id_of[j] = ad.ids[t.n0 + min(wn * (TN / WN) + 16 * j + (lane & 15), n_valid - 1)];
-    int last = -1;
-    for (;;) {
-      // the least adapter above the last one
-      int next = 0x7fffffff;
-      for (int n = lane; n < n_valid; n += 64) {
-        const int id = ad.ids[t.n0 + n];
-        if (id > last && id < ad.Na) next = min(next, id);
-      }
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) next = min(next, __shfl_xor(next, d));
-      next = __builtin_amdgcn_readfirstlane(next);
-      if (next == 0x7fffffff) break;
-      last = next;
-      const T* const Ba = B + (int64_t)next * a.M * ad.Nl;
-      for (int k0 = 0; k0 < PARTS * Nlp; k0 += TK) {
-        __syncthreads();  // every wave is done with the buffers
-        for (int u = tid; u < XU; u += NT) {
-          constexpr int CE = 16 / (int)sizeof(T);
-          const int r = u >> 3, c = unit_at<T, true, TM>(r, u & 7) - r * 8;
-          const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
-          const int valid = r < m_valid && part < PARTS ? ad.Nl - rk : 0;
-          buf0[u] = load_unit(Ba + (int64_t)(m0 + r) * ad.Nl + rk, valid);
-        }
-        for (int u = tid; u < YU; u += NT) {
-          constexpr int CE = 16 / (int)sizeof(T);
-          const int r = u >> 3, c = unit_at<T, true, TN>(r, u & 7) - r * 8;
-          const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
-          const bool ok = r < n_valid && part < PARTS;
-          float h[CE];
-#pragma unroll
-          for (int e = 0; e < CE; ++e) {
-            h[e] = 0.f;
-            if (ok && rk + e < ad.Nl)
-              h[e] = ad.H[(int64_t)(t.n0 + r) * ad.Nl + rk + e] * (ad.scales ? ad.scales[next] : 1.f);
-          }
-          u32x4_t v;
-          if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(h[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p0 = bf16_part(h[2 * e], part), p1 = bf16_part(h[2 * e + 1], part);
-              v[e] = (__float_as_uint(p0) >> 16) | (__float_as_uint(p1) & 0xffff0000u);
-            }
-          }
-          buf0[XU + u] = v;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          f32x4_t part[NI];
-#pragma unroll
-          for (int i = 0; i < NI; ++i) part[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const u32x4_t yf = read_frag<T, true, TN>(buf0 + XU, wn * (TN / WN) + 16 * j, ks, lane);
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-              part[i] = mma<T>(read_frag<T, true, TM>(buf0, wm * (TM / WM) + 16 * i, ks, lane), yf, part[i]);
-          }
-          if (id_of[j] == next)
-#pragma unroll
-            for (int i = 0; i < NI; ++i) acc[i][j] += part[i];
-        }
-      }
-    }
-  }
-
-  // rows whose start lets four results be stored at once
-  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
-  const int l16 = lane & 15, G = lane >> 4;
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int n = wn * (TN / WN) + 16 * j + l16;
-    if (n < n_valid) {
-      // adapted rows go back to where they came from
-      const int64_t at = MODE == kAdapt ? (int64_t)rows[t.n0 + n] : (int64_t)n;
-      TO* const row = D + at * a.ldd;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-        store4(row, m0 + wm * (TM / WM) + 16 * i + 4 * G, a.M, acc[i][j], whole);
-    }
-  }
+  if constexpr (MODE == kAdapt)
+    low_rank<T, TO, TM, TN, NT>(a, ad, w, buf0, tid, acc, xrow, yrow);
+  store_tile<T, TO, MODE, false>(a, w, lane, acc, xrow, yrow);
 }
 
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>

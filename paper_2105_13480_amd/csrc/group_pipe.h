@@ -1,0 +1,341 @@
+// The pipelined tile kernel of the grouped products: 256 x 256 results of
+// bf16 operands with 16-byte aligned rows.
+//
+// Eight waves of 128 (m) x 64 (n) results, two on each SIMD.  A stage is 64 of
+// k: 64 KB of LDS in four halves (128 rows of Y, 128 of X, the other 128 of
+// each), two stages in LDS.  A wave's results are four quarters, one per half
+// of X and of Y, and a stage is four phases of one quarter, 16 MFMAs:
+//   phase  reads from LDS       copies (two stages ahead)   products
+//     0    X half 0             Y half 0                    X0 Y0
+//     1    Y half 1             X half 0                    X0 Y1
+//     2    X half 1             Y half 1                    X1 Y1
+//     3    Y half 0 (next)      X half 1                    X1 Y0
+// so that no phase reads more than its products take (8 or 4 KB a wave at 128
+// bytes a clock against 256 clocks).  A phase is two slots between barriers,
+// memory then products; waves 4 to 7 run one slot behind waves 0 to 3, so on
+// each SIMD one wave feeds the matrix unit while the other reads.  A half is
+// copied over as soon as the later waves have read it, six phases before it
+// is read: every memory slot waits for all but its wave's last 12 copies
+// (copies beyond the end of k read zeros, so the count always holds).
+#pragma once
+
+#include "group_kernel.h"
+
+namespace cnnlib {
+namespace group {
+
+constexpr int kPipeHalf = 1024;                  // units of a half: 128 rows of 64 of k
+constexpr int kPipeRows = 4096;                  // source rows kept in LDS (gathered k)
+constexpr int kPipeLds = 8 * kPipeHalf * 16;     // two stages
+enum Half { kY0 = 0, kX0 = 1, kY1 = 2, kX1 = 3 };
+
+// Eight (NB = 2) or sixteen (NB = 4) transposing reads of the operands of NB
+// blocks of 16 tile rows, whose addresses are p[i]: for each 32 values of k
+// (8 KB apart) rows of k 0..3 and 4..7 (1 KB apart) of each 16 lanes.  One
+// block that also waits for them, so the values are defined when it ends and
+// the compiler adds no wait for the copies in flight.
+__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[2], u32x4_t (&f)[2][2]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  u32x2_t r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:9216\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:9216\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
+        "=&v"(r[7])
+      : "v"(p[0]), "v"(p[1])
+      : "memory");
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x2_t lo = r[4 * ks + 2 * i], hi = r[4 * ks + 2 * i + 1];
+      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    }
+#else
+  (void)p;
+  (void)f;
+#endif
+}
+__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[4], u32x4_t (&f)[4][2]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  u32x2_t r[16];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n\t"
+      "ds_read_b64_tr_b16 %1, %16 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %17\n\t"
+      "ds_read_b64_tr_b16 %3, %17 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %4, %18\n\t"
+      "ds_read_b64_tr_b16 %5, %18 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %6, %19\n\t"
+      "ds_read_b64_tr_b16 %7, %19 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %8, %16 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %9, %16 offset:9216\n\t"
+      "ds_read_b64_tr_b16 %10, %17 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %11, %17 offset:9216\n\t"
+      "ds_read_b64_tr_b16 %12, %18 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %13, %18 offset:9216\n\t"
+      "ds_read_b64_tr_b16 %14, %19 offset:8192\n\t"
+      "ds_read_b64_tr_b16 %15, %19 offset:9216\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
+        "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]),
+        "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+      : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
+      : "memory");
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2_t lo = r[8 * ks + 2 * i], hi = r[8 * ks + 2 * i + 1];
+      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    }
+#else
+  (void)p;
+  (void)f;
+#endif
+}
+
+// One operand: its copies to LDS and its reads from there.  KC: k last, rows
+// may be gathered; else the tile's own index last, rows of k may be gathered.
+// NB: blocks of 16 rows a wave reads from each half.
+template <bool KC, bool GATHER, int NB> struct PipeOperand {
+  const bf16_t* base;   // tile start (not gathered KC: of its first row)
+  const bf16_t* p[KC && GATHER ? 4 : 1];
+  uint32_t off[KC ? 4 : 2];  // bytes from base: rows half * 128 + j * 64 + tid / 8 | columns of a half
+  int c8;               // KC: first k of this thread's unit within a stage
+  int64_t ld;
+  uint32_t frag[KC ? 2 : NB];  // LDS bytes within a half, KC: of each 32 of k
+
+  // n: rows of the tile index that are there; index: source rows, if gathered.
+  __device__ __forceinline__ void init(int tid, const bf16_t* b, int64_t i0, int n, int64_t ld_,
+                                       const int32_t* index, int nsrc, int row0, int lane) {
+    ld = ld_;
+    const int l16 = lane & 15, G = lane >> 4;
+    if constexpr (KC) {
+      const int r0 = tid >> 3;
+      c8 = 8 * ((tid & 7) ^ ((r0 >> 1) & 7));
+      base = b + i0 * ld;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        // a row that is not there reads one that is: its results are not stored
+        const int r = min(h * 64 + r0, n - 1);
+        if constexpr (GATHER) {
+          int64_t row = index ? (int64_t)index[i0 + r] : i0 + r;
+          if (row < 0 || row >= nsrc) row = 0;  // zeroed when stored
+          p[h] = b + row * ld + c8;
+          off[h] = 0;
+        } else {
+          off[h] = (uint32_t)((r * ld + c8) * 2);
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+        frag[ks] = (uint32_t)(((row0 + l16) * 8 + ((4 * ks + G) ^ ((l16 >> 1) & 7))) * 16);
+    } else {
+      const int k = tid >> 4, g = (k & 3) | ((k >> 1) & 4);
+      const int c = (tid & 15) ^ (g << 1);
+      base = b + i0;
+      c8 = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int col = h * 128 + 8 * c;
+        off[h] = (uint32_t)(((GATHER && index ? 0 : k * ld) + (col < n ? col : 0)) * 2);
+      }
+      const int gr = (l16 >> 2) | ((G & 1) << 2);
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        frag[i] = (uint32_t)((8 * G + (l16 >> 2)) * 256 + ((((row0 >> 4) + i) ^ gr) << 5) +
+                             (l16 & 3) * 8);
+    }
+  }
+
+  // The two copies of half `h` of the stage at k0 into dst (this wave's part).
+  // idx: LDS copy of the source rows from k = 0 on (gathered rows of k).
+  __device__ __forceinline__ void copy(int tid, int h, int k0, int K, u32x4_t* dst,
+                                       const int32_t* idx, int nsrc) const {
+    const bool full = k0 + 64 <= K;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const char* src;
+      if constexpr (KC) {
+        src = GATHER ? reinterpret_cast<const char*>(p[2 * h + j] + k0)
+                     : reinterpret_cast<const char*>(base + k0) + off[2 * h + j];
+        if (!full && k0 + c8 >= K) src = reinterpret_cast<const char*>(zero_unit);
+      } else {
+        const int k = k0 + 32 * j + (tid >> 4);
+        if (GATHER && idx) {
+          const int row = idx[min(k, K - 1)];
+          const bool ok = k < K && row >= 0 && row < nsrc;
+          src = ok ? reinterpret_cast<const char*>(base + row * ld) + off[h]
+                   : reinterpret_cast<const char*>(zero_unit);
+        } else {
+          src = reinterpret_cast<const char*>(base + (int64_t)(k0 + 32 * j) * ld) + off[h];
+          if (!full && k >= K) src = reinterpret_cast<const char*>(zero_unit);
+        }
+      }
+      copy16_lds(src, dst + 512 * j);
+    }
+  }
+
+  __device__ __forceinline__ void read(uint32_t half, u32x4_t (&f)[NB][2]) const {
+    if constexpr (KC) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+          f[i][ks] = *(const __attribute__((address_space(3))) u32x4_t*)(half + frag[ks] + 2048 * i);
+    } else {
+      uint32_t q[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) q[i] = half + frag[i];
+      read_tr_blocks(q, f);
+    }
+  }
+};
+
+template <typename TO, int MODE>
+__global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, int band) {
+  typedef bf16_t T;
+  constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
+  constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE == kAdapt;
+
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  u32x4_t* const lds = reinterpret_cast<u32x4_t*>(smem);
+  int32_t* const idx = reinterpret_cast<int32_t*>(smem + kPipeLds);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int late = wave >> 2;  // one slot behind
+  const int wm = wave >> 2, wn = wave & 3;
+  auto xrow = [&](int i) { return (i >> 2) * 128 + wm * 64 + 16 * (i & 3); };
+  auto yrow = [&](int j) { return (j >> 1) * 128 + wn * 32 + 16 * (j & 1); };
+
+  Tile<T, TO> w;
+  if (!setup_tile<T, TO, MODE, 256, 256>(a, band, &w)) return;
+
+  f32x4_t acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  const bool gather_k = XG && w.rows;
+  PipeOperand<XKC, XG, 4> X;
+  PipeOperand<YKC, YG, 2> Y;
+
+  // Runs of k: all of it, but for gathered rows of k as many as LDS holds.
+  for (int kb = 0; kb < w.K; kb += kPipeRows) {
+    const int K = gather_k ? min(w.K - kb, kPipeRows) : w.K;
+    if (gather_k) {
+      __syncthreads();  // every wave is done with the last run's rows
+      for (int i = tid; i < K; i += 512) idx[i] = w.rows[kb + i];
+      __syncthreads();
+    }
+    X.init(tid, w.X, w.m0, w.m_valid, a.ldx, gather_k ? w.rows : nullptr, 0, wm * 64, lane);
+    Y.init(tid, w.Y + (gather_k ? kb * a.ldy : 0), w.n0, w.n_valid, a.ldy, YG ? w.rows : nullptr,
+           a.Nsrc, wn * 32, lane);
+    const int32_t* const xidx = gather_k ? idx : nullptr;
+
+    auto half_units = [&](int s, int h) { return lds + ((s & 1) * 4 + h) * kPipeHalf + 64 * wave; };
+    auto half_bytes = [&](int s, int h) { return lds0 + (uint32_t)(((s & 1) * 4 + h) * kPipeHalf * 16); };
+    auto copy_x = [&](int s, int h) __attribute__((always_inline)) {
+      X.copy(tid, h, 64 * s, K, half_units(s, h ? kX1 : kX0), xidx, a.Nsrc);
+    };
+    auto copy_y = [&](int s, int h) __attribute__((always_inline)) {
+      Y.copy(tid, h, 64 * s, K, half_units(s, h ? kY1 : kY0), nullptr, 0);
+    };
+    auto landed = [&]() __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    u32x4_t xf[4][2], y0[2][2], y1[2][2];
+    auto products = [&](int hm, int hn, const u32x4_t(&yf)[2][2]) __attribute__((always_inline)) {
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[4 * hm + i][2 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    const int n_st = (K + 63) / 64;
+    for (int s = 0; s < 2; ++s) {
+      copy_y(s, 0);
+      copy_x(s, 0);
+      copy_y(s, 1);
+      copy_x(s, 1);
+    }
+    landed();
+    Y.read(half_bytes(0, kY0), y0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    if (late) barrier();
+    for (int s = 0; s < n_st; ++s) {
+      X.read(half_bytes(s, kX0), xf);
+      copy_y(s + 2, 0);
+      landed();
+      products(0, 0, y0);
+      barrier();
+      Y.read(half_bytes(s, kY1), y1);
+      copy_x(s + 2, 0);
+      landed();
+      products(0, 1, y1);
+      barrier();
+      X.read(half_bytes(s, kX1), xf);
+      copy_y(s + 2, 1);
+      landed();
+      products(1, 1, y1);
+      barrier();
+      u32x4_t y0n[2][2];
+      Y.read(half_bytes(s + 1, kY0), y0n);
+      copy_x(s + 2, 1);
+      landed();
+      products(1, 0, y0);
+      barrier();
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) y0[j][ks] = y0n[j][ks];
+    }
+    if (!late) barrier();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
+    if (!gather_k) break;
+  }
+
+  if constexpr (MODE == kAdapt)
+    low_rank<T, TO, 256, 256, 512>(a, ad, w, lds, tid, acc, xrow, yrow);
+  store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
+}
+
+// Whether the byte offsets of a tile's rows fit the kernel's 32 bits.
+inline bool pipe_fits(const GroupArgs& a) { return a.ldx < (1 << 22) && a.ldy < (1 << 22); }
+
+template <typename TO, int MODE>
+hipError_t launch_pipe(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
+                       hipStream_t stream) {
+  auto* const k = group_pipe<TO, MODE>;
+  const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
+  if (e != hipSuccess) return e;
+  const int64_t grid = row_tiles * ((a.M + 255) / 256);
+  const int lds = kPipeLds + (MODE == kBwdKer && a.rows ? kPipeRows * 4 : 0);
+  k<<<dim3((uint32_t)grid), dim3(512), lds, stream>>>(a, ad, band);
+  return hipGetLastError();
+}
+
+}  // namespace group
+}  // namespace cnnlib

@@ -1,5 +1,5 @@
 // Launches of the grouped products' tile kernel (group_kernel.h).
-#include "group_kernel.h"
+#include "group_pipe.h"
 
 namespace cnnlib {
 
@@ -21,12 +21,20 @@ int64_t row_tiles(int64_t Np, int64_t Ng, bool groups, int TN) {
   return Np / TN + parts;
 }
 
+// Row tiles of TN rows of a launch.
+template <int MODE> int64_t row_tiles_of(const GroupArgs& a, int TN) {
+  if (MODE == kBwdKer) return (int64_t)a.Ng * ((a.N + TN - 1) / TN);
+  return row_tiles(a.N, a.Ng, MODE != kAdapt, TN);
+}
+
 template <typename T, typename TO, int MODE, bool DMA>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
-  const bool groups = MODE != kAdapt;
-  const int64_t n = MODE == kBwdKer ? a.N : row_tiles(a.N, a.Ng, groups, 128);
-  const int64_t rt = MODE == kBwdKer ? (int64_t)a.Ng * ((a.N + 127) / 128) : n;
-  return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA>(a, ad, rt, 8, stream);
+  if constexpr (sizeof(T) == 2 && DMA) {
+    const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
+    if (rows >= 192 && a.M >= 192 && pipe_fits(a))
+      return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
+  }
+  return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
 }
 
 template <typename T, typename TO, int MODE>
