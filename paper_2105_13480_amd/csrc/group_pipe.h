@@ -5,19 +5,23 @@
 // k: 64 KB of LDS in four halves (128 rows of Y, 128 of X, the other 128 of
 // each), two stages in LDS.  A wave's results are four quarters, one per half
 // of X and of Y, and a stage is four phases of one quarter, 16 MFMAs:
-//   phase  reads from LDS       copies (two stages ahead)   products
-//     0    X half 0             Y half 0                    X0 Y0
-//     1    Y half 1             X half 0                    X0 Y1
-//     2    X half 1             Y half 1                    X1 Y1
-//     3    Y half 0 (next)      X half 1                    X1 Y0
+//   phase  reads from LDS       copies              products
+//     0    X half 0             X half 1 of s + 1   X0 Y0
+//     1    Y half 1             Y half 0 of s + 2   X0 Y1
+//     2    X half 1             X half 0 of s + 2   X1 Y1
+//     3    Y half 0 of s + 1    Y half 1 of s + 2   X1 Y0
 // so that no phase reads more than its products take (8 or 4 KB a wave at 128
 // bytes a clock against 256 clocks).  A phase is two slots between barriers,
 // memory then products; waves 4 to 7 run one slot behind waves 0 to 3, so on
-// each SIMD one wave feeds the matrix unit while the other reads.  A half is
-// copied over as soon as the later waves have read it, six phases before it
-// is read: every memory slot waits for all but its wave's last 12 copies
-// (copies beyond the end of k read zeros, so the count always holds).
+// each SIMD one wave feeds the matrix unit while the other reads.  A wave's
+// reads are done by the end of its products slot, which the later waves end
+// two slots after the earlier ones began to read: from the second phase after
+// a read on, the half may be copied over.  That is six phases before it is
+// read again, so every memory slot waits for all but its wave's last ten
+// copies (copies beyond the end of k read zeros: the count always holds).
 #pragma once
+
+#include <type_traits>
 
 #include "group_kernel.h"
 
@@ -106,38 +110,37 @@ __device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[4], u32x4_t (
 // may be gathered; else the tile's own index last, rows of k may be gathered.
 // NB: blocks of 16 rows a wave reads from each half.
 template <bool KC, bool GATHER, int NB> struct PipeOperand {
-  const bf16_t* base;   // tile start (not gathered KC: of its first row)
-  const bf16_t* p[KC && GATHER ? 4 : 1];
+  const bf16_t* base;   // the tensor, or the tile's start
   uint32_t off[KC ? 4 : 2];  // bytes from base: rows half * 128 + j * 64 + tid / 8 | columns of a half
   int c8;               // KC: first k of this thread's unit within a stage
   int64_t ld;
-  uint32_t frag[KC ? 2 : NB];  // LDS bytes within a half, KC: of each 32 of k
+  uint32_t frag[KC ? 2 : 1][KC ? 2 : NB];  // LDS bytes in half 0; KC: of each stage, each 32 of k
 
   // n: rows of the tile index that are there; index: source rows, if gathered.
   __device__ __forceinline__ void init(int tid, const bf16_t* b, int64_t i0, int n, int64_t ld_,
-                                       const int32_t* index, int nsrc, int row0, int lane) {
+                                       const int32_t* index, int nsrc, int row0, int lane,
+                                       uint32_t lds) {
     ld = ld_;
     const int l16 = lane & 15, G = lane >> 4;
     if constexpr (KC) {
       const int r0 = tid >> 3;
       c8 = 8 * ((tid & 7) ^ ((r0 >> 1) & 7));
-      base = b + i0 * ld;
+      base = GATHER && index ? b : b + i0 * ld;
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        // a row that is not there reads one that is: its results are not stored
-        const int r = min(h * 64 + r0, n - 1);
-        if constexpr (GATHER) {
-          int64_t row = index ? (int64_t)index[i0 + r] : i0 + r;
-          if (row < 0 || row >= nsrc) row = 0;  // zeroed when stored
-          p[h] = b + row * ld + c8;
-          off[h] = 0;
-        } else {
-          off[h] = (uint32_t)((r * ld + c8) * 2);
-        }
+        // a row that is not there reads one that is: its results are not
+        // stored, or (no source row) stored as zeros
+        int64_t r = min(h * 64 + r0, n - 1);
+        if constexpr (GATHER)
+          if (index) {
+            r = index[i0 + r];
+            if (r < 0 || r >= nsrc) r = 0;
+          }
+        off[h] = (uint32_t)((r * ld + c8) * 2);
       }
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
-        frag[ks] = (uint32_t)(((row0 + l16) * 8 + ((4 * ks + G) ^ ((l16 >> 1) & 7))) * 16);
+        frag[0][ks] = lds + (uint32_t)(((row0 + l16) * 8 + ((4 * ks + G) ^ ((l16 >> 1) & 7))) * 16);
     } else {
       const int k = tid >> 4, g = (k & 3) | ((k >> 1) & 4);
       const int c = (tid & 15) ^ (g << 1);
@@ -151,50 +154,53 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
       const int gr = (l16 >> 2) | ((G & 1) << 2);
 #pragma unroll
       for (int i = 0; i < NB; ++i)
-        frag[i] = (uint32_t)((8 * G + (l16 >> 2)) * 256 + ((((row0 >> 4) + i) ^ gr) << 5) +
-                             (l16 & 3) * 8);
+        frag[0][i] = lds + (uint32_t)((8 * G + (l16 >> 2)) * 256 + ((((row0 >> 4) + i) ^ gr) << 5) +
+                                      (l16 & 3) * 8);
     }
+    if constexpr (KC)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) frag[1][ks] = frag[0][ks] + 4 * kPipeHalf * 16;
   }
 
   // The two copies of half `h` of the stage at k0 into dst (this wave's part).
-  // idx: LDS copy of the source rows from k = 0 on (gathered rows of k).
-  __device__ __forceinline__ void copy(int tid, int h, int k0, int K, u32x4_t* dst,
-                                       const int32_t* idx, int nsrc) const {
-    const bool full = k0 + 64 <= K;
+  // CHECK: the stage may reach past K.  idx: bytes from base of the rows of k
+  // this thread copies (~0: none), if they are gathered.
+  template <bool CHECK>
+  __device__ __forceinline__ void copy(int tid, int h, int k0, int K, u32x4_t* dst, bool gathered,
+                                       const uint32_t (&idx)[2]) const {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const char* src;
+      bool ok = true;
       if constexpr (KC) {
-        src = GATHER ? reinterpret_cast<const char*>(p[2 * h + j] + k0)
-                     : reinterpret_cast<const char*>(base + k0) + off[2 * h + j];
-        if (!full && k0 + c8 >= K) src = reinterpret_cast<const char*>(zero_unit);
+        src = reinterpret_cast<const char*>(base + k0) + off[2 * h + j];
+        if constexpr (CHECK) ok = k0 + c8 < K;
+      } else if (GATHER && gathered) {
+        src = reinterpret_cast<const char*>(base) + idx[j] + off[h];
+        ok = idx[j] != ~0u;
       } else {
-        const int k = k0 + 32 * j + (tid >> 4);
-        if (GATHER && idx) {
-          const int row = idx[min(k, K - 1)];
-          const bool ok = k < K && row >= 0 && row < nsrc;
-          src = ok ? reinterpret_cast<const char*>(base + row * ld) + off[h]
-                   : reinterpret_cast<const char*>(zero_unit);
-        } else {
-          src = reinterpret_cast<const char*>(base + (int64_t)(k0 + 32 * j) * ld) + off[h];
-          if (!full && k >= K) src = reinterpret_cast<const char*>(zero_unit);
-        }
+        src = reinterpret_cast<const char*>(base + (int64_t)(k0 + 32 * j) * ld) + off[h];
+        if constexpr (CHECK) ok = k0 + 32 * j + (tid >> 4) < K;
       }
+      if (CHECK || (GATHER && !KC))
+        src = ok ? src : reinterpret_cast<const char*>(zero_unit);
       copy16_lds(src, dst + 512 * j);
     }
   }
 
-  __device__ __forceinline__ void read(uint32_t half, u32x4_t (&f)[NB][2]) const {
+  template <int PAR> __device__ __forceinline__ void read(uint32_t half, u32x4_t (&f)[NB][2]) const {
     if constexpr (KC) {
+      typedef const __attribute__((address_space(3))) char* lds_ptr;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int i = 0; i < NB; ++i)
-          f[i][ks] = *(const __attribute__((address_space(3))) u32x4_t*)(half + frag[ks] + 2048 * i);
+          f[i][ks] = *(const __attribute__((address_space(3))) u32x4_t*)(
+              (lds_ptr)frag[PAR][ks] + (half + 2048 * i));
     } else {
       uint32_t q[NB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) q[i] = half + frag[i];
+      for (int i = 0; i < NB; ++i) q[i] = frag[0][i] + (PAR * 4 * kPipeHalf * 16 + half);
       read_tr_blocks(q, f);
     }
   }
@@ -208,8 +214,7 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
 
   extern __shared__ __attribute__((aligned(16))) char smem[];
   u32x4_t* const lds = reinterpret_cast<u32x4_t*>(smem);
-  int32_t* const idx = reinterpret_cast<int32_t*>(smem + kPipeLds);
-  const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
+  uint32_t* const idx = reinterpret_cast<uint32_t*>(smem + kPipeLds);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int late = wave >> 2;  // one slot behind
@@ -229,38 +234,50 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
   const bool gather_k = XG && w.rows;
   PipeOperand<XKC, XG, 4> X;
   PipeOperand<YKC, YG, 2> Y;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
 
   // Runs of k: all of it, but for gathered rows of k as many as LDS holds.
   for (int kb = 0; kb < w.K; kb += kPipeRows) {
     const int K = gather_k ? min(w.K - kb, kPipeRows) : w.K;
     if (gather_k) {
       __syncthreads();  // every wave is done with the last run's rows
-      for (int i = tid; i < K; i += 512) idx[i] = w.rows[kb + i];
+      for (int i = tid; i < kPipeRows + 192; i += 512) {
+        const int r = i < K ? w.rows[kb + i] : -1;
+        idx[i] = r >= 0 && r < a.Nsrc ? (uint32_t)(r * a.ldx * 2) : ~0u;
+      }
       __syncthreads();
     }
-    X.init(tid, w.X, w.m0, w.m_valid, a.ldx, gather_k ? w.rows : nullptr, 0, wm * 64, lane);
+    X.init(tid, w.X, w.m0, w.m_valid, a.ldx, gather_k ? w.rows : nullptr, 0, wm * 64, lane, lds0);
     Y.init(tid, w.Y + (gather_k ? kb * a.ldy : 0), w.n0, w.n_valid, a.ldy, YG ? w.rows : nullptr,
-           a.Nsrc, wn * 32, lane);
-    const int32_t* const xidx = gather_k ? idx : nullptr;
+           a.Nsrc, wn * 32, lane, lds0);
 
-    auto half_units = [&](int s, int h) { return lds + ((s & 1) * 4 + h) * kPipeHalf + 64 * wave; };
-    auto half_bytes = [&](int s, int h) { return lds0 + (uint32_t)(((s & 1) * 4 + h) * kPipeHalf * 16); };
-    auto copy_x = [&](int s, int h) __attribute__((always_inline)) {
-      X.copy(tid, h, 64 * s, K, half_units(s, h ? kX1 : kX0), xidx, a.Nsrc);
-    };
-    auto copy_y = [&](int s, int h) __attribute__((always_inline)) {
-      Y.copy(tid, h, 64 * s, K, half_units(s, h ? kY1 : kY0), nullptr, 0);
-    };
-    auto landed = [&]() __attribute__((always_inline)) {
-      asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto barrier = [&]() __attribute__((always_inline)) {
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_barrier" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
     u32x4_t xf[4][2], y0[2][2], y1[2][2];
+    uint32_t xi[2] = {0, 0};
+    const uint32_t none[2] = {0, 0};
+    auto fetch_rows = [&](int s) __attribute__((always_inline)) {
+      if (XG && gather_k) {
+        xi[0] = idx[64 * s + (tid >> 4)];
+        xi[1] = idx[64 * s + 32 + (tid >> 4)];
+      }
+    };
+    auto half_units = [&](int par, int h) { return lds + (par * 4 + h) * kPipeHalf + 64 * wave; };
+    auto copy_x = [&](auto par, auto check, int s, int h) __attribute__((always_inline)) {
+      X.template copy<check.value>(tid, h, 64 * s, K, half_units(par.value, h ? kX1 : kX0), gather_k, xi);
+    };
+    auto copy_y = [&](auto par, auto check, int s, int h) __attribute__((always_inline)) {
+      Y.template copy<check.value>(tid, h, 64 * s, K, half_units(par.value, h ? kY1 : kY0), false, none);
+    };
+    // end of a memory slot: this wave's copies but the last ten have landed
+    auto landed = [&]() __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(10)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // end of a products slot: this wave's reads are done
+    auto done = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
     auto products = [&](int hm, int hn, const u32x4_t(&yf)[2][2]) __attribute__((always_inline)) {
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -272,47 +289,66 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
             acc[4 * hm + i][2 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
       __builtin_amdgcn_s_setprio(0);
     };
-
-    const int n_st = (K + 63) / 64;
-    for (int s = 0; s < 2; ++s) {
-      copy_y(s, 0);
-      copy_x(s, 0);
-      copy_y(s, 1);
-      copy_x(s, 1);
-    }
-    landed();
-    Y.read(half_bytes(0, kY0), y0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
-    if (late) barrier();
-    for (int s = 0; s < n_st; ++s) {
-      X.read(half_bytes(s, kX0), xf);
-      copy_y(s + 2, 0);
+    auto stage = [&](auto par, auto check, int s) __attribute__((always_inline)) {
+      constexpr int P = par.value;
+      std::integral_constant<int, 1 - P> other;
+      X.template read<P>(kX0 * kPipeHalf * 16, xf);
+      copy_x(other, check, s + 1, 1);
       landed();
       products(0, 0, y0);
-      barrier();
-      Y.read(half_bytes(s, kY1), y1);
-      copy_x(s + 2, 0);
+      done();
+      Y.template read<P>(kY1 * kPipeHalf * 16, y1);
+      copy_y(par, check, s + 2, 0);
+      fetch_rows(s + 2);
       landed();
       products(0, 1, y1);
-      barrier();
-      X.read(half_bytes(s, kX1), xf);
-      copy_y(s + 2, 1);
+      done();
+      X.template read<P>(kX1 * kPipeHalf * 16, xf);
+      copy_x(par, check, s + 2, 0);
       landed();
       products(1, 1, y1);
-      barrier();
-      u32x4_t y0n[2][2];
-      Y.read(half_bytes(s + 1, kY0), y0n);
-      copy_x(s + 2, 1);
+      done();
+      u32x4_t next[2][2];
+      Y.template read<1 - P>(kY0 * kPipeHalf * 16, next);
+      copy_y(par, check, s + 2, 1);
       landed();
       products(1, 0, y0);
-      barrier();
+      done();
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) y0[j][ks] = y0n[j][ks];
+        for (int ks = 0; ks < 2; ++ks) y0[j][ks] = next[j][ks];
+    };
+
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    constexpr std::integral_constant<bool, true> check;
+    constexpr std::integral_constant<bool, false> whole;
+    const int n_st = (K + 63) / 64;
+    fetch_rows(0);
+    copy_y(even, check, 0, 0);
+    copy_x(even, check, 0, 0);
+    copy_y(even, check, 0, 1);
+    copy_x(even, check, 0, 1);
+    fetch_rows(1);
+    copy_y(odd, check, 1, 0);
+    copy_x(odd, check, 1, 0);
+    copy_y(odd, check, 1, 1);
+    landed();
+    Y.template read<0>(kY0 * kPipeHalf * 16, y0);
+    done();
+    if (late) done();
+    int s = 0;
+    // stages whose copies all lie within K, then the rest
+    for (; 64 * (s + 4) <= K; s += 2) {
+      stage(even, whole, s);
+      stage(odd, whole, s + 1);
     }
-    if (!late) barrier();
+    for (; s < n_st; s += 2) {
+      stage(even, check, s);
+      if (s + 1 < n_st) stage(odd, check, s + 1);
+    }
+    if (!late) done();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
     if (!gather_k) break;
   }
@@ -322,8 +358,12 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 
-// Whether the byte offsets of a tile's rows fit the kernel's 32 bits.
-inline bool pipe_fits(const GroupArgs& a) { return a.ldx < (1 << 22) && a.ldy < (1 << 22); }
+// Whether the byte offsets of a tile's rows, or of any row that may be
+// gathered, fit the kernel's 32 bits.
+inline bool pipe_fits(const GroupArgs& a, int mode) {
+  const int64_t ld = mode == kBwdKer ? a.ldx : a.ldy;
+  return a.ldx < (1 << 22) && a.ldy < (1 << 22) && (!a.rows || a.Nsrc * ld * 2 < (1LL << 32) - 65536);
+}
 
 template <typename TO, int MODE>
 hipError_t launch_pipe(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
@@ -332,7 +372,7 @@ hipError_t launch_pipe(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tile
   const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
   if (e != hipSuccess) return e;
   const int64_t grid = row_tiles * ((a.M + 255) / 256);
-  const int lds = kPipeLds + (MODE == kBwdKer && a.rows ? kPipeRows * 4 : 0);
+  const int lds = kPipeLds + (MODE == kBwdKer && a.rows ? (kPipeRows + 192) * 4 : 0);
   k<<<dim3((uint32_t)grid), dim3(512), lds, stream>>>(a, ad, band);
   return hipGetLastError();
 }

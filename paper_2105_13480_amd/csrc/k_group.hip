@@ -31,7 +31,7 @@ template <typename T, typename TO, int MODE, bool DMA>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   if constexpr (sizeof(T) == 2 && DMA) {
     const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
-    if (rows >= 192 && a.M >= 192 && pipe_fits(a))
+    if (rows >= 192 && a.M >= 192 && pipe_fits(a, MODE))
       return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
   }
   return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
