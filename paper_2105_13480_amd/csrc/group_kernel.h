@@ -252,13 +252,29 @@ __device__ __forceinline__ void group_rows(const int32_t* off, int Ng, int Np, i
   *hi = g < Ng ? off[g + 1] : Np;
 }
 
-// Inclusive sum over the wave's lanes.
-__device__ __forceinline__ int wave_scan(int v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
+// v of the lane that a data-parallel move names; 0 where there is none.
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ int move_lanes(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+
+// Inclusive sum over the wave's lanes: within rows of 16 by shifts of 1, 2, 4
+// and 8, then each row's last lane into the rows after it.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += move_lanes<0x111>(v);
+  v += move_lanes<0x112>(v);
+  v += move_lanes<0x114>(v);
+  v += move_lanes<0x118>(v);
+  v += move_lanes<0x142, 0xa>(v);  // lane 15 of rows 0 and 2 into rows 1 and 3
+  v += move_lanes<0x143, 0xc>(v);  // lane 31 into rows 2 and 3
+  return v;
+}
+
+// The least v of each row of 16 lanes, in all of them.
+__device__ __forceinline__ int row16_min(int v) {
+  v = min(v, move_lanes<0xb1>(v));   // quad_perm 1,0,3,2
+  v = min(v, move_lanes<0x4e>(v));   // quad_perm 2,3,0,1
+  v = min(v, move_lanes<0x141>(v));  // row_half_mirror
+  v = min(v, move_lanes<0x140>(v));  // row_mirror
   return v;
 }
 
@@ -278,35 +294,37 @@ __device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, in
     if (bid >= nt * MT) return false;
     j0 = xcd_remap(bid, nt * MT);
   } else {
-    int total = 0;
+    // up to 63 groups: one pass, else one for the total and one for the tile
+    int lo = 0, hi = 0, incl = 0, total = 0;
     for (int base = 0; base <= Ng; base += 64) {
       const int g = base + lane;
-      int lo = 0, hi = 0;
+      lo = hi = 0;
       if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
       if (__ballot(lo < 0 || hi < lo || hi > Np || (g == 0 && lo != 0))) return false;
-      total += __shfl(wave_scan((hi - lo + TN - 1) / TN, lane), 63);
+      incl = wave_scan((hi - lo + TN - 1) / TN);
+      total += __builtin_amdgcn_readlane(incl, 63);
     }
-    total = __builtin_amdgcn_readfirstlane(total);
     if (bid >= total * MT) return false;
     const int L = xcd_remap(bid, total * MT);
     int before = 0;
     for (int base = 0;; base += 64) {
-      const int g = base + lane;
-      int lo = 0, hi = 0;
-      if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
-      const int n = (hi - lo + TN - 1) / TN;
-      const int incl = before + wave_scan(n, lane);
-      const uint64_t here = __ballot(L < incl * MT);
+      if (Ng >= 64) {
+        const int g = base + lane;
+        lo = hi = 0;
+        if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
+        incl = wave_scan((hi - lo + TN - 1) / TN);
+      }
+      const uint64_t here = __ballot(L < (before + incl) * MT);
       if (here) {
         const int who = __ffsll((unsigned long long)here) - 1;
-        nt = __builtin_amdgcn_readfirstlane(__shfl(n, who));
-        j0 = L - (__builtin_amdgcn_readfirstlane(__shfl(incl, who)) - nt) * MT;
-        t->g = __builtin_amdgcn_readfirstlane(base + who);
-        lo_g = __builtin_amdgcn_readfirstlane(__shfl(lo, who));
-        hi_g = __builtin_amdgcn_readfirstlane(__shfl(hi, who));
+        lo_g = __builtin_amdgcn_readlane(lo, who);
+        hi_g = __builtin_amdgcn_readlane(hi, who);
+        nt = (hi_g - lo_g + TN - 1) / TN;
+        j0 = L - (before + __builtin_amdgcn_readlane(incl, who) - nt) * MT;
+        t->g = base + who;
         break;
       }
-      before = __shfl(incl, 63);
+      before += __builtin_amdgcn_readlane(incl, 63);
     }
   }
   const int b = j0 / (band * MT), rb = min(band, nt - b * band), j = j0 - b * band * MT;
@@ -417,96 +435,98 @@ __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>
 }
 
 // The low-rank part of an adapted tile, added to acc: for each adapter that
-// rows of the tile name, one more run of k, added to those rows only (another
-// adapter's infinities must not meet them, not even as products with zero).
-// H is fp32; in bf16 it enters as the sum of its leading two (bf16 Out) or
-// three (fp32 Out) bf16 parts, each a run of the ranks padded to 8, so the
-// product keeps H to 2^-16 (2^-24) of itself, below the rounding of Out.
-// buf: 8 (TM + TN) units that no wave uses any more after a barrier.
-template <typename T, typename TO, int TM, int TN, int NT, int NI, int NJ, typename XR, typename YR>
+// the wave's rows name, one more run of k over the parts of H.  Both operands
+// come straight from memory (a few KB that the workgroup's waves share in
+// their caches), so there is nothing to wait for but this wave's own loads.
+// Each adapter's products go to its own rows only: another's infinities must
+// not meet them, not even as products with zero.  Four by two blocks of acc
+// at a time, so that no more is carried around the loops.
+// WHOLE: Nl is a multiple of a unit, else B's rows are read by elements.
+template <typename T, typename TO, bool WHOLE, int NI, int NJ, typename XR, typename YR>
 __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad,
-                                         const Tile<T, TO>& w, u32x4_t* buf, int tid,
-                                         f32x4_t (&acc)[NI][NJ], XR xrow, YR yrow) {
-  constexpr int CE = 16 / (int)sizeof(T), TK = 8 * CE;
-  constexpr int XU = 8 * TM, YU = 8 * TN;
-  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
-  const int lane = tid & 63;
-  const int Nlp = (ad.Nl + 7) & ~7;
-  const T* const B = reinterpret_cast<const T*>(ad.B);
-  int id_of[NJ];  // adapter of this lane's row in each block of 16
+                                         const Tile<T, TO>& w, int lane, f32x4_t (&acc)[NI][NJ],
+                                         XR xrow, YR yrow) {
+  constexpr int CE = 16 / (int)sizeof(T), STEP = 4 * CE;
+  constexpr int BATCH = WHOLE ? 2 : 1;  // steps whose loads are in flight together
+  const u32x4_t zero = {0u, 0u, 0u, 0u};
+  const int l16 = lane & 15, G = lane >> 4;
+  const T* const H = reinterpret_cast<const T*>(ad.Hp) + (int64_t)w.n0 * ad.hl;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
-    id_of[j] = ad.ids[w.n0 + min(yrow(j) + (lane & 15), w.n_valid - 1)];
-  int last = -1;
-  for (;;) {
-    // the least adapter above the last one
-    int next = 0x7fffffff;
-    for (int n = lane; n < w.n_valid; n += 64) {
-      const int id = ad.ids[w.n0 + n];
-      if (id > last && id < ad.Na) next = min(next, id);
+  for (int j0 = 0; j0 < NJ; j0 += 2) {
+    int id_of[2];  // adapter of this lane's rows; past the tile, the last row's
+    uint32_t hrow[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int n = min(yrow(j0 + j) + l16, w.n_valid - 1);
+      id_of[j] = ad.ids[w.n0 + n];
+      hrow[j] = (uint32_t)(n * ad.hl);
     }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) next = min(next, __shfl_xor(next, d));
-    next = __builtin_amdgcn_readfirstlane(next);
-    if (next == 0x7fffffff) break;
-    last = next;
-    const T* const Ba = B + (int64_t)next * a.M * ad.Nl;
-    const float scale = ad.scales ? ad.scales[next] : 1.f;
-    for (int k0 = 0; k0 < PARTS * Nlp; k0 += TK) {
-      __syncthreads();  // every wave is done with the buffer
-      for (int u = tid; u < XU; u += NT) {
-        const int r = u >> 3, c = unit_at<T, true, TM>(r, u & 7) - r * 8;
-        const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
-        const int valid = r < w.m_valid && part < PARTS ? ad.Nl - rk : 0;
-        buf[u] = load_unit(Ba + (int64_t)(w.m0 + r) * ad.Nl + rk, valid);
-      }
-      for (int u = tid; u < YU; u += NT) {
-        const int r = u >> 3, c = unit_at<T, true, TN>(r, u & 7) - r * 8;
-        const int kk = k0 + c * CE, part = kk / Nlp, rk = kk - part * Nlp;
-        const bool ok = r < w.n_valid && part < PARTS;
-        float h[CE];
+    for (int i0 = 0; i0 < NI; i0 += 4) {
+      uint32_t brow[4];
 #pragma unroll
-        for (int e = 0; e < CE; ++e) {
-          h[e] = 0.f;
-          if (ok && rk + e < ad.Nl) h[e] = ad.H[(int64_t)(w.n0 + r) * ad.Nl + rk + e] * scale;
-        }
-        u32x4_t v;
-        if constexpr (sizeof(T) == 4) {
+      for (int i = 0; i < 4; ++i)
+        brow[i] = (uint32_t)(min(xrow(i0 + i) + l16, w.m_valid - 1) * ad.Nl);
+      int last = -1;
+#pragma unroll 1
+      for (;;) {
+        int next = 0x7fffffff;  // the least adapter above the last one
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(h[e]);
-        } else {
+        for (int j = 0; j < 2; ++j)
+          if (id_of[j] > last && id_of[j] < ad.Na) next = min(next, id_of[j]);
+        // the four rows of 16 lanes hold the same
+        next = __builtin_amdgcn_readfirstlane(row16_min(next));
+        if (next == 0x7fffffff) break;
+        last = next;
+        const T* const B = reinterpret_cast<const T*>(ad.B) + ((int64_t)next * a.M + w.m0) * ad.Nl;
+#pragma unroll 1
+        for (int k0 = 0; k0 < ad.hl; k0 += BATCH * STEP) {
+          u32x4_t xf[BATCH][4], yf[BATCH][2];
+          bool in[BATCH];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p0 = bf16_part(h[2 * e], part), p1 = bf16_part(h[2 * e + 1], part);
-            v[e] = (__float_as_uint(p0) >> 16) | (__float_as_uint(p1) & 0xffff0000u);
+          for (int s = 0; s < BATCH; ++s) {
+            in[s] = k0 + s * STEP + CE * G < ad.hl;
+            const int kk = in[s] ? k0 + s * STEP + CE * G : 0, rank = kk % ad.nlp;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) __builtin_memcpy(&yf[s][j], H + hrow[j] + kk, 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const T* const row = B + brow[i];
+              if constexpr (WHOLE) {
+                __builtin_memcpy(&xf[s][i], row + rank, 16);
+              } else {
+                T v[CE];
+#pragma unroll
+                for (int e = 0; e < CE; ++e) v[e] = row[min(rank + e, ad.Nl - 1)];
+#pragma unroll
+                for (int e = 0; e < CE; ++e) v[e] = rank + e < ad.Nl ? v[e] : (T)0;
+                __builtin_memcpy(&xf[s][i], v, 16);
+              }
+            }
           }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f32x4_t sum = acc[i0 + i][j0 + j];
+#pragma unroll
+              for (int s = 0; s < BATCH; ++s)
+                sum = mma<T>(in[s] ? xf[s][i] : zero, in[s] ? yf[s][j] : zero, sum);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[i0 + i][j0 + j][e] = id_of[j] == next ? sum[e] : acc[i0 + i][j0 + j][e];
+            }
         }
-        buf[XU + u] = v;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        u32x4_t yf[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) yf[ks] = read_frag<T, true, TN>(buf + XU, yrow(j), ks, lane);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          f32x4_t part = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ks = 0; ks < 2; ++ks)
-            part = mma<T>(read_frag<T, true, TM>(buf, xrow(i), ks, lane), yf[ks], part);
-          if (id_of[j] == next) acc[i][j] += part;
-        }
-        __builtin_amdgcn_sched_barrier(0);  // not all rows' operands at once
       }
     }
   }
 }
 
 // TM x TN results by WM x WN waves.  DMA: both operands by 16-byte copies to
-// LDS (16-byte aligned rows), else through registers.
-template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>
-__global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
+// LDS (16-byte aligned rows), else through registers.  WHOLE: see low_rank.
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA, bool WHOLE>
+__global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
   constexpr int NT = 64 * WM * WN;
   constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
   constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE == kAdapt;  // gathered operands
@@ -575,15 +595,14 @@ __global__ __launch_bounds__(64 * WM * WN) void group_tiles(GroupArgs a, AdaptAr
       sy.commit(tid, nxt + XU);
     }
   }
-  if constexpr (MODE == kAdapt)
-    low_rank<T, TO, TM, TN, NT>(a, ad, w, buf0, tid, acc, xrow, yrow);
+  if constexpr (MODE == kAdapt) low_rank<T, TO, WHOLE>(a, ad, w, lane, acc, xrow, yrow);
   store_tile<T, TO, MODE, false>(a, w, lane, acc, xrow, yrow);
 }
 
-template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA>
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA, bool WHOLE = true>
 hipError_t launch_tiles(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
                         hipStream_t stream) {
-  auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DMA>;
+  auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DMA, WHOLE>;
   const int lds = 2 * 8 * (TM + TN) * 16;
   if (lds > 64 * 1024) {
     const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));

@@ -353,8 +353,7 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
     if (!gather_k) break;
   }
 
-  if constexpr (MODE == kAdapt)
-    low_rank<T, TO, 256, 256, 512>(a, ad, w, lds, tid, acc, xrow, yrow);
+  if constexpr (MODE == kAdapt) low_rank<T, TO, true>(a, ad, w, lane, acc, xrow, yrow);
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 

@@ -1,0 +1,441 @@
+// Products of few rows: grouped products with a few rows a group, and adapted
+// projections of up to a few dozen rows (serving steps).
+//
+// Such a product is bound by reading Ker once: a workgroup takes 16 FB features
+// by 16 RB rows, its waves share the contraction (wave w takes every NW-th
+// 256-byte run of k), and both operands go straight from memory to the MFMA
+// registers, no LDS and no barrier until the waves' sums meet: 16 rows of 64
+// bytes a load, four loads a run.  Rows beyond a tile's last read a row that
+// is there; their results are not stored.
+#include "group_kernel.h"
+
+namespace cnnlib {
+
+namespace {
+
+using namespace group;
+
+// A run's operands: four loads of 16 rows by 64 bytes of each block.
+template <typename T, int FB, int RB> struct Run {
+  static constexpr int CE = 16 / (int)sizeof(T), LEN = 16 * CE;
+  u32x4_t x[FB][4], y[RB][4];
+
+  // All loads before anything that waits for one.
+  __device__ __forceinline__ void load(const T* const (&xp)[FB], const T* const (&yp)[RB], int k0,
+                                       int G) {
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) __builtin_memcpy(&x[f][i], xp[f] + k0 + (4 * i + G) * CE, 16);
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) __builtin_memcpy(&y[b][i], yp[b] + k0 + (4 * i + G) * CE, 16);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[FB][RB]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[f][b] = mma<T>(x[f][i], y[b][i], acc[f][b]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// acc[f][b] += the 16 features of block f by the 16 rows of block b, over the
+// runs of k that `wave` of `nw` takes in [0, K).  x, y: this lane's feature
+// row (l % 16) and row of each block.  Where registers allow, a run's loads
+// are issued before the last one's products.
+template <typename T, int FB, int RB>
+__device__ __forceinline__ void few_rows_dot(const T* const (&x)[FB], const T* const (&y)[RB],
+                                             int K, int wave, int nw, int lane,
+                                             f32x4_t (&acc)[FB][RB]) {
+  typedef Run<T, FB, RB> R;
+  const int G = lane >> 4, step = nw * R::LEN;
+  int k0 = wave * R::LEN;
+  R a;
+#ifndef PIPEMAX
+#define PIPEMAX 3
+#endif
+  if constexpr (FB + RB <= PIPEMAX) {
+    R b;
+    if (k0 + R::LEN <= K) a.load(x, y, k0, G);
+    for (; k0 + R::LEN <= K; k0 += 2 * step) {
+      const bool second = k0 + step + R::LEN <= K;
+      if (second) b.load(x, y, k0 + step, G);
+      a.multiply(acc);
+      if (!second) {
+        k0 += step;
+        break;
+      }
+      if (k0 + 2 * step + R::LEN <= K) a.load(x, y, k0 + 2 * step, G);
+      b.multiply(acc);
+    }
+  } else {
+    for (; k0 + R::LEN <= K; k0 += step) {
+      a.load(x, y, k0, G);
+      a.multiply(acc);
+    }
+  }
+  if (k0 < K) {  // the last, shorter run: what lies past K is zero on both sides
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k0 + (4 * i + G) * R::CE;
+#pragma unroll
+      for (int f = 0; f < FB; ++f) a.x[f][i] = load_unit(x[f] + k, K - k);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) a.y[b][i] = load_unit(y[b] + k, K - k);
+    }
+    a.multiply(acc);
+  }
+}
+
+// Leaves the waves' sums where block_sum finds them.  red: nw * FB * RB * 64 units.
+template <int FB, int RB>
+__device__ __forceinline__ void leave_sums(f32x4_t* red, const f32x4_t (&acc)[FB][RB], int wave,
+                                           int nw, int lane) {
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) red[((f * RB + b) * nw + wave) * 64 + lane] = acc[f][b];
+  __syncthreads();
+}
+// The waves' sums of block f * RB + b added in wave order.
+__device__ __forceinline__ f32x4_t block_sum(const f32x4_t* red, int block, int nw, int lane) {
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  for (int w = 0; w < nw; ++w) s += red[(block * nw + w) * 64 + lane];
+  return s;
+}
+
+// This lane's feature rows from m0 on; past the last, the last.
+template <typename T, int FB>
+__device__ __forceinline__ void feature_rows(const T* X, int64_t ld, int m0, int M, int l16,
+                                             const T* (&x)[FB]) {
+#pragma unroll
+  for (int f = 0; f < FB; ++f) x[f] = X + (int64_t)min(m0 + 16 * f + l16, M - 1) * ld;
+}
+
+template <int FB, int RB>
+__device__ __forceinline__ void clear(f32x4_t (&acc)[FB][RB]) {
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[f][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+}
+
+// PARTS 0: results to D.  Else scaled results to rows of the low-rank operand:
+// PARTS parts of nlp ranks, and zeros where M < nlp.
+template <typename T, typename TO, int FB, int RB, int NW, int PARTS>
+__global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) {
+  __shared__ f32x4_t red[NW * FB * RB * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int MT = (a.M + 16 * FB - 1) / (16 * FB);
+  RowTile t;
+  if (!find_tile<16 * RB>(a.off, a.Ng, a.N, MT, blockIdx.x, 1, &t)) return;
+  const int l16 = lane & 15, G = lane >> 4;
+  const int m0 = 16 * FB * t.mt, n_valid = min(t.n1 - t.n0, 16 * RB);
+  const bool live = t.g < a.Ng;
+  if (PARTS && !live) return;  // rows without an adapter
+
+  const T* const X = reinterpret_cast<const T*>(a.X) + (live ? t.g : 0) * a.xgroup;
+  const T* x[FB];
+  feature_rows<T, FB>(X, a.ldx, m0, a.M, l16, x);
+  const T* y[RB];
+  uint32_t none = 0;  // blocks whose row of this lane is no row of In
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    int64_t r = t.n0 + min(16 * b + l16, n_valid - 1);
+    if (a.rows) r = a.rows[r];
+    if (r < 0 || r >= a.Nsrc) {
+      none |= 1u << b;
+      r = 0;
+    }
+    y[b] = reinterpret_cast<const T*>(a.Y) + r * a.ldy;
+  }
+  f32x4_t acc[FB][RB];
+  clear(acc);
+  if (live) few_rows_dot<T, FB, RB>(x, y, a.K, wave, NW, lane, acc);
+  leave_sums(red, acc, wave, NW, lane);
+
+  for (int blk = wave; blk < FB * RB; blk += NW) {
+    const int b = blk % RB, n = 16 * b + l16, m = m0 + 16 * (blk / RB) + 4 * G;
+    if (n >= n_valid) continue;
+    f32x4_t s = block_sum(red, blk, NW, lane);
+    if (!live || (none >> b & 1)) s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if constexpr (PARTS == 0) {
+      const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
+      store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s, whole);
+    } else {
+      const float scale = ad.scales ? ad.scales[t.g] : 1.f;
+      T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(t.n0 + n) * ad.hl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (m + e >= ad.nlp) break;
+        const float h = m + e < a.M ? s[e] * scale : 0.f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          if constexpr (sizeof(T) == 4) row[m + e] = h;
+          else row[p * ad.nlp + m + e] = (T)(__float_as_uint(bf16_part(h, p)) >> 16);
+        }
+      }
+    }
+  }
+}
+
+// Few adapted rows, first launch: partial sums of both products that read In.
+// The first workgroups, (tile of 16 rows, q, z), take every Q-th of the
+// adapters that the tile's rows name, 16 DF ranks at a time, over slice z of
+// k: H[z][n][r] = sum_k In[n, k] A[ids[n]][r, k].  The rest, (block of 16 FB
+// features, slice of k), take all rows: part[z][n][m] = sum_k In[n, k] Ker[m, k].
+// Neither waits for the other, and a slice is short, so that all of Ker is
+// asked for at once.
+template <typename T, int DF, int FB, int RB, int NW>
+__global__ __launch_bounds__(64 * NW) void adapt_few_sums(GroupArgs a, AdaptArgs ad, FewPlan f) {
+  __shared__ f32x4_t red[NW * (DF > FB * RB ? DF : FB * RB) * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, G = lane >> 4;
+  int bid = blockIdx.x;
+  if (bid < f.downs) {
+    const int z = bid % f.kh, q0 = bid / f.kh % f.q, n0 = 16 * (bid / (f.kh * f.q));
+    const int k_lo = z * f.hslice, n_valid = min(a.N - n0, 16);
+    const int K = min(a.K - k_lo, f.hslice);
+    const int n = n0 + min(l16, n_valid - 1);
+    const int id = ad.ids[n];
+    const T* y[1] = {reinterpret_cast<const T*>(a.Y) + (int64_t)n * a.ldy + k_lo};
+    float* const H = ad.H + ((int64_t)z * a.N + n) * ad.Nl;
+    int last = -1;
+    for (int q = 0;; ++q) {
+      int next = id > last && id < ad.Na ? id : 0x7fffffff;
+      next = __builtin_amdgcn_readfirstlane(row16_min(next));
+      if (next == 0x7fffffff) break;
+      last = next;
+      if (q % f.q != q0) continue;
+      const T* const A = reinterpret_cast<const T*>(ad.A) + (int64_t)next * ad.Nl * a.K + k_lo;
+      for (int r0 = 0; r0 < ad.Nl; r0 += 16 * DF) {
+        const T* x[DF];
+        f32x4_t acc[DF][1];
+        feature_rows<T, DF>(A, a.K, r0, ad.Nl, l16, x);
+        clear(acc);
+        few_rows_dot<T, DF, 1>(x, y, K, wave, NW, lane, acc);
+        leave_sums(red, acc, wave, NW, lane);
+        if (l16 < n_valid && id == next)
+          for (int b = wave; b < DF; b += NW)
+            store4(H, r0 + 16 * b + 4 * G, ad.Nl, block_sum(red, b, NW, lane), (ad.Nl & 3) == 0);
+        __syncthreads();  // before the next sums overwrite `red`
+      }
+    }
+    return;
+  }
+  bid -= f.downs;
+  const int z = bid / f.blocks, m0 = 16 * FB * (bid % f.blocks), k_lo = z * f.kslice;
+  const T* x[FB];
+  feature_rows<T, FB>(reinterpret_cast<const T*>(a.X) + k_lo, a.ldx, m0, a.M, l16, x);
+  const T* y[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    y[b] = reinterpret_cast<const T*>(a.Y) + (int64_t)min(16 * b + l16, a.N - 1) * a.ldy + k_lo;
+  f32x4_t acc[FB][RB];
+  clear(acc);
+  few_rows_dot<T, FB, RB>(x, y, min(a.K - k_lo, f.kslice), wave, NW, lane, acc);
+  leave_sums(red, acc, wave, NW, lane);
+  for (int blk = wave; blk < FB * RB; blk += NW) {
+    const int n = 16 * (blk % RB) + l16, m = m0 + 16 * (blk / RB) + 4 * G;
+    if (n < a.N)
+      store4(ad.part + ((int64_t)z * a.N + n) * a.M, m, a.M, block_sum(red, blk, NW, lane), (a.M & 3) == 0);
+  }
+}
+
+// Second launch: Out = the slices' sums, in order, and each row's low-rank
+// part in fp32; a thread has four features of a row.
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad, FewPlan f) {
+  const int per = (a.M + 3) / 4;
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= per * a.N) return;
+  const int n = i / per, m = 4 * (i - n * per);
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < f.ks; ++z) {
+    const float* const src = ad.part + ((int64_t)z * a.N + n) * a.M + m;
+    if (a.M % 4 == 0) {
+      sum += *reinterpret_cast<const f32x4_t*>(src);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += src[min(e, a.M - 1 - m)];
+    }
+  }
+  const int id = ad.ids[n];
+  if (id >= 0 && id < ad.Na) {
+    const T* const B = reinterpret_cast<const T*>(ad.B) + ((int64_t)id * a.M + m) * ad.Nl;
+    const float* const H = ad.H + (int64_t)n * ad.Nl;
+    const int64_t hz = (int64_t)a.N * ad.Nl;
+    f32x4_t d = {0.f, 0.f, 0.f, 0.f};
+    int r = 0;
+#pragma unroll 2
+    for (; r + 8 <= ad.Nl; r += 8) {
+      float h[8] = {};
+      for (int z = 0; z < f.kh; ++z) {
+        float p[8];
+        __builtin_memcpy(p, H + z * hz + r, sizeof(p));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] += p[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        T b[8];
+        __builtin_memcpy(b, B + (int64_t)min(e, a.M - 1 - m) * ad.Nl + r, sizeof(b));
+#pragma unroll
+        for (int t = 0; t < 8; ++t) d[e] += h[t] * to_f32(b[t]);
+      }
+    }
+    for (; r < ad.Nl; ++r) {
+      float h = 0.f;
+      for (int z = 0; z < f.kh; ++z) h += H[z * hz + r];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] += h * to_f32(B[(int64_t)min(e, a.M - 1 - m) * ad.Nl + r]);
+    }
+    const float s = ad.scales ? ad.scales[id] : 1.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += s * d[e];
+  }
+  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
+  store4(reinterpret_cast<TO*>(a.D) + (int64_t)n * a.ldd, m, a.M, sum, whole);
+}
+
+template <typename T, typename TO, int FB, int RB, int NW>
+hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
+  const int64_t mt = (a.M + 16 * FB - 1) / (16 * FB), parts = a.Ng + 1 < a.N ? a.Ng + 1 : a.N;
+  const dim3 grid((uint32_t)((a.N / (16 * RB) + parts) * mt)), block(64 * NW);
+  group_few<T, TO, FB, RB, NW, 0><<<grid, block, 0, stream>>>(a, AdaptArgs{});
+  return hipGetLastError();
+}
+
+// Whether k holds a run for each of sixteen waves.
+#ifndef LK
+#define LK 16
+#endif
+#ifndef FNW
+#define FNW 4
+#endif
+#ifndef BNW
+#define BNW 4
+#endif
+#ifndef BFB
+#define BFB 4
+#endif
+template <typename T> bool long_k(const GroupArgs& a) { return a.K >= LK * (256 / (int)sizeof(T)); }
+
+template <typename T, typename TO> hipError_t launch_few_typed(const GroupArgs& a, hipStream_t stream) {
+  const int64_t rows = a.N / a.Ng;
+  if (rows <= 8) return launch_few<T, TO, 1, 1, FNW>(a, stream);
+  return launch_few<T, TO, BFB, 2, BNW>(a, stream);
+}
+
+#ifndef DNW
+#define DNW 8
+#endif
+#ifndef DFB
+#define DFB 4
+#endif
+#ifndef DRB
+#define DRB 2
+#endif
+template <typename T, typename TO, int PARTS>
+hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+  const int64_t parts = ad.Na + 1 < a.N ? ad.Na + 1 : a.N;
+  GroupArgs h = a;
+  h.X = ad.A;
+  h.xgroup = (int64_t)ad.Nl * a.K;
+  h.M = ad.Nl;
+  h.Ng = ad.Na;
+  const dim3 block(64 * DNW);
+  auto grid = [&](int FB, int RB) {
+    return dim3((uint32_t)((a.N / (16 * RB) + parts) * ((ad.Nl + 16 * FB - 1) / (16 * FB))));
+  };
+  if (ad.Nl <= 16)
+    group_few<T, TO, 1, 2, DNW, PARTS><<<grid(1, 2), block, 0, stream>>>(h, ad);
+  else
+    group_few<T, TO, DFB, DRB, DNW, PARTS><<<grid(DFB, DRB), block, 0, stream>>>(h, ad);
+  return hipGetLastError();
+}
+
+template <typename T, int DF, int FB, int RB>
+void launch_sums(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
+  adapt_few_sums<T, DF, FB, RB, 4>
+      <<<dim3((uint32_t)(f.downs + f.blocks * f.ks)), dim3(256), 0, stream>>>(a, ad, f);
+}
+template <typename T, int DF>
+void launch_sums_rows(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
+  switch ((a.N + 15) / 16) {
+    case 1: launch_sums<T, DF, 1, 1>(a, ad, f, stream); break;
+    case 2: launch_sums<T, DF, 2, 2>(a, ad, f, stream); break;
+    case 3: launch_sums<T, DF, 2, 3>(a, ad, f, stream); break;
+    default: launch_sums<T, DF, 2, 4>(a, ad, f, stream); break;
+  }
+}
+
+template <typename T, typename TO>
+hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+  constexpr int RUN = 256 / (int)sizeof(T);
+  FewPlan f = adapt_few_plan(a.N, a.K, a.M);
+  // slices of k of whole runs
+  f.hslice = ((a.K + f.kh - 1) / f.kh + RUN - 1) / RUN * RUN;
+  f.kslice = ((a.K + f.ks - 1) / f.ks + RUN - 1) / RUN * RUN;
+  f.q = ad.Na < 16 ? ad.Na : 16;
+  f.downs = (a.N + 15) / 16 * f.q * f.kh;
+  if (ad.Nl <= 16) launch_sums_rows<T, 1>(a, ad, f, stream);
+  else launch_sums_rows<T, 4>(a, ad, f, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t threads = (int64_t)a.N * ((a.M + 3) / 4);
+  adapt_few_out<T, TO><<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, stream>>>(a, ad, f);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool group_few_fits(const GroupArgs& a) { return a.N <= 24 * (int64_t)a.Ng; }
+
+hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
+  switch (dtype) {
+    case CNN_F32: return launch_few_typed<float, float>(a, stream);
+    case CNN_BF16: return launch_few_typed<bf16_t, float>(a, stream);
+    default: return launch_few_typed<bf16_t, bf16_t>(a, stream);
+  }
+}
+
+hipError_t launch_adapt_down(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
+  switch (dtype) {
+    case CNN_F32: return launch_down<float, float, 1>(a, ad, stream);
+    case CNN_BF16: return launch_down<bf16_t, float, 3>(a, ad, stream);
+    default: return launch_down<bf16_t, bf16_t, 2>(a, ad, stream);
+  }
+}
+
+bool adapt_few(int64_t Nt) { return Nt <= 64; }
+
+FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk) {
+  FewPlan f = {};
+  // two blocks of features a workgroup but for the fewest rows: In is read
+  // half as often
+  const int fb = Nt <= 16 ? 1 : 2;
+  f.blocks = (int32_t)((Nk + 16 * fb - 1) / (16 * fb));
+  // two workgroups a CU, as long as each of their four waves has a run of k
+  const int64_t most = Nc / 512 < 1 ? 1 : Nc / 512 > 8 ? 8 : Nc / 512;
+  const int64_t want = (512 + f.blocks - 1) / f.blocks;
+  f.ks = (int32_t)(want < most ? want : most);
+  f.kh = (int32_t)most;
+  return f;
+}
+
+hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype,
+                            hipStream_t stream) {
+  switch (dtype) {
+    case CNN_F32: return launch_adapt_typed<float, float>(a, ad, stream);
+    case CNN_BF16: return launch_adapt_typed<bf16_t, float>(a, ad, stream);
+    default: return launch_adapt_typed<bf16_t, bf16_t>(a, ad, stream);
+  }
+}
+
+}  // namespace cnnlib

@@ -31,9 +31,12 @@ template <typename T, typename TO, int MODE, bool DMA>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   if constexpr (sizeof(T) == 2 && DMA) {
     const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
-    if (rows >= 192 && a.M >= 192 && pipe_fits(a, MODE))
+    if (rows >= 192 && a.M >= 192 && pipe_fits(a, MODE) && ad.nlp == ad.Nl)
       return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
   }
+  if (MODE == kAdapt && ad.nlp != ad.Nl)
+    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA, MODE != kAdapt>(
+        a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
   return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
 }
 
@@ -59,8 +62,7 @@ hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipS
 }  // namespace
 
 hipError_t launch_group_fwd(const GroupArgs& a, int dtype, hipStream_t stream) {
-  if (a.N <= 8 * (int64_t)a.Ng) return launch_group_skinny(a, dtype, 1, stream);
-  if (a.N <= 24 * (int64_t)a.Ng) return launch_group_skinny(a, dtype, 2, stream);
+  if (group_few_fits(a)) return launch_group_few(a, dtype, stream);
   return launch_typed<kFwd>(a, AdaptArgs{}, dtype, stream);
 }
 hipError_t launch_group_bwd_in(const GroupArgs& a, int dtype, hipStream_t stream) {
@@ -71,16 +73,7 @@ hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t strea
 }
 
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
-  // H of the ordered rows: the product grouped by adapter, fp32
-  GroupArgs h = a;
-  h.X = ad.A;
-  h.D = ad.H;
-  h.ldx = a.ldx;
-  h.ldd = ad.Nl;
-  h.xgroup = (int64_t)ad.Nl * a.K;
-  h.M = ad.Nl;
-  h.Ng = ad.Na;
-  hipError_t e = launch_typed<kFwd>(h, AdaptArgs{}, dtype == CNN_F32 ? CNN_F32 : CNN_BF16, stream);
+  const hipError_t e = launch_adapt_down(a, ad, dtype, stream);
   if (e != hipSuccess) return e;
   GroupArgs g = a;
   g.off = nullptr;

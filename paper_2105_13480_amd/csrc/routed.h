@@ -25,16 +25,35 @@ struct GroupArgs {
 };
 
 // The low-rank part beside a product:
-// D[n][m] += scales[a] sum_r H[n][r] B[a][m][r], a = ids[n].
+// D[n][m] += scales[a] sum_r H[n][r] B[a][m][r], H = In A[a]^T, a = ids[n].
 struct AdaptArgs {
   const void* A;         // [Na][Nl][Nc]
   const void* B;         // [Na][Nk][Nl]
   const int32_t* ids;    // adapter of each row, in the order of H; outside [0, Na): none
   const float* scales;   // [Na] or NULL
-  float* H;              // In A^T: [Nt][Nl]; few rows: [kz][Nt][Nl] partial sums
   int32_t Na, Nl;
-  int32_t kz;
+  // Many rows, in the order of their adapters: scaled H as operand rows of
+  // `hl` elements, in bf16 the leading two or three bf16 parts of the fp32
+  // values, `nlp` ranks each (Nl up to a unit, zeros past it).
+  void* Hp;
+  int32_t nlp, hl;
+  // Few rows, as they come: partial sums over slices of k.
+  float* H;              // [kh][Nt][Nl]
+  float* part;           // [ks][Nt][Nk]
 };
+
+// How an adapted product of few rows is split.
+struct FewPlan {
+  int32_t blocks;  // of features
+  int32_t ks, kh;  // slices of k of the projection and of H
+  int32_t kslice, hslice, q, downs;  // set by the launch: their lengths, and H's workgroups
+};
+
+// Ranks of one part of an operand row of H, and the row's elements.
+inline int adapt_nlp(int64_t Nl, int dtype) {
+  return (int)(dtype == CNN_F32 ? (Nl + 3) & ~(int64_t)3 : (Nl + 7) & ~(int64_t)7);
+}
+inline int adapt_parts(int dtype) { return dtype == CNN_F32 ? 1 : dtype == CNN_BF16 ? 3 : 2; }
 
 // The rows of a problem in the order of a key (experts of (row, choice) pairs,
 // adapters of rows): a counting sort by workgroups of `chunk` rows.
@@ -75,14 +94,16 @@ hipError_t launch_combine_bwd(const void* dOut, const void* In, const int32_t* s
 hipError_t launch_group_fwd(const GroupArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_group_bwd_in(const GroupArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t stream);
-// Products of few rows a group, straight from memory: row tiles of 16 rb rows.
-hipError_t launch_group_skinny(const GroupArgs& a, int dtype, int rb, hipStream_t stream);
+// Products of few rows a group, straight from memory.
+bool group_few_fits(const GroupArgs& a);
+hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream);
 // Whether an adapted product of Nt rows runs the few-rows kernels, which take
-// the rows as they come and keep adapt_slices partial sums of each element of H.
+// the rows as they come.
 bool adapt_few(int64_t Nt);
-int adapt_slices(int64_t Nc);
+FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk);
 hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
-// Rows in the order of their adapters (a.rows, ad.ids).
+// Rows in the order of their adapters (a.off, a.rows, ad.ids).
+hipError_t launch_adapt_down(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 
 }  // namespace cnnlib

@@ -135,22 +135,26 @@ int64_t route_ws_bytes(int64_t Nt, int64_t Ng) {
   return nblocks > 1 ? round16((int64_t)nblocks * Ng * 4) : 0;
 }
 
-// The adapted projection's workspace: H, and for the ordered form the order.
+// The adapted projection's workspace: few rows, the slices' sums; many, H and
+// the order of the rows.
 struct AdaptWs {
-  int64_t h, counts, off, rows, keys, total;
+  int64_t h, part, counts, off, rows, keys, total;
 };
-AdaptWs adapt_ws(int64_t Nt, int64_t Nc, int64_t Na, int64_t Nl) {
+AdaptWs adapt_ws(int64_t Nt, int64_t Nc, int64_t Nk, int64_t Na, int64_t Nl) {
   AdaptWs w = {};
-  const bool few = adapt_few(Nt);
-  w.h = round16((few ? adapt_slices(Nc) : 1) * Nt * Nl * 4);
-  if (!few) {
+  if (adapt_few(Nt)) {
+    const FewPlan f = adapt_few_plan(Nt, Nc, Nk);
+    w.h = round16(f.kh * Nt * Nl * 4);
+    w.part = round16(f.ks * Nt * Nk * 4);
+  } else {
     int32_t chunk, nblocks;
     order_blocks(Nt, &chunk, &nblocks);
+    w.h = round16(Nt * adapt_nlp(Nl, CNN_BF16) * 6);  // three bf16 parts, or fp32
     w.counts = round16((int64_t)nblocks * Na * 4);
     w.off = round16((Na + 1) * 4);
     w.rows = w.keys = round16(Nt * 4);
   }
-  w.total = w.h + w.counts + w.off + w.rows + w.keys;
+  w.total = w.h + w.part + w.counts + w.off + w.rows + w.keys;
   return w;
 }
 
@@ -344,7 +348,7 @@ int cnn_adapt_ws(int64_t Nt, int64_t Nc, int64_t Nk, int64_t Na, int64_t Nl, int
     if (!ws_bytes) return fail(CNN_E_NULL, "ws_bytes must be non-NULL");
     int st = check_adapt(Nt, Nc, Nk, Na, Nl);
     if (st) return st;
-    *ws_bytes = adapt_ws(Nt, Nc, Na, Nl).total;
+    *ws_bytes = adapt_ws(Nt, Nc, Nk, Na, Nl).total;
     return (int)CNN_OK;
   });
 }
@@ -358,7 +362,7 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     if ((st = check_adapt(Nt, Nc, Nk, Na, Nl)) || (st = check_type(dtype)) ||
         (st = check_tiles(Nt, Na, Nk)))
       return st;
-    const AdaptWs w = adapt_ws(Nt, Nc, Na, Nl);
+    const AdaptWs w = adapt_ws(Nt, Nc, Nk, Na, Nl);
     const int es = in_bytes(dtype);
     const Buf in[] = {{"In", In, Nt * Nc, es}, {"Ker", Ker, Nk * Nc, es}, {"A", A, Na * Nl * Nc, es},
                       {"B", B, Na * Nk * Nl, es}, {"Ids", Ids, Nt, 4},
@@ -374,13 +378,15 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     a.Ng = 1; a.Nsrc = (int32_t)Nt;
     AdaptArgs ad = {};
     ad.A = A; ad.B = B; ad.ids = Ids; ad.scales = Scales;
-    ad.H = (float*)p;
     ad.Na = (int32_t)Na; ad.Nl = (int32_t)Nl;
     if (adapt_few(Nt)) {
-      ad.kz = adapt_slices(Nc);
+      ad.H = (float*)p;
+      ad.part = (float*)(p + w.h);
       return launched(launch_adapt_few(a, ad, dtype, (hipStream_t)stream));
     }
-    ad.kz = 1;
+    ad.Hp = p;
+    ad.nlp = adapt_nlp(Nl, dtype);
+    ad.hl = ad.nlp * adapt_parts(dtype);
     OrderArgs o = {};
     o.key = Ids;
     o.counts = (int32_t*)(p += w.h);
