@@ -83,131 +83,261 @@ template <typename T, bool KC, int R> __device__ __forceinline__ int unit_at(int
 }
 
 // Stages one operand: R tile rows by TK values of k, 8 R units by NT threads.
-template <typename T, bool KC, int R, int NT, bool DMA, bool GATHER> struct Stager {
+// Rows of the tile past its last read one that is there (their results are not
+// stored; source rows that are not there are stored as zeros).
+template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
   static constexpr int CE = 16 / (int)sizeof(T);
   static constexpr int TK = 128 / (int)sizeof(T);
-  static constexpr int NU = 8 * R / NT;  // units a thread copies per stage
+  static constexpr int NU = 8 * R / NT;  // units a thread stages
   static constexpr int U = KC ? 8 : R / CE;
   static_assert(8 * R % NT == 0, "whole rounds");
 
-  const T* p[NU];   // the unit's first element at k = 0
-  int lim[NU];      // KC: elements of k from the unit's first; MC: elements of the tile index
-  int krow[NU];     // MC: row of k within a stage
-  u32x4_t reg[DMA ? 1 : NU];
+  const T* p[NU];  // the unit's first element at k = 0, or (rows of k) of a row
+  int at[NU];      // KC: the unit's first k within a stage; else its row of k
+  int lim[KC ? 1 : NU];  // elements of the row from the unit's first
+  u32x4_t reg[NU];
 
   // base: the tensor at its first k; rows [i0, i0 + n) of the tile index are
-  // valid; ld: elements from row to row; K: extent of k (KC).
-  // index: for a gathered KC operand, the source row of each tile row.
-  __device__ __forceinline__ void init(int tid, const T* base, int64_t ld, int64_t i0, int n, int K,
+  // there; ld: elements from row to row; index: source rows of a gathered
+  // KC operand.
+  __device__ __forceinline__ void init(int tid, const T* base, int64_t ld, int64_t i0, int n,
                                        const int32_t* index, int nsrc) {
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
       const int u = j * NT + tid;
-      const int r = u / U, pos = u % U;
-      const int c = unit_at<T, KC, R>(r, pos) - r * U;  // the permutation is its own inverse
+      const int r = u / U;
+      const int c = unit_at<T, KC, R>(r, u % U) - r * U;  // the permutation is its own inverse
       if constexpr (KC) {
-        int64_t row = i0 + r;
-        bool ok = r < n;
-        if constexpr (GATHER) {
-          if (ok && index) {
+        int64_t row = i0 + min(r, n - 1);
+        if constexpr (GATHER)
+          if (index) {
             row = index[row];
-            ok = row >= 0 && row < nsrc;
+            if (row < 0 || row >= nsrc) row = 0;
           }
-        }
-        p[j] = base + (ok ? row * ld : 0) + c * CE;
-        lim[j] = ok ? K - c * CE : 0;
-        krow[j] = 0;
+        at[j] = c * CE;
+        p[j] = base + row * ld + at[j];
       } else {
-        p[j] = base + i0 + c * CE;
+        at[j] = r;
         lim[j] = n - c * CE;
-        krow[j] = r;
+        p[j] = base + i0 + (lim[j] > 0 ? c * CE : 0);
       }
     }
   }
 
-  // Source and valid elements of unit j of the stage at k0.  MC: `index` as
-  // in init for the rows of k; nk rows of k in all.
-  __device__ __forceinline__ const T* at(int j, int k0, int64_t ld, int nk, const int32_t* index,
-                                         int nsrc, int* valid) const {
-    if constexpr (KC) {
-      *valid = lim[j] - k0;
-      return p[j] + k0;
-    } else {
-      const int k = k0 + krow[j];
-      int64_t row = k;
-      bool ok = k < nk;
-      if constexpr (GATHER) {
-        if (ok && index) {
-          row = index[k];
-          ok = row >= 0 && row < nsrc;
+  // The row of k that unit j reads in the stage at k0, of nk; false: none.
+  __device__ __forceinline__ bool row_of(int j, int k0, int nk, const int32_t* index, int nsrc,
+                                         int64_t* row) const {
+    const int k = k0 + at[j];
+    bool ok = k < nk;
+    *row = max(min(k, nk - 1), 0);  // the first is there even where nk = 0 asks for zeros
+    if constexpr (GATHER)
+      if (index) {
+        *row = index[*row];
+        if (*row < 0 || *row >= nsrc) {
+          *row = 0;
+          ok = false;
         }
       }
-      *valid = ok ? lim[j] : 0;
-      return p[j] + (ok ? row * ld : 0);
-    }
+    return ok;
   }
 
-  __device__ __forceinline__ void issue(int tid, u32x4_t* lds, int k0, int64_t ld, int nk,
-                                        const int32_t* index, int nsrc) {
+  // Straight to LDS, in whole units; what lies past K (nk) reads zeros.
+  __device__ __forceinline__ void copy(int tid, u32x4_t* lds, int k0, int64_t ld, int nk,
+                                       const int32_t* index, int nsrc) const {
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
-      int valid;
-      const T* src = at(j, k0, ld, nk, index, nsrc, &valid);
-      if constexpr (DMA) {
-        // whole units only: a unit that starts inside a row ends inside it
-        const void* from = valid > 0 ? (const void*)src : (const void*)zero_unit;
-        copy16_lds(from, lds + j * NT + (__builtin_amdgcn_readfirstlane(tid) & ~63));
+      const T* src;
+      bool ok;
+      if constexpr (KC) {
+        src = p[j] + k0;
+        ok = k0 + at[j] < nk;
       } else {
-        reg[j] = load_unit(src, valid);
+        int64_t row;
+        ok = row_of(j, k0, nk, index, nsrc, &row);
+        src = p[j] + row * ld;
       }
+      copy16_lds(ok ? (const void*)src : (const void*)zero_unit,
+                 lds + j * NT + (__builtin_amdgcn_readfirstlane(tid) & ~63));
     }
   }
-  __device__ __forceinline__ void commit(int tid, u32x4_t* lds) {
-    if constexpr (!DMA) {
+
+  // Through registers, at any alignment: loads, and later the LDS writes.
+  __device__ __forceinline__ void load(int k0, int64_t ld, int nk, const int32_t* index, int nsrc) {
+    if constexpr (KC) {
+      if (k0 + TK <= nk) {  // the whole stage lies within K
 #pragma unroll
-      for (int j = 0; j < NU; ++j) lds[j * NT + tid] = reg[j];
+        for (int j = 0; j < NU; ++j) __builtin_memcpy(&reg[j], p[j] + k0, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NU; ++j) reg[j] = load_unit(p[j] + k0, nk - k0 - at[j]);
+      }
+    } else {
+      int64_t row[NU];
+      bool ok[NU];
+#pragma unroll
+      for (int j = 0; j < NU; ++j) {
+        ok[j] = row_of(j, k0, nk, index, nsrc, &row[j]);
+        reg[j] = u32x4_t{0u, 0u, 0u, 0u};
+        if (lim[j] >= CE) __builtin_memcpy(&reg[j], p[j] + row[j] * ld, 16);
+        else reg[j] = load_unit(p[j] + row[j] * ld, lim[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < NU; ++j) reg[j] = ok[j] ? reg[j] : u32x4_t{0u, 0u, 0u, 0u};
     }
+  }
+  __device__ __forceinline__ void commit(int tid, u32x4_t* lds) const {
+#pragma unroll
+    for (int j = 0; j < NU; ++j) lds[j * NT + tid] = reg[j];
   }
 };
 
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ u32x2_t read_tr(const bf16_t* p) {
+// The transposing reads of NB blocks of 16 tile rows at LDS addresses p[i]: for
+// the 32 values of k from each of two starts KSTEP bytes apart, rows of k 0..3
+// and 4..7 (KROWS bytes apart) of each 16 lanes.  Lane 4v + q of 16 reads row
+// v, columns 4q .. 4q+3, and receives column l % 16 of the four rows.  One
+// block that also waits for them, so the values are defined when it ends, and
+// the compiler adds no wait for the copies to LDS that are in flight.
+template <int KROWS, int KSTEP>
+__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[1], u32x4_t (&f)[1][2]) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                         LDS_AS(s16x4_t, const_cast<bf16_t*>(p))));
+  u32x2_t r[4];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4\n\t"
+      "ds_read_b64_tr_b16 %1, %4 offset:%5\n\t"
+      "ds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
+      "ds_read_b64_tr_b16 %3, %4 offset:%7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(p[0]), "n"(KROWS), "n"(KSTEP), "n"(KSTEP + KROWS)
+      : "memory");
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+    f[0][ks] = u32x4_t{r[2 * ks][0], r[2 * ks][1], r[2 * ks + 1][0], r[2 * ks + 1][1]};
 #else
   (void)p;
-  return u32x2_t{0u, 0u};
+  (void)f;
+#endif
+}
+template <int KROWS, int KSTEP>
+__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[2], u32x4_t (&f)[2][2]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  u32x2_t r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:%11\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
+        "=&v"(r[7])
+      : "v"(p[0]), "v"(p[1]), "n"(KROWS), "n"(KSTEP), "n"(KSTEP + KROWS)
+      : "memory");
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x2_t lo = r[4 * ks + 2 * i], hi = r[4 * ks + 2 * i + 1];
+      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    }
+#else
+  (void)p;
+  (void)f;
+#endif
+}
+template <int KROWS, int KSTEP>
+__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[4], u32x4_t (&f)[4][2]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  u32x2_t r[16];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n\t"
+      "ds_read_b64_tr_b16 %1, %16 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %2, %17\n\t"
+      "ds_read_b64_tr_b16 %3, %17 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %4, %18\n\t"
+      "ds_read_b64_tr_b16 %5, %18 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %6, %19\n\t"
+      "ds_read_b64_tr_b16 %7, %19 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %8, %16 offset:%21\n\t"
+      "ds_read_b64_tr_b16 %9, %16 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %10, %17 offset:%21\n\t"
+      "ds_read_b64_tr_b16 %11, %17 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %12, %18 offset:%21\n\t"
+      "ds_read_b64_tr_b16 %13, %18 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %14, %19 offset:%21\n\t"
+      "ds_read_b64_tr_b16 %15, %19 offset:%22\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
+        "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]),
+        "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+      : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(KROWS), "n"(KSTEP), "n"(KSTEP + KROWS)
+      : "memory");
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2_t lo = r[8 * ks + 2 * i], hi = r[8 * ks + 2 * i + 1];
+      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    }
+#else
+  (void)p;
+  (void)f;
 #endif
 }
 
-// The operand of 16 tile rows from i0 for the k sub-step ks.  bf16: 32 values
-// of k, lane l row l % 16 and k = 8 (l / 16) + 0..7.  fp32: 16 values of k,
-// element e of lane l is k = 4 (l / 16) + e, used by the e-th of four MFMAs.
-template <typename T, bool KC, int R>
-__device__ __forceinline__ u32x4_t read_frag(const u32x4_t* lds, int i0, int ks, int lane) {
-  const int l16 = lane & 15, G = lane >> 4;
-  if constexpr (KC) {
-    return lds[unit_at<T, true, R>(i0 + l16, 4 * ks + G)];
-  } else if constexpr (sizeof(T) == 2) {
-    // 4 rows of k by 16 columns for each 16 lanes: lane 4v + q reads row v,
-    // columns 4q .. 4q+3, and receives column l % 16 of the four rows
-    const int k = 32 * ks + 8 * G + (l16 >> 2), q = l16 & 3;
-    const bf16_t* base = reinterpret_cast<const bf16_t*>(lds);
-    const bf16_t* a = base + 8 * unit_at<T, false, R>(k, (i0 >> 3) + (q >> 1)) + 4 * (q & 1);
-    const bf16_t* b = base + 8 * unit_at<T, false, R>(k + 4, (i0 >> 3) + (q >> 1)) + 4 * (q & 1);
-    const u32x2_t lo = read_tr(a), hi = read_tr(b);
-    return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-  } else {
-    const uint32_t* base = reinterpret_cast<const uint32_t*>(lds);
-    u32x4_t v;
+// Reads a stage's operands of NB blocks of 16 tile rows from row0 on, for both
+// sub-steps.  bf16: 32 values of k each, lane l row l % 16 and k = 8 (l / 16) +
+// 0..7.  fp32: 16 values of k, element e of lane l is k = 4 (l / 16) + e, used
+// by the e-th of four MFMAs.
+template <typename T, bool KC, int R, int NB> struct Reader {
+  uint32_t at[KC ? 2 : NB];
+
+  __device__ __forceinline__ void init(int row0, int lane) {
+    const int l16 = lane & 15, G = lane >> 4;
+    if constexpr (KC) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      v[e] = base[4 * unit_at<T, false, R>(16 * ks + 4 * G + e, (i0 >> 2) + (l16 >> 2)) + (l16 & 3)];
-    return v;
+      for (int ks = 0; ks < 2; ++ks) at[ks] = 16 * unit_at<T, true, R>(row0 + l16, 4 * ks + G);
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        at[i] = 16 * unit_at<T, false, R>(8 * G + (l16 >> 2), (row0 >> 3) + 2 * i + ((l16 & 3) >> 1)) +
+                8 * (l16 & 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        at[i] = 16 * unit_at<T, false, R>(4 * G, (row0 >> 2) + 4 * i + (l16 >> 2)) + 4 * (l16 & 3);
+    }
   }
-}
+  __device__ __forceinline__ void read(const u32x4_t* lds, u32x4_t (&f)[NB][2]) const {
+    const char* const base = reinterpret_cast<const char*>(lds);
+    if constexpr (KC) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+          f[i][ks] = *reinterpret_cast<const u32x4_t*>(base + at[ks] + 2048 * i);
+    } else if constexpr (sizeof(T) == 2) {
+      // the unit permutation is that of 4 and of 32 rows further on
+      const uint32_t start = (uint32_t)(uintptr_t)LDS_AS(char, const_cast<char*>(base));
+      uint32_t q[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) q[i] = start + at[i];
+      read_tr_blocks<4 * 2 * R, 32 * 2 * R>(q, f);
+    } else {
+      // of the 3 rows further on, and of 16
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            f[i][ks][e] = *reinterpret_cast<const uint32_t*>(base + at[i] + (16 * ks + e) * 4 * R);
+    }
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ f32x4_t mma(u32x4_t x, u32x4_t y, f32x4_t acc) {
@@ -523,21 +653,21 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
   }
 }
 
-// TM x TN results by WM x WN waves.  DMA: both operands by 16-byte copies to
-// LDS (16-byte aligned rows), else through registers.  WHOLE: see low_rank.
-template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA, bool WHOLE>
+// TM x TN results by WM x WN waves.  DEPTH > 0: both operands are copied
+// straight to LDS (rows on 4-byte boundaries), DEPTH - 1 stages ahead in a ring
+// of DEPTH; where K ends inside a unit, its last stage goes through registers.
+// DEPTH 0: through registers, at any alignment, two stages.  WHOLE: see low_rank.
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
   constexpr int NT = 64 * WM * WN;
   constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
   constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE == kAdapt;  // gathered operands
-  constexpr int TK = 128 / (int)sizeof(T);
-  constexpr int KS = 2;  // sub-steps of a stage: 32 (bf16) or 16 (fp32) values of k
+  constexpr int CE = 16 / (int)sizeof(T), TK = 8 * CE;
   constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
-  constexpr int XU = 8 * TM, YU = 8 * TN;
+  constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
 
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  u32x4_t* const buf0 = reinterpret_cast<u32x4_t*>(smem);
-  u32x4_t* const buf1 = buf0 + XU + YU;
+  u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
@@ -546,11 +676,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
 
   Tile<T, TO> w;
   if (!setup_tile<T, TO, MODE, TM, TN>(a, band, &w)) return;
-  Stager<T, XKC, TM, NT, DMA, XG> sx;
-  Stager<T, YKC, TN, NT, DMA, YG> sy;
-  sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, w.K, nullptr, 0);
-  sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, w.K, YG ? w.rows : nullptr, a.Nsrc);
+  Stager<T, XKC, TM, NT, XG> sx;
+  Stager<T, YKC, TN, NT, YG> sy;
   const int32_t* const xrows = XG ? w.rows : nullptr;
+  Reader<T, XKC, TM, NI> rx;
+  Reader<T, YKC, TN, NJ> ry;
+  rx.init(xrow(0), lane);
+  ry.init(yrow(0), lane);
 
   f32x4_t acc[NI][NJ];
 #pragma unroll
@@ -559,51 +691,77 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
+    u32x4_t xf[NI][2], yf[NJ][2];
+    rx.read(buf, xf);
+    ry.read(buf + XU, yf);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      u32x4_t xf[NI], yf[NJ];
-#pragma unroll
-      for (int i = 0; i < NI; ++i) xf[i] = read_frag<T, XKC, TM>(buf, xrow(i), ks, lane);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) yf[j] = read_frag<T, YKC, TN>(buf + XU, yrow(j), ks, lane);
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i], yf[j], acc[i][j]);
-    }
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i][ks], yf[j][ks], acc[i][j]);
+  };
+  auto load = [&](int s) __attribute__((always_inline)) {
+    sx.load(s * TK, a.ldx, w.K, xrows, a.Nsrc);
+    sy.load(s * TK, a.ldy, w.K, nullptr, 0);
+  };
+  auto commit = [&](int s) __attribute__((always_inline)) {
+    sx.commit(tid, ring + (s & 1) * STAGE);
+    sy.commit(tid, ring + (s & 1) * STAGE + XU);
   };
 
-  const int n_st = (w.K + TK - 1) / TK;
-  if (n_st > 0) {
-    sx.issue(tid, buf0, 0, a.ldx, w.K, xrows, a.Nsrc);
-    sy.issue(tid, buf0 + XU, 0, a.ldy, w.K, nullptr, 0);
-    sx.commit(tid, buf0);
-    sy.commit(tid, buf0 + XU);
-  }
-  for (int s = 0; s < n_st; ++s) {
-    u32x4_t* const cur = s & 1 ? buf1 : buf0;
-    u32x4_t* const nxt = s & 1 ? buf0 : buf1;
-    // this stage has landed and every wave is done with the other buffer
-    __syncthreads();
-    if (s + 1 < n_st) {
-      sx.issue(tid, nxt, (s + 1) * TK, a.ldx, w.K, xrows, a.Nsrc);
-      sy.issue(tid, nxt + XU, (s + 1) * TK, a.ldy, w.K, nullptr, 0);
-    }
-    compute(cur);
-    if (s + 1 < n_st) {
-      sx.commit(tid, nxt);
-      sy.commit(tid, nxt + XU);
+  if (w.K > 0) {
+    sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, nullptr, 0);
+    sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, YG ? w.rows : nullptr, a.Nsrc);
+    if constexpr (DEPTH > 0) {
+      constexpr int COPIES = sx.NU + sy.NU;  // of a thread and stage
+      const bool ends_inside = (XKC || YKC) && w.K % CE != 0;
+      const int n_st = ends_inside ? w.K / TK : (w.K + TK - 1) / TK;
+      auto copy = [&](int s) __attribute__((always_inline)) {
+        // past the last stage: zeros, so that every wait counts the same
+        u32x4_t* const dst = ring + (s % DEPTH) * STAGE;
+        const int K = s < n_st ? w.K : 0;
+        sx.copy(tid, dst, s * TK, a.ldx, K, xrows, a.Nsrc);
+        sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
+      };
+#pragma unroll
+      for (int s = 0; s < DEPTH - 1; ++s) copy(s);
+      for (int s = 0; s < n_st; ++s) {
+        // this wave's copies of stage s have landed (the later ones' may be in
+        // flight), then every wave's; every wave is done with stage s - 1
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
+        copy(s + DEPTH - 1);
+        compute(ring + (s % DEPTH) * STAGE);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
+      if (ends_inside && n_st * TK < w.K) {
+        load(n_st);
+        __syncthreads();
+        commit(0);
+        __syncthreads();
+        compute(ring);
+      }
+    } else {
+      const int n_st = (w.K + TK - 1) / TK;
+      load(0);
+      commit(0);
+      for (int s = 0; s < n_st; ++s) {
+        __syncthreads();  // stage s is there; every wave is done with stage s - 1
+        if (s + 1 < n_st) load(s + 1);
+        compute(ring + (s & 1) * STAGE);
+        if (s + 1 < n_st) commit(s + 1);
+      }
     }
   }
   if constexpr (MODE == kAdapt) low_rank<T, TO, WHOLE>(a, ad, w, lane, acc, xrow, yrow);
-  store_tile<T, TO, MODE, false>(a, w, lane, acc, xrow, yrow);
+  store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 
-template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, bool DMA, bool WHOLE = true>
+template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE = true>
 hipError_t launch_tiles(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
                         hipStream_t stream) {
-  auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DMA, WHOLE>;
-  const int lds = 2 * 8 * (TM + TN) * 16;
+  auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DEPTH, WHOLE>;
+  const int lds = (DEPTH > 0 ? DEPTH : 2) * 8 * (TM + TN) * 16;
   if (lds > 64 * 1024) {
     const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
     if (e != hipSuccess) return e;

@@ -33,79 +33,6 @@ constexpr int kPipeRows = 4096;                  // source rows kept in LDS (gat
 constexpr int kPipeLds = 8 * kPipeHalf * 16;     // two stages
 enum Half { kY0 = 0, kX0 = 1, kY1 = 2, kX1 = 3 };
 
-// Eight (NB = 2) or sixteen (NB = 4) transposing reads of the operands of NB
-// blocks of 16 tile rows, whose addresses are p[i]: for each 32 values of k
-// (8 KB apart) rows of k 0..3 and 4..7 (1 KB apart) of each 16 lanes.  One
-// block that also waits for them, so the values are defined when it ends and
-// the compiler adds no wait for the copies in flight.
-__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[2], u32x4_t (&f)[2][2]) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  u32x2_t r[8];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\t"
-      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %2, %9\n\t"
-      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %4, %8 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %5, %8 offset:9216\n\t"
-      "ds_read_b64_tr_b16 %6, %9 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %7, %9 offset:9216\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
-        "=&v"(r[7])
-      : "v"(p[0]), "v"(p[1])
-      : "memory");
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x2_t lo = r[4 * ks + 2 * i], hi = r[4 * ks + 2 * i + 1];
-      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-    }
-#else
-  (void)p;
-  (void)f;
-#endif
-}
-__device__ __forceinline__ void read_tr_blocks(const uint32_t (&p)[4], u32x4_t (&f)[4][2]) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  u32x2_t r[16];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %16\n\t"
-      "ds_read_b64_tr_b16 %1, %16 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %2, %17\n\t"
-      "ds_read_b64_tr_b16 %3, %17 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %4, %18\n\t"
-      "ds_read_b64_tr_b16 %5, %18 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %6, %19\n\t"
-      "ds_read_b64_tr_b16 %7, %19 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %8, %16 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %9, %16 offset:9216\n\t"
-      "ds_read_b64_tr_b16 %10, %17 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %11, %17 offset:9216\n\t"
-      "ds_read_b64_tr_b16 %12, %18 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %13, %18 offset:9216\n\t"
-      "ds_read_b64_tr_b16 %14, %19 offset:8192\n\t"
-      "ds_read_b64_tr_b16 %15, %19 offset:9216\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]),
-        "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]),
-        "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
-      : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
-      : "memory");
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x2_t lo = r[8 * ks + 2 * i], hi = r[8 * ks + 2 * i + 1];
-      f[i][ks] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-    }
-#else
-  (void)p;
-  (void)f;
-#endif
-}
-
 // One operand: its copies to LDS and its reads from there.  KC: k last, rows
 // may be gathered; else the tile's own index last, rows of k may be gathered.
 // NB: blocks of 16 rows a wave reads from each half.
@@ -201,7 +128,7 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
       uint32_t q[NB];
 #pragma unroll
       for (int i = 0; i < NB; ++i) q[i] = frag[0][i] + (PAR * 4 * kPipeHalf * 16 + half);
-      read_tr_blocks(q, f);
+      read_tr_blocks<1024, 8192>(q, f);
     }
   }
 };

@@ -7,10 +7,11 @@ namespace {
 
 using namespace group;
 
-// Whether copies of whole 16-byte units may be used: every row starts on a
-// 16-byte boundary and holds whole units.
-bool units_ok(const void* p, int64_t ld, int64_t extent, int esize) {
-  return ((uintptr_t)p & 15) == 0 && (ld * esize) % 16 == 0 && (extent * esize) % 16 == 0;
+// Whether an operand can be copied straight to LDS, 16 bytes at a time: rows
+// on 4-byte boundaries, and where its own index is last, whole units of it (k
+// last: the kernel sees to the end of K).
+bool copies_ok(const void* p, int64_t ld, int64_t extent, bool kc, int esize) {
+  return ((uintptr_t)p & 3) == 0 && (ld * esize) % 4 == 0 && (kc || (extent * esize) % 16 == 0);
 }
 
 // Tiles that the worst split of Np rows into Ng groups and the rows past them
@@ -27,35 +28,39 @@ template <int MODE> int64_t row_tiles_of(const GroupArgs& a, int TN) {
   return row_tiles(a.N, a.Ng, MODE != kAdapt, TN);
 }
 
-template <typename T, typename TO, int MODE, bool DMA>
+template <typename T, typename TO, int MODE, bool WHOLE>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
-  if constexpr (sizeof(T) == 2 && DMA) {
-    const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
-    if (rows >= 192 && a.M >= 192 && pipe_fits(a, MODE) && ad.nlp == ad.Nl)
+  constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
+  const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
+  const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
+  if constexpr (sizeof(T) == 2 && WHOLE)
+    if (dma && rows >= 192 && a.M >= 192 && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE))
       return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
+  // results of 128 x 128 tiles: do they make a workgroup for each CU?
+  const int64_t big = row_tiles_of<MODE>(a, 128) * ((a.M + 127) / 128);
+  if (big >= 256) {
+    if (dma)
+      return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
+    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
   }
-  if (MODE == kAdapt && ad.nlp != ad.Nl)
-    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA, MODE != kAdapt>(
-        a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
-  return launch_tiles<T, TO, MODE, 128, 128, 2, 2, DMA>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
+  if (dma)
+    return launch_tiles<T, TO, MODE, 64, 64, 2, 2, 4, WHOLE>(a, ad, row_tiles_of<MODE>(a, 64), 16, stream);
+  return launch_tiles<T, TO, MODE, 64, 64, 2, 2, 0, WHOLE>(a, ad, row_tiles_of<MODE>(a, 64), 16, stream);
 }
 
 template <typename T, typename TO, int MODE>
-hipError_t launch_aligned(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
-  // a KC operand's rows hold K values, an MC operand's the tile index
-  const int64_t ex = MODE == kFwd || MODE == kAdapt ? a.K : a.M;
-  const int64_t ey = MODE == kBwdKer ? a.N : a.K;
-  if (units_ok(a.X, a.ldx, ex, sizeof(T)) && units_ok(a.Y, a.ldy, ey, sizeof(T)))
-    return launch_sized<T, TO, MODE, true>(a, ad, stream);
-  return launch_sized<T, TO, MODE, false>(a, ad, stream);
+hipError_t launch_ranks(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+  if constexpr (MODE == kAdapt)
+    if (ad.nlp != ad.Nl) return launch_sized<T, TO, MODE, false>(a, ad, stream);
+  return launch_sized<T, TO, MODE, true>(a, ad, stream);
 }
 
 template <int MODE>
 hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
   switch (dtype) {
-    case CNN_F32: return launch_aligned<float, float, MODE>(a, ad, stream);
-    case CNN_BF16: return launch_aligned<bf16_t, float, MODE>(a, ad, stream);
-    default: return launch_aligned<bf16_t, bf16_t, MODE>(a, ad, stream);
+    case CNN_F32: return launch_ranks<float, float, MODE>(a, ad, stream);
+    case CNN_BF16: return launch_ranks<bf16_t, float, MODE>(a, ad, stream);
+    default: return launch_ranks<bf16_t, bf16_t, MODE>(a, ad, stream);
   }
 }
 
