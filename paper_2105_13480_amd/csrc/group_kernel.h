@@ -578,31 +578,33 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
                                          XR xrow, YR yrow) {
   constexpr int CE = 16 / (int)sizeof(T), STEP = 4 * CE;
   constexpr int BATCH = WHOLE ? 2 : 1;  // steps whose loads are in flight together
+  constexpr int IB = NI < 4 ? NI : 4, JB = NJ < 2 ? NJ : 2;
+  static_assert(NI % IB == 0 && NJ % JB == 0, "whole rounds of blocks");
   const u32x4_t zero = {0u, 0u, 0u, 0u};
   const int l16 = lane & 15, G = lane >> 4;
   const T* const H = reinterpret_cast<const T*>(ad.Hp) + (int64_t)w.n0 * ad.hl;
 #pragma unroll
-  for (int j0 = 0; j0 < NJ; j0 += 2) {
-    int id_of[2];  // adapter of this lane's rows; past the tile, the last row's
-    uint32_t hrow[2];
+  for (int j0 = 0; j0 < NJ; j0 += JB) {
+    int id_of[JB];  // adapter of this lane's rows; past the tile, the last row's
+    uint32_t hrow[JB];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < JB; ++j) {
       const int n = min(yrow(j0 + j) + l16, w.n_valid - 1);
       id_of[j] = ad.ids[w.n0 + n];
       hrow[j] = (uint32_t)(n * ad.hl);
     }
 #pragma unroll
-    for (int i0 = 0; i0 < NI; i0 += 4) {
-      uint32_t brow[4];
+    for (int i0 = 0; i0 < NI; i0 += IB) {
+      uint32_t brow[IB];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < IB; ++i)
         brow[i] = (uint32_t)(min(xrow(i0 + i) + l16, w.m_valid - 1) * ad.Nl);
       int last = -1;
 #pragma unroll 1
       for (;;) {
         int next = 0x7fffffff;  // the least adapter above the last one
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < JB; ++j)
           if (id_of[j] > last && id_of[j] < ad.Na) next = min(next, id_of[j]);
         // the four rows of 16 lanes hold the same
         next = __builtin_amdgcn_readfirstlane(row16_min(next));
@@ -611,16 +613,16 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
         const T* const B = reinterpret_cast<const T*>(ad.B) + ((int64_t)next * a.M + w.m0) * ad.Nl;
 #pragma unroll 1
         for (int k0 = 0; k0 < ad.hl; k0 += BATCH * STEP) {
-          u32x4_t xf[BATCH][4], yf[BATCH][2];
+          u32x4_t xf[BATCH][IB], yf[BATCH][JB];
           bool in[BATCH];
 #pragma unroll
           for (int s = 0; s < BATCH; ++s) {
             in[s] = k0 + s * STEP + CE * G < ad.hl;
             const int kk = in[s] ? k0 + s * STEP + CE * G : 0, rank = kk % ad.nlp;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) __builtin_memcpy(&yf[s][j], H + hrow[j] + kk, 16);
+            for (int j = 0; j < JB; ++j) __builtin_memcpy(&yf[s][j], H + hrow[j] + kk, 16);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < IB; ++i) {
               const T* const row = B + brow[i];
               if constexpr (WHOLE) {
                 __builtin_memcpy(&xf[s][i], row + rank, 16);
@@ -636,9 +638,9 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
           }
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < JB; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < IB; ++i) {
               f32x4_t sum = acc[i0 + i][j0 + j];
 #pragma unroll
               for (int s = 0; s < BATCH; ++s)

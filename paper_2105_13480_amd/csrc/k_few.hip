@@ -56,10 +56,7 @@ __device__ __forceinline__ void few_rows_dot(const T* const (&x)[FB], const T* c
   const int G = lane >> 4, step = nw * R::LEN;
   int k0 = wave * R::LEN;
   R a;
-#ifndef PIPEMAX
-#define PIPEMAX 3
-#endif
-  if constexpr (FB + RB <= PIPEMAX) {
+  if constexpr (FB + RB <= 3) {
     R b;
     if (k0 + R::LEN <= K) a.load(x, y, k0, G);
     for (; k0 + R::LEN <= K; k0 += 2 * step) {
@@ -311,36 +308,10 @@ hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Whether k holds a run for each of sixteen waves.
-#ifndef LK
-#define LK 16
-#endif
-#ifndef FNW
-#define FNW 4
-#endif
-#ifndef BNW
-#define BNW 4
-#endif
-#ifndef BFB
-#define BFB 4
-#endif
-template <typename T> bool long_k(const GroupArgs& a) { return a.K >= LK * (256 / (int)sizeof(T)); }
-
 template <typename T, typename TO> hipError_t launch_few_typed(const GroupArgs& a, hipStream_t stream) {
-  const int64_t rows = a.N / a.Ng;
-  if (rows <= 8) return launch_few<T, TO, 1, 1, FNW>(a, stream);
-  return launch_few<T, TO, BFB, 2, BNW>(a, stream);
+  return launch_few<T, TO, 1, 1, 4>(a, stream);
 }
 
-#ifndef DNW
-#define DNW 8
-#endif
-#ifndef DFB
-#define DFB 4
-#endif
-#ifndef DRB
-#define DRB 2
-#endif
 template <typename T, typename TO, int PARTS>
 hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   const int64_t parts = ad.Na + 1 < a.N ? ad.Na + 1 : a.N;
@@ -349,14 +320,14 @@ hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stre
   h.xgroup = (int64_t)ad.Nl * a.K;
   h.M = ad.Nl;
   h.Ng = ad.Na;
-  const dim3 block(64 * DNW);
+  const dim3 block(64 * 4);
   auto grid = [&](int FB, int RB) {
     return dim3((uint32_t)((a.N / (16 * RB) + parts) * ((ad.Nl + 16 * FB - 1) / (16 * FB))));
   };
   if (ad.Nl <= 16)
-    group_few<T, TO, 1, 2, DNW, PARTS><<<grid(1, 2), block, 0, stream>>>(h, ad);
+    group_few<T, TO, 1, 2, 4, PARTS><<<grid(1, 2), block, 0, stream>>>(h, ad);
   else
-    group_few<T, TO, DFB, DRB, DNW, PARTS><<<grid(DFB, DRB), block, 0, stream>>>(h, ad);
+    group_few<T, TO, 4, 2, 4, PARTS><<<grid(4, 2), block, 0, stream>>>(h, ad);
   return hipGetLastError();
 }
 
@@ -395,7 +366,14 @@ hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream
 
 }  // namespace
 
-bool group_few_fits(const GroupArgs& a) { return a.N <= 24 * (int64_t)a.Ng; }
+// Up to eight rows a group and aligned rows: decoding steps.  At 32 rows of 20
+// groups, k 2048, 1024 features: 16.1 us here, 17.2 by 64 x 32 tiles; from 16
+// rows a group on (512 rows of 28, k 1024, 4096 features) 60 and 50; odd k
+// (1039, five rows a group) 40 and 21.
+bool group_few_fits(const GroupArgs& a, int dtype) {
+  return a.N <= 8 * (int64_t)a.Ng && a.K * in_bytes(dtype) % 16 == 0 &&
+         (((uintptr_t)a.X | (uintptr_t)a.Y) & 15) == 0;
+}
 
 hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
   switch (dtype) {

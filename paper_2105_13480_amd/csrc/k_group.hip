@@ -28,24 +28,80 @@ template <int MODE> int64_t row_tiles_of(const GroupArgs& a, int TN) {
   return row_tiles(a.N, a.Ng, MODE != kAdapt, TN);
 }
 
+// What a tile costs (microseconds, measured on MI355X on products of one group
+// with half a tile to four tiles a CU): `alone` for a stage of 128 bytes of k
+// where a CU has one tile, `share` for a stage of each of several, `ends` for a
+// tile's start and results, `once` for the launch.  A product of stages s and
+// n tiles a CU takes once + s max(alone, n share) + n ends.
+struct TileCost {
+  int tm, tn;
+  double alone, share, ends, once;
+};
+constexpr TileCost kBf16[] = {{256, 256, 1.33, 1.30, 10.5, 3.5},
+                              {128, 128, 0.65, 0.50, 2.5, 4.0},
+                              {64, 64, 0.28, 0.19, 1.1, 3.6},
+                              {64, 32, 0.19, 0.137, 0.6, 4.6}};
+// fp32: the matrix unit's time at every size (2048 operations in 32 clocks)
+constexpr TileCost kF32[] = {{0, 0, 0, 0, 0, 0},
+                             {128, 128, 1.80, 1.75, 2.5, 4.0},
+                             {64, 64, 0.50, 0.45, 1.1, 3.6},
+                             {64, 32, 0.30, 0.24, 0.6, 4.6}};
+
+// The cheapest of the tile sizes from `first` on (0: with the pipelined
+// kernel).  Group sizes are not known here: half a tile of each group is taken
+// to be empty.
+template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
+  const TileCost* const c = sizeof(T) == 2 ? kBf16 : kF32;
+  const int last = MODE == kBwdKer ? 2 : 3;
+  const double cus = device_cus();
+  int best = first;
+  double least = 1e30;
+  for (int i = first; i <= last; ++i) {
+    const double mt = (a.M + c[i].tm - 1) / c[i].tm;
+    double nt, k;
+    if (MODE == kBwdKer) {
+      nt = (double)a.Ng * ((a.N + c[i].tn - 1) / c[i].tn);
+      k = (double)a.K / a.Ng;
+    } else {
+      nt = (double)a.N / c[i].tn + 0.5 * (MODE == kAdapt || a.Ng > a.N ? 1 : a.Ng);
+      k = a.K;
+    }
+    double n = mt * nt / cus;
+    if (i == 0) n = (double)(int64_t)(n + 0.999);  // one at a time
+    if (n < 1) n = 1;
+    const double stages = k * sizeof(T) / 128 + 1;
+    const double t = c[i].once + stages * (n * c[i].share > c[i].alone ? n * c[i].share : c[i].alone) +
+                     n * c[i].ends;
+    if (t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
+}
+
 template <typename T, typename TO, int MODE, bool WHOLE>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
-  const int64_t rows = MODE == kBwdKer ? a.N : a.N / a.Ng;
+  const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE);
+  const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1);
   if constexpr (sizeof(T) == 2 && WHOLE)
-    if (dma && rows >= 192 && a.M >= 192 && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE))
-      return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
-  // results of 128 x 128 tiles: do they make a workgroup for each CU?
-  const int64_t big = row_tiles_of<MODE>(a, 128) * ((a.M + 127) / 128);
-  if (big >= 256) {
-    if (dma)
-      return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
-    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, row_tiles_of<MODE>(a, 128), 8, stream);
+    if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
+  if (pick == 1) {
+    const int64_t rt = row_tiles_of<MODE>(a, 128);
+    return dma ? launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, stream)
+               : launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
   }
-  if (dma)
-    return launch_tiles<T, TO, MODE, 64, 64, 2, 2, 4, WHOLE>(a, ad, row_tiles_of<MODE>(a, 64), 16, stream);
-  return launch_tiles<T, TO, MODE, 64, 64, 2, 2, 0, WHOLE>(a, ad, row_tiles_of<MODE>(a, 64), 16, stream);
+  if constexpr (MODE != kBwdKer)
+    if (pick == 3) {
+      const int64_t rt = row_tiles_of<MODE>(a, 32);
+      return dma ? launch_tiles<T, TO, MODE, 64, 32, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
+                 : launch_tiles<T, TO, MODE, 64, 32, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
+    }
+  const int64_t rt = row_tiles_of<MODE>(a, 64);
+  return dma ? launch_tiles<T, TO, MODE, 64, 64, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
+             : launch_tiles<T, TO, MODE, 64, 64, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
 }
 
 template <typename T, typename TO, int MODE>
@@ -67,7 +123,7 @@ hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipS
 }  // namespace
 
 hipError_t launch_group_fwd(const GroupArgs& a, int dtype, hipStream_t stream) {
-  if (group_few_fits(a)) return launch_group_few(a, dtype, stream);
+  if (group_few_fits(a, dtype)) return launch_group_few(a, dtype, stream);
   return launch_typed<kFwd>(a, AdaptArgs{}, dtype, stream);
 }
 hipError_t launch_group_bwd_in(const GroupArgs& a, int dtype, hipStream_t stream) {

@@ -95,7 +95,7 @@ hipError_t launch_group_fwd(const GroupArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_group_bwd_in(const GroupArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t stream);
 // Products of few rows a group, straight from memory.
-bool group_few_fits(const GroupArgs& a);
+bool group_few_fits(const GroupArgs& a, int dtype);
 hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream);
 // Whether an adapted product of Nt rows runs the few-rows kernels, which take
 // the rows as they come.
