@@ -95,6 +95,7 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
   const T* p[NU];  // the unit's first element at k = 0, or (rows of k) of a row
   int at[NU];      // KC: the unit's first k within a stage; else its row of k
   int lim[KC ? 1 : NU];  // elements of the row from the unit's first
+  int src[GATHER && !KC ? NU : 1];
   u32x4_t reg[NU];
 
   // base: the tensor at its first k; rows [i0, i0 + n) of the tile index are
@@ -124,7 +125,15 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     }
   }
 
-  // The row of k that unit j reads in the stage at k0, of nk; false: none.
+  // Gathered rows of k: the source rows of the stage at k0 (of nk rows of k),
+  // asked for a stage before they are used.
+  __device__ __forceinline__ void fetch(int k0, int nk, const int32_t* index) {
+    if constexpr (GATHER && !KC)
+      if (index)
+#pragma unroll
+        for (int j = 0; j < NU; ++j) src[j] = index[max(min(k0 + at[j], nk - 1), 0)];
+  }
+  // The row that unit j reads in the stage at k0 (the one fetched); false: none.
   __device__ __forceinline__ bool row_of(int j, int k0, int nk, const int32_t* index, int nsrc,
                                          int64_t* row) const {
     const int k = k0 + at[j];
@@ -132,7 +141,7 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     *row = max(min(k, nk - 1), 0);  // the first is there even where nk = 0 asks for zeros
     if constexpr (GATHER)
       if (index) {
-        *row = index[*row];
+        *row = src[j];
         if (*row < 0 || *row >= nsrc) {
           *row = 0;
           ok = false;
@@ -353,14 +362,16 @@ __device__ __forceinline__ f32x4_t mma(u32x4_t x, u32x4_t y, f32x4_t acc) {
   }
 }
 
-// Four consecutive results from `m` of one row, as many as lie below M.
+// Four consecutive results from `m` of one row, as many as lie below M, at any
+// element alignment.
 template <typename TO>
-__device__ __forceinline__ void store4(TO* row, int m, int M, f32x4_t v, bool whole) {
-  if (whole && m + 4 <= M) {
+__device__ __forceinline__ void store4(TO* row, int m, int M, f32x4_t v) {
+  if (m + 4 <= M) {
     if constexpr (sizeof(TO) == 4) {
-      *reinterpret_cast<f32x4_t*>(row + m) = v;
+      __builtin_memcpy(row + m, &v, 16);
     } else {
-      *reinterpret_cast<u32x2_t*>(row + m) = u32x2_t{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+      const u32x2_t p = {pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+      __builtin_memcpy(row + m, &p, 8);
     }
   } else {
 #pragma unroll
@@ -533,8 +544,7 @@ template <typename T, typename TO, int MODE, bool MASK, int NI, int NJ, typename
 __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>& w, int lane,
                                            f32x4_t (&acc)[NI][NJ], XR xrow, YR yrow) {
   const int l16 = lane & 15, m0 = w.m0 + 4 * (lane >> 4);
-  // rows whose starts and ends let every four results be stored at once
-  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0 && (a.M & 3) == 0;
+  const bool fours = (a.M & 3) == 0;  // no row ends inside four results
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int n = yrow(j) + l16;
@@ -555,10 +565,10 @@ __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>
       f32x4_t v = acc[i][j];
       if constexpr (MASK)
         if (!live) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (whole) {
-        if (m < a.M) store4(row, m, a.M, v, true);
+      if (fours) {
+        if (m < a.M) store4(row, m, m + 4, v);
       } else {
-        store4(row, m, a.M, v, false);
+        store4(row, m, a.M, v);
       }
     }
   }
@@ -705,6 +715,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
   };
   auto load = [&](int s) __attribute__((always_inline)) {
     sx.load(s * TK, a.ldx, w.K, xrows, a.Nsrc);
+    sx.fetch((s + 1) * TK, w.K, xrows);
     sy.load(s * TK, a.ldy, w.K, nullptr, 0);
   };
   auto commit = [&](int s) __attribute__((always_inline)) {
@@ -715,6 +726,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
   if (w.K > 0) {
     sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, nullptr, 0);
     sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, YG ? w.rows : nullptr, a.Nsrc);
+    sx.fetch(0, w.K, xrows);
     if constexpr (DEPTH > 0) {
       constexpr int COPIES = sx.NU + sy.NU;  // of a thread and stage
       const bool ends_inside = (XKC || YKC) && w.K % CE != 0;
@@ -724,6 +736,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
         u32x4_t* const dst = ring + (s % DEPTH) * STAGE;
         const int K = s < n_st ? w.K : 0;
         sx.copy(tid, dst, s * TK, a.ldx, K, xrows, a.Nsrc);
+        // before the other copies, so that waiting for it leaves those in flight
+        sx.fetch((s + 1) * TK, w.K, xrows);
         sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
       };
 #pragma unroll

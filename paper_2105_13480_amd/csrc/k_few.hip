@@ -162,8 +162,7 @@ __global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) 
     f32x4_t s = block_sum(red, blk, NW, lane);
     if (!live || (none >> b & 1)) s = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if constexpr (PARTS == 0) {
-      const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
-      store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s, whole);
+      store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s);
     } else {
       const float scale = ad.scales ? ad.scales[t.g] : 1.f;
       T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(t.n0 + n) * ad.hl;
@@ -219,7 +218,7 @@ __global__ __launch_bounds__(64 * NW) void adapt_few_sums(GroupArgs a, AdaptArgs
         leave_sums(red, acc, wave, NW, lane);
         if (l16 < n_valid && id == next)
           for (int b = wave; b < DF; b += NW)
-            store4(H, r0 + 16 * b + 4 * G, ad.Nl, block_sum(red, b, NW, lane), (ad.Nl & 3) == 0);
+            store4(H, r0 + 16 * b + 4 * G, ad.Nl, block_sum(red, b, NW, lane));
         __syncthreads();  // before the next sums overwrite `red`
       }
     }
@@ -240,7 +239,7 @@ __global__ __launch_bounds__(64 * NW) void adapt_few_sums(GroupArgs a, AdaptArgs
   for (int blk = wave; blk < FB * RB; blk += NW) {
     const int n = 16 * (blk % RB) + l16, m = m0 + 16 * (blk / RB) + 4 * G;
     if (n < a.N)
-      store4(ad.part + ((int64_t)z * a.N + n) * a.M, m, a.M, block_sum(red, blk, NW, lane), (a.M & 3) == 0);
+      store4(ad.part + ((int64_t)z * a.N + n) * a.M, m, a.M, block_sum(red, blk, NW, lane));
   }
 }
 
@@ -296,8 +295,7 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad, 
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += s * d[e];
   }
-  const bool whole = ((uintptr_t)a.D & (4 * sizeof(TO) - 1)) == 0 && (a.ldd & 3) == 0;
-  store4(reinterpret_cast<TO*>(a.D) + (int64_t)n * a.ldd, m, a.M, sum, whole);
+  store4(reinterpret_cast<TO*>(a.D) + (int64_t)n * a.ldd, m, a.M, sum);
 }
 
 template <typename T, typename TO, int FB, int RB, int NW>
@@ -366,12 +364,13 @@ hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream
 
 }  // namespace
 
-// Up to eight rows a group and aligned rows: decoding steps.  At 32 rows of 20
-// groups, k 2048, 1024 features: 16.1 us here, 17.2 by 64 x 32 tiles; from 16
-// rows a group on (512 rows of 28, k 1024, 4096 features) 60 and 50; odd k
-// (1039, five rows a group) 40 and 21.
+// Up to eight rows a group, aligned rows, and two runs of k for each of the
+// four waves: decoding steps.  bf16, at 32 rows of 20 groups, k 2048, 1024
+// features: 16.1 us here, 17.2 by 64 x 32 tiles; with k 512 (49 rows of 38
+// groups, 4096 features) 42 and 33; at 16 rows a group (512 rows of 28, k
+// 1024, 4096 features) 60 and 49; odd k (1039, five rows a group) 40 and 21.
 bool group_few_fits(const GroupArgs& a, int dtype) {
-  return a.N <= 8 * (int64_t)a.Ng && a.K * in_bytes(dtype) % 16 == 0 &&
+  return a.N <= 8 * (int64_t)a.Ng && a.K * in_bytes(dtype) >= 2048 && a.K * in_bytes(dtype) % 16 == 0 &&
          (((uintptr_t)a.X | (uintptr_t)a.Y) & 15) == 0;
 }
 

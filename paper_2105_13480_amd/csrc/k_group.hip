@@ -66,9 +66,7 @@ template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
       nt = (double)a.N / c[i].tn + 0.5 * (MODE == kAdapt || a.Ng > a.N ? 1 : a.Ng);
       k = a.K;
     }
-    double n = mt * nt / cus;
-    if (i == 0) n = (double)(int64_t)(n + 0.999);  // one at a time
-    if (n < 1) n = 1;
+    const double n = 1 + (double)(int64_t)(mt * nt / cus - 1e-3);  // of the CU with most
     const double stages = k * sizeof(T) / 128 + 1;
     const double t = c[i].once + stages * (n * c[i].share > c[i].alone ? n * c[i].share : c[i].alone) +
                      n * c[i].ends;
