@@ -183,14 +183,20 @@ __global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) 
 // Few adapted rows, first launch: partial sums of both products that read In.
 // The first workgroups, (tile of 16 rows, q, z), take every Q-th of the
 // adapters that the tile's rows name, 16 DF ranks at a time, over slice z of
-// k: H[z][n][r] = sum_k In[n, k] A[ids[n]][r, k].  The rest, (block of 16 FB
+// k: H[z][n][r] = sum_k In[n, k] A[ids[n]][r, k].  The rest, (block of 64
 // features, slice of k), take all rows: part[z][n][m] = sum_k In[n, k] Ker[m, k].
-// Neither waits for the other, and a slice is short, so that all of Ker is
-// asked for at once.
-template <typename T, int DF, int FB, int RB, int NW>
-__global__ __launch_bounds__(64 * NW) void adapt_few_sums(GroupArgs a, AdaptArgs ad, FewPlan f) {
-  __shared__ f32x4_t red[NW * (DF > FB * RB ? DF : FB * RB) * 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Neither waits for the other, and a slice is short, so that most of Ker is
+// asked for at once.  RING: the projection's operands go through a ring of
+// four stages in LDS (4-byte boundaries, whole units of k: 64 features read In
+// a quarter as often as 16), else straight to the registers.
+constexpr int kSumWaves = 4, kSumDepth = 4, kSumFeatures = 64;
+
+template <typename T, int DF, int TN, bool RING>
+__global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, AdaptArgs ad, FewPlan f) {
+  constexpr int NW = kSumWaves, NT = 64 * NW, RB = TN / 16;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  f32x4_t* const red = reinterpret_cast<f32x4_t*>(smem);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, G = lane >> 4;
   int bid = blockIdx.x;
   if (bid < f.downs) {
@@ -225,41 +231,95 @@ __global__ __launch_bounds__(64 * NW) void adapt_few_sums(GroupArgs a, AdaptArgs
     return;
   }
   bid -= f.downs;
-  const int z = bid / f.blocks, m0 = 16 * FB * (bid % f.blocks), k_lo = z * f.kslice;
-  const T* x[FB];
-  feature_rows<T, FB>(reinterpret_cast<const T*>(a.X) + k_lo, a.ldx, m0, a.M, l16, x);
-  const T* y[RB];
+  const int z = bid / f.blocks, m0 = kSumFeatures * (bid % f.blocks), k_lo = z * f.kslice;
+  const int K = min(a.K - k_lo, f.kslice);
+  const T* const X = reinterpret_cast<const T*>(a.X) + k_lo;
+  const T* const Y = reinterpret_cast<const T*>(a.Y) + k_lo;
+  float* const part = ad.part + (int64_t)z * a.N * a.M;
+  if constexpr (RING) {
+    constexpr int TK = 128 / (int)sizeof(T), XU = 8 * kSumFeatures, STAGE = XU + 8 * TN;
+    u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
+    Stager<T, true, kSumFeatures, NT, false> sx;
+    Stager<T, true, TN, NT, false> sy;
+    constexpr int COPIES = sx.NU + sy.NU;
+    Reader<T, true, kSumFeatures, 1> rx;
+    Reader<T, true, TN, RB> ry;
+    rx.init(16 * wave, lane);
+    ry.init(0, lane);
+    sx.init(tid, X, a.ldx, m0, min(a.M - m0, kSumFeatures), nullptr, 0);
+    sy.init(tid, Y, a.ldy, 0, a.N, nullptr, 0);
+    f32x4_t acc[RB];
 #pragma unroll
-  for (int b = 0; b < RB; ++b)
-    y[b] = reinterpret_cast<const T*>(a.Y) + (int64_t)min(16 * b + l16, a.N - 1) * a.ldy + k_lo;
-  f32x4_t acc[FB][RB];
-  clear(acc);
-  few_rows_dot<T, FB, RB>(x, y, min(a.K - k_lo, f.kslice), wave, NW, lane, acc);
-  leave_sums(red, acc, wave, NW, lane);
-  for (int blk = wave; blk < FB * RB; blk += NW) {
-    const int n = 16 * (blk % RB) + l16, m = m0 + 16 * (blk / RB) + 4 * G;
-    if (n < a.N)
-      store4(ad.part + ((int64_t)z * a.N + n) * a.M, m, a.M, block_sum(red, blk, NW, lane));
+    for (int b = 0; b < RB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int n_st = (K + TK - 1) / TK;
+    auto copy = [&](int s) __attribute__((always_inline)) {
+      u32x4_t* const dst = ring + s % kSumDepth * STAGE;
+      sx.copy(tid, dst, s * TK, a.ldx, K, nullptr, 0);
+      sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
+    };
+#pragma unroll
+    for (int s = 0; s < kSumDepth - 1; ++s) copy(s);
+    for (int s = 0; s < n_st; ++s) {
+      // as in group_tiles
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 2)) : "memory");
+      copy(s + kSumDepth - 1);
+      u32x4_t xf[1][2], yf[RB][2];
+      rx.read(ring + s % kSumDepth * STAGE, xf);
+      ry.read(ring + s % kSumDepth * STAGE + XU, yf);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[b] = mma<T>(xf[0][ks], yf[b][ks], acc[b]);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int n = 16 * b + l16;
+      if (n < a.N) store4(part + (int64_t)n * a.M, m0 + 16 * wave + 4 * G, a.M, acc[b]);
+    }
+  } else {
+    const T* y[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) y[b] = Y + (int64_t)min(16 * b + l16, a.N - 1) * a.ldy;
+    // two blocks of features at a time
+    for (int m = m0; m < min(m0 + kSumFeatures, a.M); m += 32) {
+      const T* x[2];
+      feature_rows<T, 2>(X, a.ldx, m, a.M, l16, x);
+      f32x4_t acc[2][RB];
+      clear(acc);
+      few_rows_dot<T, 2, RB>(x, y, K, wave, NW, lane, acc);
+      leave_sums(red, acc, wave, NW, lane);
+      for (int blk = wave; blk < 2 * RB; blk += NW) {
+        const int n = 16 * (blk % RB) + l16;
+        if (n < a.N)
+          store4(part + (int64_t)n * a.M, m + 16 * (blk / RB) + 4 * G, a.M, block_sum(red, blk, NW, lane));
+      }
+      __syncthreads();
+    }
   }
 }
 
 // Second launch: Out = the slices' sums, in order, and each row's low-rank
 // part in fp32; a thread has four features of a row.
-template <typename T, typename TO>
-__global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad, FewPlan f) {
+template <typename T, typename TO, int KS, int KH>
+__global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) {
   const int per = (a.M + 3) / 4;
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i >= per * a.N) return;
   const int n = i / per, m = 4 * (i - n * per);
+  const int left = a.M - 1 - m;  // features after the first
   f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < f.ks; ++z) {
+#pragma unroll
+  for (int z = 0; z < KS; ++z) {
     const float* const src = ad.part + ((int64_t)z * a.N + n) * a.M + m;
-    if (a.M % 4 == 0) {
-      sum += *reinterpret_cast<const f32x4_t*>(src);
+    f32x4_t p;
+    if (left >= 3) {
+      __builtin_memcpy(&p, src, 16);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += src[min(e, a.M - 1 - m)];
+      for (int e = 0; e < 4; ++e) p[e] = src[min(e, left)];
     }
+    sum += p;
   }
   const int id = ad.ids[n];
   if (id >= 0 && id < ad.Na) {
@@ -270,26 +330,27 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad, 
     int r = 0;
 #pragma unroll 2
     for (; r + 8 <= ad.Nl; r += 8) {
-      float h[8] = {};
-      for (int z = 0; z < f.kh; ++z) {
-        float p[8];
-        __builtin_memcpy(p, H + z * hz + r, sizeof(p));
+      float p[KH][8];
+      T b[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] += p[e];
-      }
+      for (int z = 0; z < KH; ++z) __builtin_memcpy(p[z], H + z * hz + r, sizeof(p[z]));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        T b[8];
-        __builtin_memcpy(b, B + (int64_t)min(e, a.M - 1 - m) * ad.Nl + r, sizeof(b));
+      for (int e = 0; e < 4; ++e) __builtin_memcpy(b[e], B + (int64_t)min(e, left) * ad.Nl + r, sizeof(b[e]));
 #pragma unroll
-        for (int t = 0; t < 8; ++t) d[e] += h[t] * to_f32(b[t]);
+      for (int t = 0; t < 8; ++t) {
+        float h = p[0][t];
+#pragma unroll
+        for (int z = 1; z < KH; ++z) h += p[z][t];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] += h * to_f32(b[e][t]);
       }
     }
     for (; r < ad.Nl; ++r) {
       float h = 0.f;
-      for (int z = 0; z < f.kh; ++z) h += H[z * hz + r];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) d[e] += h * to_f32(B[(int64_t)min(e, a.M - 1 - m) * ad.Nl + r]);
+      for (int z = 0; z < KH; ++z) h += H[z * hz + r];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] += h * to_f32(B[(int64_t)min(e, left) * ad.Nl + r]);
     }
     const float s = ad.scales ? ad.scales[id] : 1.f;
 #pragma unroll
@@ -329,36 +390,52 @@ hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stre
   return hipGetLastError();
 }
 
-template <typename T, int DF, int FB, int RB>
+template <typename T, int DF, int TN>
 void launch_sums(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
-  adapt_few_sums<T, DF, FB, RB, 4>
-      <<<dim3((uint32_t)(f.downs + f.blocks * f.ks)), dim3(256), 0, stream>>>(a, ad, f);
-}
-template <typename T, int DF>
-void launch_sums_rows(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
-  switch ((a.N + 15) / 16) {
-    case 1: launch_sums<T, DF, 1, 1>(a, ad, f, stream); break;
-    case 2: launch_sums<T, DF, 2, 2>(a, ad, f, stream); break;
-    case 3: launch_sums<T, DF, 2, 3>(a, ad, f, stream); break;
-    default: launch_sums<T, DF, 2, 4>(a, ad, f, stream); break;
+  constexpr int CE = 16 / (int)sizeof(T);
+  const dim3 grid((uint32_t)(f.downs + f.blocks * f.ks)), block(64 * kSumWaves);
+  const int red = 16 * 64 * kSumWaves * (DF > TN / 8 ? DF : TN / 8);
+  const bool ring = (((uintptr_t)a.X | (uintptr_t)a.Y) & 3) == 0 && a.K % CE == 0;
+  if (ring) {
+    const int lds = kSumDepth * 8 * (kSumFeatures + TN) * 16;
+    adapt_few_sums<T, DF, TN, true><<<grid, block, lds > red ? lds : red, stream>>>(a, ad, f);
+  } else {
+    adapt_few_sums<T, DF, TN, false><<<grid, block, red, stream>>>(a, ad, f);
   }
+}
+
+template <typename T, typename TO, int KS>
+void launch_out(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
+  const int64_t threads = (int64_t)a.N * ((a.M + 3) / 4);
+  const dim3 grid((uint32_t)((threads + 255) / 256)), block(256);
+  if (f.kh == 1) adapt_few_out<T, TO, KS, 1><<<grid, block, 0, stream>>>(a, ad);
+  else adapt_few_out<T, TO, KS, 4><<<grid, block, 0, stream>>>(a, ad);
 }
 
 template <typename T, typename TO>
 hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   constexpr int RUN = 256 / (int)sizeof(T);
   FewPlan f = adapt_few_plan(a.N, a.K, a.M);
-  // slices of k of whole runs
+  // slices of k of whole runs; the last may be shorter or empty
   f.hslice = ((a.K + f.kh - 1) / f.kh + RUN - 1) / RUN * RUN;
   f.kslice = ((a.K + f.ks - 1) / f.ks + RUN - 1) / RUN * RUN;
   f.q = ad.Na < 16 ? ad.Na : 16;
   f.downs = (a.N + 15) / 16 * f.q * f.kh;
-  if (ad.Nl <= 16) launch_sums_rows<T, 1>(a, ad, f, stream);
-  else launch_sums_rows<T, 4>(a, ad, f, stream);
+  if (a.N <= 32) {
+    if (ad.Nl <= 16) launch_sums<T, 1, 32>(a, ad, f, stream);
+    else launch_sums<T, 4, 32>(a, ad, f, stream);
+  } else {
+    if (ad.Nl <= 16) launch_sums<T, 1, 64>(a, ad, f, stream);
+    else launch_sums<T, 4, 64>(a, ad, f, stream);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t threads = (int64_t)a.N * ((a.M + 3) / 4);
-  adapt_few_out<T, TO><<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, stream>>>(a, ad, f);
+  switch (f.ks) {
+    case 1: launch_out<T, TO, 1>(a, ad, f, stream); break;
+    case 2: launch_out<T, TO, 2>(a, ad, f, stream); break;
+    case 4: launch_out<T, TO, 4>(a, ad, f, stream); break;
+    default: launch_out<T, TO, 8>(a, ad, f, stream); break;
+  }
   return hipGetLastError();
 }
 
@@ -393,16 +470,13 @@ hipError_t launch_adapt_down(const GroupArgs& a, const AdaptArgs& ad, int dtype,
 bool adapt_few(int64_t Nt) { return Nt <= 64; }
 
 FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk) {
+  (void)Nt;
   FewPlan f = {};
-  // two blocks of features a workgroup but for the fewest rows: In is read
-  // half as often
-  const int fb = Nt <= 16 ? 1 : 2;
-  f.blocks = (int32_t)((Nk + 16 * fb - 1) / (16 * fb));
-  // two workgroups a CU, as long as each of their four waves has a run of k
-  const int64_t most = Nc / 512 < 1 ? 1 : Nc / 512 > 8 ? 8 : Nc / 512;
-  const int64_t want = (512 + f.blocks - 1) / f.blocks;
-  f.ks = (int32_t)(want < most ? want : most);
-  f.kh = (int32_t)most;
+  f.blocks = (int32_t)((Nk + kSumFeatures - 1) / kSumFeatures);
+  // slices of k: a workgroup for each CU, of 256 values of k at least
+  f.ks = 1;
+  while (f.ks < 8 && f.ks * f.blocks < 256 && Nc >= 512 * f.ks) f.ks *= 2;
+  f.kh = Nc >= 1024 ? 4 : 1;
   return f;
 }
 
