@@ -64,54 +64,74 @@ __global__ __launch_bounds__(256) void combine_rows(const T* In, const int32_t* 
   store_row<TO, V>(Out + t * Nk + k, n, acc);
 }
 
-// One wave per token: dIn[p] = gate dOut[t] and dGates[t, j] = dOut[t] . In[p]
-// for each of its Kt rows p.  The workgroups past the tokens' write zeros to
-// the rows that no token has (rows[p] < 0).
-template <typename T, typename TO, int V>
+// W waves per place p: with t = rows[p] and j the choice whose slot p is,
+// dIn[p] = gate dOut[t] and dGates[t, j] = dOut[t] . In[p]; zeros where no row
+// has the place.  In the order of the places, In and dIn are read and written
+// straight through, and dOut's rows (a Kt-th of the bytes) come from the caches
+// the second time.  The last workgroups clear dGates of the choices without a
+// place.
+template <typename T, typename TO, int V, int W>
 __global__ __launch_bounds__(256) void combine_rows_bwd(const T* dOut, const T* In,
                                                         const int32_t* slots, const int32_t* rows,
                                                         const float* gates, TO* dIn, float* dGates,
                                                         int64_t Nt, int Kt, int64_t Np, int64_t Nk,
-                                                        int64_t token_blocks) {
-  const int lane = threadIdx.x & 63;
-  const int64_t b = blockIdx.x;
-  if (b >= token_blocks) {
-    const int64_t p0 = ((b - token_blocks) * 4 + (threadIdx.x >> 6)) * 64;
-    uint64_t gone = __ballot(p0 + lane < Np && rows[min(p0 + lane, Np - 1)] < 0);
-    while (gone) {
-      const int64_t p = p0 + __ffsll((unsigned long long)gone) - 1;
-      gone &= gone - 1;
-      const float z[V] = {};
-      for (int64_t k = lane * V; k < Nk; k += 64 * V)
-        store_row<TO, V>(dIn + p * Nk + k, (int)min<int64_t>(Nk - k, V), z);
-    }
+                                                        int64_t place_blocks) {
+  __shared__ float sums[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x >= place_blocks) {
+    const int64_t i = (blockIdx.x - place_blocks) * 256 + threadIdx.x;
+    if (i < Nt * Kt && (slots[i] < 0 || slots[i] >= Np)) dGates[i] = 0.f;
     return;
   }
-  const int64_t t = b * 4 + (threadIdx.x >> 6);
-  if (t >= Nt) return;
-  for (int j = 0; j < Kt; ++j) {
-    const int p = slots[t * Kt + j];
-    float dot = 0.f;
-    if (p >= 0 && p < Np) {
-      const float g = gates ? gates[t * Kt + j] : 1.f;
-#pragma unroll 4
-      for (int64_t k = lane * V; k < Nk; k += 64 * V) {
-        const int n = (int)min<int64_t>(Nk - k, V);
+  const int64_t p = (int64_t)blockIdx.x * (4 / W) + wave / W;
+  const bool there = p < Np;
+  const int row = there ? __builtin_amdgcn_readfirstlane(rows[p]) : -1;
+  // the choice of this place: the lanes look at Kt slots of the row
+  int64_t pair = -1;
+  if (row >= 0 && row < Nt)
+    for (int j0 = 0; j0 < Kt && pair < 0; j0 += 64) {
+      const uint64_t hit = __ballot(j0 + lane < Kt && slots[(int64_t)row * Kt + min(j0 + lane, Kt - 1)] == p);
+      if (hit) pair = (int64_t)row * Kt + j0 + __ffsll((unsigned long long)hit) - 1;
+    }
+  float dot = 0.f;
+  if (there) {
+    TO* const out = dIn + p * Nk;
+    if (pair < 0) {
+      const float z[V] = {};
+      for (int64_t k = ((wave % W) * 64 + lane) * V; k < Nk; k += W * 64 * V)
+        store_row<TO, V>(out + k, (int)min<int64_t>(Nk - k, V), z);
+    } else {
+      const T* const drow = dOut + row * Nk;
+      const T* const irow = In + p * Nk;
+      const float g = gates ? gates[pair] : 1.f;
+      auto columns = [&](int64_t k, int n) __attribute__((always_inline)) {
         float d[V], x[V];
-        load_row<T, V>(dOut + t * Nk + k, n, d);
-        load_row<T, V>(In + p * Nk + k, n, x);
+        load_row<T, V>(irow + k, n, x);
+        load_row<T, V>(drow + k, n, d);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           dot += d[e] * x[e];
           d[e] *= g;
         }
-        store_row<TO, V>(dIn + p * Nk + k, n, d);
+        store_row<TO, V>(out + k, n, d);
+      };
+      for (int64_t k = ((wave % W) * 64 + lane) * V; k < Nk; k += W * 64 * V) {
+        if (k + V <= Nk) columns(k, V);
+        else columns(k, (int)(Nk - k));
       }
     }
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
-    if (lane == 0 && dGates) dGates[t * Kt + j] = dot;
   }
+  if (!dGates) return;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) dot += __shfl_xor(dot, d);
+  if (W > 1) {
+    if (lane == 0) sums[wave] = dot;
+    __syncthreads();
+    dot = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) dot += sums[wave / W * W + w];
+  }
+  if (pair >= 0 && wave % W == 0 && lane == 0) dGates[pair] = dot;
 }
 
 template <typename T, typename TO>
@@ -130,11 +150,15 @@ hipError_t launch_bwd(const void* dOut, const void* In, const int32_t* slots, co
                       const float* gates, void* dIn, float* dGates, int64_t Nt, int Kt, int64_t Np,
                       int64_t Nk, hipStream_t stream) {
   constexpr int V = 16 / (int)sizeof(T);
-  const int64_t token_blocks = (Nt + 3) / 4, zero_blocks = (Np + 255) / 256;
-  combine_rows_bwd<T, TO, V>
-      <<<dim3((uint32_t)(token_blocks + zero_blocks)), dim3(256), 0, stream>>>(
-          reinterpret_cast<const T*>(dOut), reinterpret_cast<const T*>(In), slots, rows, gates,
-          reinterpret_cast<TO*>(dIn), dGates, Nt, Kt, Np, Nk, token_blocks);
+  // a wave for each 64 V columns, up to four
+  const int w = Nk <= 64 * V ? 1 : Nk <= 128 * V ? 2 : 4;
+  const int64_t place_blocks = (Np * w + 3) / 4, clear_blocks = dGates ? (Nt * Kt + 255) / 256 : 0;
+  if (!place_blocks && !clear_blocks) return hipSuccess;
+  auto* const k = w == 1 ? combine_rows_bwd<T, TO, V, 1>
+                  : w == 2 ? combine_rows_bwd<T, TO, V, 2> : combine_rows_bwd<T, TO, V, 4>;
+  k<<<dim3((uint32_t)(place_blocks + clear_blocks)), dim3(256), 0, stream>>>(
+      reinterpret_cast<const T*>(dOut), reinterpret_cast<const T*>(In), slots, rows, gates,
+      reinterpret_cast<TO*>(dIn), dGates, Nt, Kt, Np, Nk, place_blocks);
   return hipGetLastError();
 }
 

@@ -3,9 +3,11 @@
 //
 // Choice: a row's logits are held by LT lanes (16, or 64 for more than 256
 // experts), E of them a lane, as unsigned keys whose order is the logits';
-// not-allowed ones (-inf, NaN) have key 0.  Each of the Kt largest is one
-// maximum over the lanes of (key, ~expert) as a 64-bit value, so ties go to
-// the lowest expert and every lane knows the result.  Four rows a wave.
+// not-allowed ones (-inf, NaN) have key 0.  Each of the Kt largest is a
+// maximum over the lanes by data-parallel moves, so every lane knows it: in
+// bf16 of (16-bit key, ~expert) as one value, in fp32 of the key and then of
+// the lowest expert that has it; ties go to the lowest expert.  Four rows a
+// wave.
 //
 // Order: a counting sort, stable.  A workgroup owns a chunk of rows; the
 // chunk's counts per expert go to the workspace, then every workgroup adds up
@@ -64,55 +66,75 @@ template <int LT> __device__ __forceinline__ float row_sum(float s) {
 // e^(x - m), 1 at x = m (also where both are infinite).
 __device__ __forceinline__ float weight_of(float x, float m) { return x == m ? 1.f : expf(x - m); }
 
-// Choice and weights of one row, the same in all of its lanes but for lane j
-// holding choice j (-1: none) and its weight.
+// The largest (MAX) or least v of the row's lanes, in all of them.
+template <int LT, bool MAX> __device__ __forceinline__ uint32_t row_best(uint32_t v) {
+  butterfly<LT>([&](auto from) {
+    const uint32_t o = from(v);
+    v = MAX ? (o > v ? o : v) : (o < v ? o : v);
+  });
+  return v;
+}
+
+// Choice and weights of one row: lane j holds choice j (-1: none) and its weight.
 template <typename T, int LT, int E>
 __device__ __forceinline__ void choose_row(const T* logits, int Ng, int Kt, int over_all, int li,
                                            bool row_ok, int* choice, float* gate) {
-  uint32_t key[E];
+  constexpr bool PACK = sizeof(T) == 2;
+  uint32_t key[E];  // PACK: key in the upper half, ~expert in the lower
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const int e = i * LT + li;
     key[i] = row_ok && e < Ng ? logit_key(to_f32(logits[e])) : 0u;
   }
+  float top = 0.f, total = 0.f;
+  if (over_all) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) best = key[i] > best ? key[i] : best;
+    best = row_best<LT, true>(best);
+    top = best ? key_logit(best) : 0.f;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (key[i] != 0u) s += weight_of(key_logit(key[i]), top);
+    total = row_sum<LT>(s);
+  }
+  if constexpr (PACK)
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (key[i] != 0u) key[i] = (key[i] & 0xffff0000u) | (0xffffu ^ (uint32_t)(i * LT + li));
   uint32_t my_key = 0;
   int mine = -1;
-  float top = 0.f, total = 0.f;
   for (int j = 0; j < Kt; ++j) {
-    uint32_t hi = key[0], lo = (uint32_t)~li;
+    uint32_t best = key[0];
 #pragma unroll
-    for (int i = 1; i < E; ++i)
-      if (key[i] > hi) {
-        hi = key[i];
-        lo = ~(uint32_t)(i * LT + li);
-      }
-    butterfly<LT>([&](auto from) {
-      const uint32_t oh = from(hi), ol = from(lo);
-      const bool take = oh > hi || (oh == hi && ol > lo);
-      hi = take ? oh : hi;
-      lo = take ? ol : lo;
-    });
-    const int e = (int)~lo;
-    if (hi != 0u) {
-      const float x = key_logit(hi);
-      if (j == 0) {
-        top = x;
-        if (over_all) {
-          float s = 0.f;
+    for (int i = 1; i < E; ++i) best = key[i] > best ? key[i] : best;
+    best = row_best<LT, true>(best);
+    int e;
+    if constexpr (PACK) {
+      e = (int)(0xffffu ^ (best & 0xffffu));
 #pragma unroll
-          for (int i = 0; i < E; ++i)
-            if (key[i] != 0u) s += weight_of(key_logit(key[i]), top);
-          total = row_sum<LT>(s);
-        }
+      for (int i = 0; i < E; ++i) key[i] = key[i] == best ? 0u : key[i];
+      // the logit's key again: a negative bf16's has ones below
+      best = best & 0x80000000u || !best ? best & 0xffff0000u : best | 0xffffu;
+    } else {
+      uint32_t lowest = ~0u;
+#pragma unroll
+      for (int i = E - 1; i >= 0; --i) lowest = key[i] == best ? (uint32_t)(i * LT + li) : lowest;
+      e = (int)row_best<LT, false>(lowest);
+#pragma unroll
+      for (int i = 0; i < E; ++i) key[i] = e == i * LT + li ? 0u : key[i];
+    }
+    if (best != 0u) {
+      const float x = key_logit(best);
+      if (!over_all) {
+        if (j == 0) top = x;
+        total += weight_of(x, top);
       }
-      if (!over_all) total += weight_of(x, top);
       if (li == j) {
-        my_key = hi;
+        my_key = best;
         mine = e;
       }
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (e == i * LT + li) key[i] = 0u;
     }
   }
   *choice = mine;
@@ -232,7 +254,9 @@ __global__ __launch_bounds__(kOrderThreads) void order_count(OrderArgs o) {
   for (int e = tid; e < o.Ng; e += kOrderThreads) o.counts[(int64_t)blockIdx.x * o.Ng + e] = hist[e];
 }
 
-// Places of one chunk of rows, from the counts of all chunks.
+// Places of one chunk of rows, from the counts of all chunks, or (KEYS: few
+// rows) from all keys.
+template <bool KEYS>
 __global__ __launch_bounds__(kOrderThreads) void order_place(OrderArgs o) {
   __shared__ OrderShared s;
   __shared__ int32_t whole[kMaxExperts], ahead[kMaxExperts];
@@ -240,9 +264,17 @@ __global__ __launch_bounds__(kOrderThreads) void order_place(OrderArgs o) {
   const int t0 = b * o.chunk, t1 = min(o.Nt, t0 + o.chunk);
   for (int e = tid; e < Ng; e += kOrderThreads) whole[e] = ahead[e] = 0;
   __syncthreads();
+  if constexpr (KEYS) {
+    for (int i = tid; i < o.Nt * o.Kt; i += kOrderThreads) {
+      const int e = o.key[i];
+      if (e < 0 || e >= Ng) continue;
+      atomicAdd(&whole[e], 1);
+      if (i < t0 * o.Kt) atomicAdd(&ahead[e], 1);
+    }
+  }
   // thread (x, y): key x of every ny-th chunk
   const int ny = max(1, kOrderThreads / Ng), x = tid % Ng, y = tid / Ng;
-  if (y < ny) {
+  if (!KEYS && y < ny) {
     int w = 0, h = 0;
 #pragma unroll 8
     for (int c = y; c < o.nblocks; c += ny) {
@@ -383,10 +415,15 @@ void order_blocks(int64_t Nt, int32_t* chunk, int32_t* nblocks) {
 }
 
 hipError_t launch_order(const OrderArgs& o, hipStream_t stream) {
+  // every workgroup counts all keys: two a thread, against another launch
+  if (o.Nt * o.Kt <= 2 * kOrderThreads) {
+    order_place<true><<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
+    return hipGetLastError();
+  }
   order_count<<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  order_place<<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
+  order_place<false><<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
   return hipGetLastError();
 }
 
@@ -396,7 +433,7 @@ hipError_t launch_route(const RouteArgs& a, const OrderArgs& o, bool bf16, hipSt
   const hipError_t e =
       bf16 ? launch_choose<bf16_t, false>(a, o, stream) : launch_choose<float, false>(a, o, stream);
   if (e != hipSuccess) return e;
-  order_place<<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
+  order_place<false><<<dim3(o.nblocks), dim3(kOrderThreads), 0, stream>>>(o);
   return hipGetLastError();
 }
 

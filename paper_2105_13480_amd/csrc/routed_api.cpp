@@ -4,6 +4,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include "routed.h"
 
 using namespace cnnlib;
@@ -237,7 +239,7 @@ static int check_combine(int64_t Nt, int64_t Kt, int64_t Np, int64_t Nk, int dty
                     {"Nk", Nk, 1, kFeatures}};
   int st;
   if ((st = check_sizes(s)) || (st = check_type(dtype))) return st;
-  return check_grid(Nt * ((Nk + 3) / 4) / 256 + Np / 256 + 2);
+  return check_grid(std::max(Nt * ((Nk + 3) / 4) / 256 + 1, Np + Nt * Kt / 256 + 2));
 }
 
 int cnn_combine(const void* In, const int32_t* Slots, const float* Gates, void* Out, int64_t Nt,
