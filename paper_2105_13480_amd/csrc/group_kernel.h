@@ -538,37 +538,72 @@ __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T,
   return true;
 }
 
+// Eight consecutive bf16 results from `m` of one row, as many as lie below M.
+__device__ __forceinline__ void store8(bf16_t* row, int m, int M, u32x4_t v) {
+  if (m + 8 <= M) {
+    __builtin_memcpy(row + m, &v, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (m + e < M) row[m + e] = (bf16_t)(v[e >> 1] >> (16 * (e & 1)));
+  }
+}
+
 // Results acc[i][j] of 16 values of m from xrow(i) by 16 rows from yrow(j).
-// MASK: rows whose source row is not there are stored as zeros.
+// MASK: rows whose source row is not there are stored as zeros.  A lane has
+// four results of a row in each block: 16 bytes of fp32, 64 bytes a row and
+// store.  In bf16 two neighbouring blocks trade the odd 16 lanes of the one for
+// the even of the other, which makes it 16 and 64 bytes again (8 bytes a lane
+// store at half the rate: 128 MB of results 40 us and, this way, 24).
 template <typename T, typename TO, int MODE, bool MASK, int NI, int NJ, typename XR, typename YR>
 __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>& w, int lane,
                                            f32x4_t (&acc)[NI][NJ], XR xrow, YR yrow) {
-  const int l16 = lane & 15, m0 = w.m0 + 4 * (lane >> 4);
-  const bool fours = (a.M & 3) == 0;  // no row ends inside four results
+  const int l16 = lane & 15, G = lane >> 4;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int n = yrow(j) + l16;
-    if (n >= w.n_valid) continue;
+    const bool there = n < w.n_valid;
     int64_t at = n;
     bool live = true;
     if constexpr (MASK || MODE == kAdapt) {
       if (w.rows) {
-        const int r = w.rows[w.n0 + n];
+        const int r = w.rows[w.n0 + min(n, w.n_valid - 1)];
         if constexpr (MODE == kAdapt) at = r;
         live = r >= 0 && r < a.Nsrc;
       }
     }
     TO* const row = w.D + at * a.ldd;
+    if constexpr (sizeof(TO) == 2 && NI % 2 == 0) {
+      const bool eights = (a.M & 7) == 0;  // no row ends inside eight results
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int m = m0 + xrow(i);
-      f32x4_t v = acc[i][j];
-      if constexpr (MASK)
-        if (!live) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (fours) {
-        if (m < a.M) store4(row, m, m + 4, v);
-      } else {
-        store4(row, m, a.M, v);
+      for (int i = 0; i < NI; i += 2) {
+        u32x4_t v;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t p = pk_bf16(acc[i][j][2 * e], acc[i][j][2 * e + 1]);
+          const uint32_t q = pk_bf16(acc[i + 1][j][2 * e], acc[i + 1][j][2 * e + 1]);
+          const auto r = __builtin_amdgcn_permlane16_swap(p, q, false, false);
+          v[e] = live ? r[0] : 0u;
+          v[2 + e] = live ? r[1] : 0u;
+        }
+        const int m = w.m0 + xrow(i) + 16 * (G & 1) + 8 * (G >> 1);
+        if (there) {
+          if (!eights) store8(row, m, a.M, v);
+          else if (m < a.M) store8(row, m, m + 8, v);
+        }
+      }
+    } else {
+      const bool fours = (a.M & 3) == 0;  // no row ends inside four results
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int m = w.m0 + xrow(i) + 4 * G;
+        f32x4_t v = acc[i][j];
+        if constexpr (MASK)
+          if (!live) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (there) {
+          if (!fours) store4(row, m, a.M, v);
+          else if (m < a.M) store4(row, m, m + 4, v);
+        }
       }
     }
   }

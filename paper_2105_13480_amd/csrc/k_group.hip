@@ -48,8 +48,8 @@ constexpr TileCost kF32[] = {{0, 0, 0, 0, 0, 0},
                              {64, 32, 0.30, 0.24, 0.6, 4.6}};
 
 // The cheapest of the tile sizes from `first` on (0: with the pipelined
-// kernel).  Group sizes are not known here: half a tile of each group is taken
-// to be empty.
+// kernel).  Group sizes are not known here: of several groups, half a tile each
+// is taken to be empty.
 template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
   const TileCost* const c = sizeof(T) == 2 ? kBf16 : kF32;
   const int last = MODE == kBwdKer ? 2 : 3;
@@ -63,7 +63,8 @@ template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
       nt = (double)a.Ng * ((a.N + c[i].tn - 1) / c[i].tn);
       k = (double)a.K / a.Ng;
     } else {
-      nt = (double)a.N / c[i].tn + 0.5 * (MODE == kAdapt || a.Ng > a.N ? 1 : a.Ng);
+      nt = a.Ng == 1 ? (double)((a.N + c[i].tn - 1) / c[i].tn)
+                     : (double)a.N / c[i].tn + 0.5 * (a.Ng < a.N ? a.Ng : a.N);
       k = a.K;
     }
     const double n = 1 + (double)(int64_t)(mt * nt / cus - 1e-3);  // of the CU with most
