@@ -9,6 +9,7 @@
 //   forward       X = Ker[g] (KC), Y = gathered In rows (KC)
 //   gradient, In  X = Ker[g] (MC), Y = dOut rows (KC)
 //   gradient, Ker X = gathered In rows (MC), Y = dOut rows (MC), k = the rows
+//   down          X = A[a] (KC), Y = In rows in the order of their adapters (KC)
 //   adapted       X = Ker, Y = In rows in the order of their adapters, one
 //                 group, then the low-rank part
 // Group sizes are read on the device, so the caller never waits for them: a
@@ -28,7 +29,7 @@
 namespace cnnlib {
 namespace group {
 
-enum Mode { kFwd = 0, kBwdIn = 1, kBwdKer = 2, kAdapt = 3 };
+enum Mode { kFwd = 0, kBwdIn = 1, kBwdKer = 2, kAdapt = 3, kDown = 4 };
 
 #define LDS_AS(T, p) ((__attribute__((address_space(3))) T*)(p))
 #define GLB_AS(T, p) ((__attribute__((address_space(1))) T*)(p))
@@ -420,47 +421,54 @@ __device__ __forceinline__ int row16_min(int v) {
 }
 
 // The tile of workgroup `bid` of a launch over the groups' row tiles by MT
-// tiles of m; false: none.  Row tiles are walked in bands: `band` row tiles by
-// every m tile, so that the tiles an XCD runs at a time share their rows of X
-// and Y in its L2.  Offsets that are not an order (documented as the caller's
-// duty) are found out by the wave that adds them up: no tile is then run.
-template <int TN>
+// tiles of m; false: none.  SPLIT: whole row tiles come first, then those that
+// a group's rows do not fill, so that the launch ends on the cheaper ones
+// (large tiles; small ones keep a group together, whose Ker they share).  Row
+// tiles are walked in bands: `band` row tiles by every m tile, so that the
+// tiles an XCD runs at a time share their rows of X and Y in its L2.  Offsets
+// that are not an order (documented as the caller's duty) are found out by the
+// wave that adds them up: no tile is then run.
+template <int TN, bool SPLIT = false>
 __device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, int MT, int bid,
                                           int band, RowTile* t) {
   const int lane = threadIdx.x & 63;
   int nt, j0, lo_g = 0, hi_g = Np;  // row tiles of the group, tile within it, its rows
+  int first = 0;                    // the first of those row tiles
   t->g = 0;
   if (!off) {
     nt = (Np + TN - 1) / TN;
     if (bid >= nt * MT) return false;
     j0 = xcd_remap(bid, nt * MT);
   } else {
-    // up to 63 groups: one pass, else one for the total and one for the tile
-    int lo = 0, hi = 0, incl = 0, total = 0;
-    for (int base = 0; base <= Ng; base += 64) {
+    // up to 63 groups: one pass, else one for the totals and one for the tile
+    int lo = 0, hi = 0, whole = 0, parts = 0, wholes = 0, partials = 0;
+    auto scan = [&](int base) __attribute__((always_inline)) {
       const int g = base + lane;
       lo = hi = 0;
       if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
-      if (__ballot(lo < 0 || hi < lo || hi > Np || (g == 0 && lo != 0))) return false;
-      incl = wave_scan((hi - lo + TN - 1) / TN);
-      total += __builtin_amdgcn_readlane(incl, 63);
+      whole = wave_scan((hi - lo + (SPLIT ? 0 : TN - 1)) / TN);
+      if (SPLIT) parts = wave_scan((hi - lo) % TN != 0);
+    };
+    for (int base = 0; base <= Ng; base += 64) {
+      scan(base);
+      if (__ballot(lo < 0 || hi < lo || hi > Np || (base + lane == 0 && lo != 0))) return false;
+      wholes += __builtin_amdgcn_readlane(whole, 63);
+      partials += __builtin_amdgcn_readlane(parts, 63);
     }
-    if (bid >= total * MT) return false;
-    const int L = xcd_remap(bid, total * MT);
+    if (bid >= (wholes + partials) * MT) return false;
+    const bool part = SPLIT && bid >= wholes * MT;
+    const int L = part ? xcd_remap(bid - wholes * MT, partials * MT) : xcd_remap(bid, wholes * MT);
     int before = 0;
     for (int base = 0;; base += 64) {
-      if (Ng >= 64) {
-        const int g = base + lane;
-        lo = hi = 0;
-        if (g <= Ng) group_rows(off, Ng, Np, g, &lo, &hi);
-        incl = wave_scan((hi - lo + TN - 1) / TN);
-      }
+      if (Ng >= 64) scan(base);
+      const int incl = part ? parts : whole;
       const uint64_t here = __ballot(L < (before + incl) * MT);
       if (here) {
         const int who = __ffsll((unsigned long long)here) - 1;
         lo_g = __builtin_amdgcn_readlane(lo, who);
         hi_g = __builtin_amdgcn_readlane(hi, who);
-        nt = (hi_g - lo_g + TN - 1) / TN;
+        nt = part ? 1 : (hi_g - lo_g + (SPLIT ? 0 : TN - 1)) / TN;
+        first = part ? (hi_g - lo_g) / TN : 0;
         j0 = L - (before + __builtin_amdgcn_readlane(incl, who) - nt) * MT;
         t->g = base + who;
         break;
@@ -470,9 +478,28 @@ __device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, in
   }
   const int b = j0 / (band * MT), rb = min(band, nt - b * band), j = j0 - b * band * MT;
   t->mt = j / rb;
-  t->n0 = lo_g + (b * band + j % rb) * TN;
+  t->n0 = lo_g + (first + b * band + j % rb) * TN;
   t->n1 = hi_g;
   return true;
+}
+
+// The group of the gradient of Ker's workgroup `bid`, tiles_per of them a
+// group: the groups with most rows come first, for a tile's time is its
+// group's rows.  Of more than 64 groups as they come.
+__device__ __forceinline__ int group_by_rows(const int32_t* off, int Ng, int Np, int bid,
+                                             int tiles_per) {
+  const int lane = threadIdx.x & 63, want = bid / tiles_per;
+  if (Ng > 64) return want;
+  int lo = 0, hi = -1;
+  if (lane < Ng) group_rows(off, Ng, Np, lane, &lo, &hi);
+  const int rows = hi - lo;
+  int rank = 0;
+  for (int g = 0; g < Ng; ++g) {
+    const int r = __builtin_amdgcn_readlane(rows, g);
+    rank += r > rows || (r == rows && g < lane);
+  }
+  const uint64_t me = __ballot(lane < Ng && rank == want);
+  return __ffsll((unsigned long long)me) - 1;
 }
 
 // Part `part` of h as the sum of bf16 values: the leading 8 bits of what the
@@ -494,7 +521,7 @@ template <typename T, typename TO> struct Tile {
   const T* Y;
   TO* D;
   const int32_t* rows;  // NULL, or the source rows of grouped rows n0 .. or of k = 0 ..
-  int K, m0, m_valid, n0, n_valid;
+  int K, m0, m_valid, n0, n_valid, g;
 };
 
 template <typename T, typename TO, int MODE, int TM, int TN>
@@ -507,9 +534,8 @@ __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T,
   int mt;
   if constexpr (MODE == kBwdKer) {
     const int NTL = (a.N + TN - 1) / TN;
-    const int L = xcd_remap(blockIdx.x, gridDim.x);
-    const int g = L / (MT * NTL);
-    const int j0 = L - g * MT * NTL;
+    const int g = group_by_rows(a.off, a.Ng, a.K, blockIdx.x, MT * NTL);
+    const int j0 = xcd_remap(blockIdx.x % (MT * NTL), MT * NTL);
     const int b = j0 / (band * MT), rb = min(band, NTL - b * band), j = j0 - b * band * MT;
     mt = j / rb;
     w->n0 = (b * band + j % rb) * TN;
@@ -519,18 +545,20 @@ __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T,
     lo = min(max(__builtin_amdgcn_readfirstlane(lo), 0), a.K);
     w->K = min(max(__builtin_amdgcn_readfirstlane(hi), lo), a.K) - lo;
     w->n_valid = min(a.N - w->n0, TN);
+    w->g = g;
     if (a.rows) w->rows += lo; else w->X += lo * a.ldx;
     w->Y += lo * a.ldy;
     w->D += g * a.dgroup + (int64_t)w->n0 * a.ldd;
   } else {
     RowTile t;
-    if (!find_tile<TN>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return false;
+    if (!find_tile<TN, TN == 256>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return false;
     w->K = t.g < a.Ng ? a.K : 0;  // the rows past the last group: no products
     w->n0 = t.n0;
+    w->g = t.g;
     w->n_valid = min(t.n1 - t.n0, TN);
     w->X += (t.g < a.Ng ? t.g : 0) * a.xgroup;
     // adapted rows go back to where they came from
-    if constexpr (MODE != kAdapt) w->D += (int64_t)t.n0 * a.ldd;
+    if constexpr (MODE < kAdapt) w->D += (int64_t)t.n0 * a.ldd;
     mt = t.mt;
   }
   w->m0 = mt * TM;
@@ -603,6 +631,41 @@ __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>
         if (there) {
           if (!fours) store4(row, m, a.M, v);
           else if (m < a.M) store4(row, m, m + 4, v);
+        }
+      }
+    }
+  }
+}
+
+// Rows of the low-rank operand from the results of In A^T: scaled, and in bf16
+// as the sum of PARTS bf16 values, each part nlp ranks (zeros past M).
+template <typename T, typename TO, int NI, int NJ, typename XR, typename YR>
+__device__ __forceinline__ void store_parts(const GroupArgs& a, const AdaptArgs& ad,
+                                            const Tile<T, TO>& w, int lane, f32x4_t (&acc)[NI][NJ],
+                                            XR xrow, YR yrow) {
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
+  const float scale = ad.scales ? ad.scales[w.g] : 1.f;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int n = yrow(j) + (lane & 15);
+    if (n >= w.n_valid) continue;
+    T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(w.n0 + n) * ad.hl;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int m = w.m0 + xrow(i) + 4 * (lane >> 4);
+      if (m >= ad.nlp) continue;  // a multiple of four
+      float h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = m + e < a.M ? acc[i][j][e] * scale : 0.f;
+      if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(row + m, h, 16);
+      } else {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          bf16_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(__float_as_uint(bf16_part(h[e], p)) >> 16);
+          __builtin_memcpy(row + p * ad.nlp + m, v, 8);
         }
       }
     }
@@ -707,8 +770,8 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
   constexpr int NT = 64 * WM * WN;
-  constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
-  constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE == kAdapt;  // gathered operands
+  constexpr bool XKC = MODE == kFwd || MODE >= kAdapt, YKC = MODE != kBwdKer;
+  constexpr bool XG = MODE == kBwdKer, YG = MODE == kFwd || MODE >= kAdapt;  // gathered operands
   constexpr int CE = 16 / (int)sizeof(T), TK = 8 * CE;
   constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
   constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
@@ -803,6 +866,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
         if (s + 1 < n_st) commit(s + 1);
       }
     }
+  }
+  if constexpr (MODE == kDown) {
+    if (w.g < a.Ng) store_parts<T, TO>(a, ad, w, lane, acc, xrow, yrow);
+    return;
   }
   if constexpr (MODE == kAdapt) low_rank<T, TO, WHOLE>(a, ad, w, lane, acc, xrow, yrow);
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);

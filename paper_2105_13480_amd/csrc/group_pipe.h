@@ -41,7 +41,7 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
   uint32_t off[KC ? 4 : 2];  // bytes from base: rows half * 128 + j * 64 + tid / 8 | columns of a half
   int c8;               // KC: first k of this thread's unit within a stage
   int64_t ld;
-  uint32_t frag[KC ? 2 : 1][KC ? 2 : NB];  // LDS bytes in half 0; KC: of each stage, each 32 of k
+  uint32_t frag[KC ? 2 : 1][KC ? 2 : 1];  // LDS bytes in half 0; KC: of each stage, each 32 of k
 
   // n: rows of the tile index that are there; index: source rows, if gathered.
   __device__ __forceinline__ void init(int tid, const bf16_t* b, int64_t i0, int n, int64_t ld_,
@@ -79,10 +79,9 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
         off[h] = (uint32_t)(((GATHER && index ? 0 : k * ld) + (col < n ? col : 0)) * 2);
       }
       const int gr = (l16 >> 2) | ((G & 1) << 2);
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-        frag[0][i] = lds + (uint32_t)((8 * G + (l16 >> 2)) * 256 + ((((row0 >> 4) + i) ^ gr) << 5) +
-                                      (l16 & 3) * 8);
+      // block i lies at this ^ 32 i: row0 is a multiple of 16 NB, so i is in the
+      // low bits of the pair of units alone
+      frag[0][0] = lds + (uint32_t)((8 * G + (l16 >> 2)) * 256 + (((row0 >> 4) ^ gr) << 5) + (l16 & 3) * 8);
     }
     if constexpr (KC)
 #pragma unroll
@@ -125,9 +124,10 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
           f[i][ks] = *(const __attribute__((address_space(3))) u32x4_t*)(
               (lds_ptr)frag[PAR][ks] + (half + 2048 * i));
     } else {
-      uint32_t q[NB];
+      uint32_t q[NB], first = frag[0][0];
+      asm volatile("" : "+v"(first));  // made anew each time: registers are short
 #pragma unroll
-      for (int i = 0; i < NB; ++i) q[i] = frag[0][i] + (PAR * 4 * kPipeHalf * 16 + half);
+      for (int i = 0; i < NB; ++i) q[i] = (first ^ (32u * i)) + (PAR * 4 * kPipeHalf * 16 + half);
       read_tr_blocks<1024, 8192>(q, f);
     }
   }
@@ -161,6 +161,7 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
   const bool gather_k = XG && w.rows;
   PipeOperand<XKC, XG, 4> X;
   PipeOperand<YKC, YG, 2> Y;
+  // the kernel has no other LDS: the ring starts at 0, as the blocks' addresses need
   const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
 
   // Runs of k: all of it, but for gathered rows of k as many as LDS holds.
@@ -216,24 +217,26 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
             acc[4 * hm + i][2 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
       __builtin_amdgcn_s_setprio(0);
     };
-    auto stage = [&](auto par, auto check, int s) __attribute__((always_inline)) {
+    // HALF: no row of Y half 1 is there, its phases only keep the step
+    auto stage = [&](auto par, auto check, auto half, int s) __attribute__((always_inline)) {
       constexpr int P = par.value;
+      constexpr bool HALF = half.value;
       std::integral_constant<int, 1 - P> other;
       X.template read<P>(kX0 * kPipeHalf * 16, xf);
       copy_x(other, check, s + 1, 1);
       landed();
       products(0, 0, y0);
       done();
-      Y.template read<P>(kY1 * kPipeHalf * 16, y1);
+      if constexpr (!HALF) Y.template read<P>(kY1 * kPipeHalf * 16, y1);
       copy_y(par, check, s + 2, 0);
       fetch_rows(s + 2);
       landed();
-      products(0, 1, y1);
+      if constexpr (!HALF) products(0, 1, y1);
       done();
       X.template read<P>(kX1 * kPipeHalf * 16, xf);
       copy_x(par, check, s + 2, 0);
       landed();
-      products(1, 1, y1);
+      if constexpr (!HALF) products(1, 1, y1);
       done();
       u32x4_t next[2][2];
       Y.template read<1 - P>(kY0 * kPipeHalf * 16, next);
@@ -265,16 +268,20 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
     Y.template read<0>(kY0 * kPipeHalf * 16, y0);
     done();
     if (late) done();
-    int s = 0;
     // stages whose copies all lie within K, then the rest
-    for (; 64 * (s + 4) <= K; s += 2) {
-      stage(even, whole, s);
-      stage(odd, whole, s + 1);
-    }
-    for (; s < n_st; s += 2) {
-      stage(even, check, s);
-      if (s + 1 < n_st) stage(odd, check, s + 1);
-    }
+    auto stages = [&](auto half) __attribute__((always_inline)) {
+      int s = 0;
+      for (; 64 * (s + 4) <= K; s += 2) {
+        stage(even, whole, half, s);
+        stage(odd, whole, half, s + 1);
+      }
+      for (; s < n_st; s += 2) {
+        stage(even, check, half, s);
+        if (s + 1 < n_st) stage(odd, check, half, s + 1);
+      }
+    };
+    if (MODE != kBwdKer && w.n_valid <= 128) stages(std::integral_constant<bool, true>{});
+    else stages(std::integral_constant<bool, false>{});
     if (!late) done();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
     if (!gather_k) break;

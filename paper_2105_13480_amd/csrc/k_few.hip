@@ -122,10 +122,8 @@ __device__ __forceinline__ void clear(f32x4_t (&acc)[FB][RB]) {
     for (int b = 0; b < RB; ++b) acc[f][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 }
 
-// PARTS 0: results to D.  Else scaled results to rows of the low-rank operand:
-// PARTS parts of nlp ranks, and zeros where M < nlp.
-template <typename T, typename TO, int FB, int RB, int NW, int PARTS>
-__global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) {
+template <typename T, typename TO, int FB, int RB, int NW>
+__global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a) {
   __shared__ f32x4_t red[NW * FB * RB * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int MT = (a.M + 16 * FB - 1) / (16 * FB);
@@ -134,7 +132,6 @@ __global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) 
   const int l16 = lane & 15, G = lane >> 4;
   const int m0 = 16 * FB * t.mt, n_valid = min(t.n1 - t.n0, 16 * RB);
   const bool live = t.g < a.Ng;
-  if (PARTS && !live) return;  // rows without an adapter
 
   const T* const X = reinterpret_cast<const T*>(a.X) + (live ? t.g : 0) * a.xgroup;
   const T* x[FB];
@@ -161,22 +158,7 @@ __global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a, AdaptArgs ad) 
     if (n >= n_valid) continue;
     f32x4_t s = block_sum(red, blk, NW, lane);
     if (!live || (none >> b & 1)) s = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    if constexpr (PARTS == 0) {
-      store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s);
-    } else {
-      const float scale = ad.scales ? ad.scales[t.g] : 1.f;
-      T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(t.n0 + n) * ad.hl;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (m + e >= ad.nlp) break;
-        const float h = m + e < a.M ? s[e] * scale : 0.f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-          if constexpr (sizeof(T) == 4) row[m + e] = h;
-          else row[p * ad.nlp + m + e] = (T)(__float_as_uint(bf16_part(h, p)) >> 16);
-        }
-      }
-    }
+    store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s);
   }
 }
 
@@ -363,31 +345,12 @@ template <typename T, typename TO, int FB, int RB, int NW>
 hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
   const int64_t mt = (a.M + 16 * FB - 1) / (16 * FB), parts = a.Ng + 1 < a.N ? a.Ng + 1 : a.N;
   const dim3 grid((uint32_t)((a.N / (16 * RB) + parts) * mt)), block(64 * NW);
-  group_few<T, TO, FB, RB, NW, 0><<<grid, block, 0, stream>>>(a, AdaptArgs{});
+  group_few<T, TO, FB, RB, NW><<<grid, block, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, typename TO> hipError_t launch_few_typed(const GroupArgs& a, hipStream_t stream) {
   return launch_few<T, TO, 1, 1, 4>(a, stream);
-}
-
-template <typename T, typename TO, int PARTS>
-hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
-  const int64_t parts = ad.Na + 1 < a.N ? ad.Na + 1 : a.N;
-  GroupArgs h = a;
-  h.X = ad.A;
-  h.xgroup = (int64_t)ad.Nl * a.K;
-  h.M = ad.Nl;
-  h.Ng = ad.Na;
-  const dim3 block(64 * 4);
-  auto grid = [&](int FB, int RB) {
-    return dim3((uint32_t)((a.N / (16 * RB) + parts) * ((ad.Nl + 16 * FB - 1) / (16 * FB))));
-  };
-  if (ad.Nl <= 16)
-    group_few<T, TO, 1, 2, 4, PARTS><<<grid(1, 2), block, 0, stream>>>(h, ad);
-  else
-    group_few<T, TO, 4, 2, 4, PARTS><<<grid(4, 2), block, 0, stream>>>(h, ad);
-  return hipGetLastError();
 }
 
 template <typename T, int DF, int TN>
@@ -456,14 +419,6 @@ hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
     case CNN_F32: return launch_few_typed<float, float>(a, stream);
     case CNN_BF16: return launch_few_typed<bf16_t, float>(a, stream);
     default: return launch_few_typed<bf16_t, bf16_t>(a, stream);
-  }
-}
-
-hipError_t launch_adapt_down(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
-  switch (dtype) {
-    case CNN_F32: return launch_down<float, float, 1>(a, ad, stream);
-    case CNN_BF16: return launch_down<bf16_t, float, 3>(a, ad, stream);
-    default: return launch_down<bf16_t, bf16_t, 2>(a, ad, stream);
   }
 }
 

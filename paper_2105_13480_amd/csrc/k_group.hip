@@ -81,7 +81,7 @@ template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
 
 template <typename T, typename TO, int MODE, bool WHOLE>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
-  constexpr bool XKC = MODE == kFwd || MODE == kAdapt, YKC = MODE != kBwdKer;
+  constexpr bool XKC = MODE == kFwd || MODE >= kAdapt, YKC = MODE != kBwdKer;
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
   const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE);
   const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1);
@@ -132,8 +132,29 @@ hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t strea
   return launch_typed<kBwdKer>(a, AdaptArgs{}, dtype, stream);
 }
 
+namespace {
+
+// Rows of the low-rank operand: the product grouped by adapter, whose ranks
+// are few: tiles of 64 ranks by 32 rows.
+template <typename T, typename TO>
+hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+  GroupArgs h = a;
+  h.X = ad.A;
+  h.xgroup = (int64_t)ad.Nl * a.K;
+  h.M = ad.Nl;
+  h.Ng = ad.Na;
+  const int64_t rt = row_tiles_of<kDown>(h, 32);
+  if (copies_ok(h.X, h.ldx, h.M, true, sizeof(T)) && copies_ok(h.Y, h.ldy, h.N, true, sizeof(T)))
+    return launch_tiles<T, TO, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream);
+  return launch_tiles<T, TO, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
+}
+
+}  // namespace
+
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
-  const hipError_t e = launch_adapt_down(a, ad, dtype, stream);
+  const hipError_t e = dtype == CNN_F32    ? launch_down<float, float>(a, ad, stream)
+                       : dtype == CNN_BF16 ? launch_down<bf16_t, float>(a, ad, stream)
+                                           : launch_down<bf16_t, bf16_t>(a, ad, stream);
   if (e != hipSuccess) return e;
   GroupArgs g = a;
   g.off = nullptr;

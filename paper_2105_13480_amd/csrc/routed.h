@@ -103,7 +103,6 @@ bool adapt_few(int64_t Nt);
 FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk);
 hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 // Rows in the order of their adapters (a.off, a.rows, ad.ids).
-hipError_t launch_adapt_down(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 
 }  // namespace cnnlib
