@@ -76,10 +76,14 @@ template <typename T, bool KC, int R> __device__ __forceinline__ int unit_at(int
   if constexpr (KC) return r * 8 + (c ^ ((r >> 1) & 7));
   constexpr int U = R * (int)sizeof(T) / 16;
   if constexpr (sizeof(T) == 2) {
-    const int g = U >= 16 ? (r & 3) | ((r >> 1) & 4) : ((r >> 1) & 1) | ((r >> 2) & 2);
+    const int g = U >= 16  ? (r & 3) | ((r >> 1) & 4)
+                  : U == 8 ? ((r >> 1) & 1) | ((r >> 2) & 2)
+                           : (r >> 3) & 1;
+    static_assert(KC || U >= 4, "a pair of units to trade places with");
     return r * U + (c ^ (g << 1));
   } else {
-    return r * U + (c ^ (((r >> 2) & 3) << 2));
+    static_assert(KC || U >= 8, "four units to trade places with");
+    return r * U + (c ^ (((r >> 2) & (U >= 16 ? 3 : 1)) << 2));
   }
 }
 

@@ -40,19 +40,21 @@ struct TileCost {
 constexpr TileCost kBf16[] = {{256, 256, 1.33, 1.30, 10.5, 3.5},
                               {128, 128, 0.65, 0.50, 2.5, 4.0},
                               {64, 64, 0.28, 0.19, 1.1, 3.6},
-                              {64, 32, 0.19, 0.137, 0.6, 4.6}};
+                              {64, 32, 0.19, 0.137, 0.6, 4.6},
+                              {32, 32, 0.17, 0.09, 0.4, 4.4}};
 // fp32: the matrix unit's time at every size (2048 operations in 32 clocks)
 constexpr TileCost kF32[] = {{0, 0, 0, 0, 0, 0},
-                             {128, 128, 1.80, 1.75, 2.5, 4.0},
-                             {64, 64, 0.50, 0.45, 1.1, 3.6},
-                             {64, 32, 0.30, 0.24, 0.6, 4.6}};
+                             {128, 128, 2.04, 2.06, 1.5, 7.5},
+                             {64, 64, 0.67, 0.565, 1.0, 3.8},
+                             {64, 32, 0.42, 0.33, 0.5, 3.6},
+                             {32, 32, 0.30, 0.18, 0.4, 3.6}};
 
 // The cheapest of the tile sizes from `first` on (0: with the pipelined
 // kernel).  Group sizes are not known here: of several groups, half a tile each
 // is taken to be empty.
 template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
   const TileCost* const c = sizeof(T) == 2 ? kBf16 : kF32;
-  const int last = MODE == kBwdKer ? 2 : 3;
+  const int last = MODE == kBwdKer ? 2 : 4;
   const double cus = device_cus();
   int best = first;
   double least = 1e30;
@@ -92,12 +94,18 @@ hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t str
     return dma ? launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, stream)
                : launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
   }
-  if constexpr (MODE != kBwdKer)
+  if constexpr (MODE != kBwdKer) {
+    if (pick == 4) {
+      const int64_t rt = row_tiles_of<MODE>(a, 32);
+      return dma ? launch_tiles<T, TO, MODE, 32, 32, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
+                 : launch_tiles<T, TO, MODE, 32, 32, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
+    }
     if (pick == 3) {
       const int64_t rt = row_tiles_of<MODE>(a, 32);
       return dma ? launch_tiles<T, TO, MODE, 64, 32, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
                  : launch_tiles<T, TO, MODE, 64, 32, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
     }
+  }
   const int64_t rt = row_tiles_of<MODE>(a, 64);
   return dma ? launch_tiles<T, TO, MODE, 64, 64, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
              : launch_tiles<T, TO, MODE, 64, 64, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
@@ -135,7 +143,7 @@ hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t strea
 namespace {
 
 // Rows of the low-rank operand: the product grouped by adapter, whose ranks
-// are few: tiles of 64 ranks by 32 rows.
+// are few: tiles of 64 or 16 ranks by 32 rows.
 template <typename T, typename TO>
 hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   GroupArgs h = a;
@@ -144,9 +152,12 @@ hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stre
   h.M = ad.Nl;
   h.Ng = ad.Na;
   const int64_t rt = row_tiles_of<kDown>(h, 32);
-  if (copies_ok(h.X, h.ldx, h.M, true, sizeof(T)) && copies_ok(h.Y, h.ldy, h.N, true, sizeof(T)))
-    return launch_tiles<T, TO, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream);
-  return launch_tiles<T, TO, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
+  const bool dma = copies_ok(h.X, h.ldx, h.M, true, sizeof(T)) && copies_ok(h.Y, h.ldy, h.N, true, sizeof(T));
+  if (ad.Nl <= 16)
+    return dma ? launch_tiles<T, TO, kDown, 16, 32, 1, 2, 6>(h, ad, rt, 1, stream)
+               : launch_tiles<T, TO, kDown, 16, 32, 1, 2, 0>(h, ad, rt, 1, stream);
+  return dma ? launch_tiles<T, TO, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream)
+             : launch_tiles<T, TO, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
 }
 
 }  // namespace
