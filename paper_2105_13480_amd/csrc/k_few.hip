@@ -166,11 +166,11 @@ __global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a) {
 // The first workgroups, (tile of 16 rows, q, z), take every Q-th of the
 // adapters that the tile's rows name, 16 DF ranks at a time, over slice z of
 // k: H[z][n][r] = sum_k In[n, k] A[ids[n]][r, k].  The rest, (block of 64
-// features, slice of k), take all rows: part[z][n][m] = sum_k In[n, k] Ker[m, k].
+// features, TN rows, slice of k): part[z][n][m] = sum_k In[n, k] Ker[m, k].
 // Neither waits for the other, and a slice is short, so that most of Ker is
 // asked for at once.  RING: the projection's operands go through a ring of
-// four stages in LDS (4-byte boundaries, whole units of k: 64 features read In
-// a quarter as often as 16), else straight to the registers.
+// four stages in LDS (rows on 4-byte boundaries; 64 features read In a quarter
+// as often as 16), else straight to the registers.
 constexpr int kSumWaves = 4, kSumDepth = 4, kSumFeatures = 64;
 
 template <typename T, int DF, int TN, bool RING>
@@ -213,11 +213,13 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
     return;
   }
   bid -= f.downs;
-  const int z = bid / f.blocks, m0 = kSumFeatures * (bid % f.blocks), k_lo = z * f.kslice;
+  const int z = bid / (f.blocks * f.rtiles), k_lo = z * f.kslice;
+  const int m0 = kSumFeatures * (bid % f.blocks), n0 = TN * (bid / f.blocks % f.rtiles);
+  const int n_valid = min(a.N - n0, TN);
   const int K = min(a.K - k_lo, f.kslice);
   const T* const X = reinterpret_cast<const T*>(a.X) + k_lo;
-  const T* const Y = reinterpret_cast<const T*>(a.Y) + k_lo;
-  float* const part = ad.part + (int64_t)z * a.N * a.M;
+  const T* const Y = reinterpret_cast<const T*>(a.Y) + n0 * a.ldy + k_lo;
+  float* const part = ad.part + ((int64_t)z * a.N + n0) * a.M;
   if constexpr (RING) {
     constexpr int TK = 128 / (int)sizeof(T), XU = 8 * kSumFeatures, STAGE = XU + 8 * TN;
     u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
@@ -229,40 +231,54 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
     rx.init(16 * wave, lane);
     ry.init(0, lane);
     sx.init(tid, X, a.ldx, m0, min(a.M - m0, kSumFeatures), nullptr, 0);
-    sy.init(tid, Y, a.ldy, 0, a.N, nullptr, 0);
+    sy.init(tid, Y, a.ldy, 0, n_valid, nullptr, 0);
     f32x4_t acc[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int n_st = (K + TK - 1) / TK;
+    // as in group_tiles; where k ends inside a unit, its last stage goes through
+    // registers
+    const bool ends_inside = K % (16 / (int)sizeof(T)) != 0;
+    const int n_st = ends_inside ? K / TK : (K + TK - 1) / TK;
     auto copy = [&](int s) __attribute__((always_inline)) {
       u32x4_t* const dst = ring + s % kSumDepth * STAGE;
-      sx.copy(tid, dst, s * TK, a.ldx, K, nullptr, 0);
-      sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
+      sx.copy(tid, dst, s * TK, a.ldx, s < n_st ? K : 0, nullptr, 0);
+      sy.copy(tid, dst + XU, s * TK, a.ldy, s < n_st ? K : 0, nullptr, 0);
     };
-#pragma unroll
-    for (int s = 0; s < kSumDepth - 1; ++s) copy(s);
-    for (int s = 0; s < n_st; ++s) {
-      // as in group_tiles
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 2)) : "memory");
-      copy(s + kSumDepth - 1);
+    auto compute = [&](const u32x4_t* stage) __attribute__((always_inline)) {
       u32x4_t xf[1][2], yf[RB][2];
-      rx.read(ring + s % kSumDepth * STAGE, xf);
-      ry.read(ring + s % kSumDepth * STAGE + XU, yf);
+      rx.read(stage, xf);
+      ry.read(stage + XU, yf);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int b = 0; b < RB; ++b) acc[b] = mma<T>(xf[0][ks], yf[b][ks], acc[b]);
+    };
+#pragma unroll
+    for (int s = 0; s < kSumDepth - 1; ++s) copy(s);
+    for (int s = 0; s < n_st; ++s) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 2)) : "memory");
+      copy(s + kSumDepth - 1);
+      compute(ring + s % kSumDepth * STAGE);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
+    if (ends_inside && n_st * TK < K) {
+      sx.load(n_st * TK, a.ldx, K, nullptr, 0);
+      sy.load(n_st * TK, a.ldy, K, nullptr, 0);
+      __syncthreads();
+      sx.commit(tid, ring);
+      sy.commit(tid, ring + XU);
+      __syncthreads();
+      compute(ring);
+    }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       const int n = 16 * b + l16;
-      if (n < a.N) store4(part + (int64_t)n * a.M, m0 + 16 * wave + 4 * G, a.M, acc[b]);
+      if (n < n_valid) store4(part + (int64_t)n * a.M, m0 + 16 * wave + 4 * G, a.M, acc[b]);
     }
   } else {
     const T* y[RB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) y[b] = Y + (int64_t)min(16 * b + l16, a.N - 1) * a.ldy;
+    for (int b = 0; b < RB; ++b) y[b] = Y + (int64_t)min(16 * b + l16, n_valid - 1) * a.ldy;
     // two blocks of features at a time
     for (int m = m0; m < min(m0 + kSumFeatures, a.M); m += 32) {
       const T* x[2];
@@ -273,7 +289,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
       leave_sums(red, acc, wave, NW, lane);
       for (int blk = wave; blk < 2 * RB; blk += NW) {
         const int n = 16 * (blk % RB) + l16;
-        if (n < a.N)
+        if (n < n_valid)
           store4(part + (int64_t)n * a.M, m + 16 * (blk / RB) + 4 * G, a.M, block_sum(red, blk, NW, lane));
       }
       __syncthreads();
@@ -355,10 +371,9 @@ template <typename T, typename TO> hipError_t launch_few_typed(const GroupArgs& 
 
 template <typename T, int DF, int TN>
 void launch_sums(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
-  constexpr int CE = 16 / (int)sizeof(T);
-  const dim3 grid((uint32_t)(f.downs + f.blocks * f.ks)), block(64 * kSumWaves);
+  const dim3 grid((uint32_t)(f.downs + f.blocks * f.rtiles * f.ks)), block(64 * kSumWaves);
   const int red = 16 * 64 * kSumWaves * (DF > TN / 8 ? DF : TN / 8);
-  const bool ring = (((uintptr_t)a.X | (uintptr_t)a.Y) & 3) == 0 && a.K % CE == 0;
+  const bool ring = (((uintptr_t)a.X | (uintptr_t)a.Y) & 3) == 0 && a.K * sizeof(T) % 4 == 0;
   if (ring) {
     const int lds = kSumDepth * 8 * (kSumFeatures + TN) * 16;
     adapt_few_sums<T, DF, TN, true><<<grid, block, lds > red ? lds : red, stream>>>(a, ad, f);
@@ -422,15 +437,18 @@ hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
   }
 }
 
-bool adapt_few(int64_t Nt) { return Nt <= 64; }
+// At 269 rows (1024 x 512, rank 8) 12.3 us this way and 17.7 in the order of the
+// adapters, at 512 (768 x 768, rank 8) 12.0 and 17.7, at 771 (fp32, 264 x 637,
+// rank 32, mixed) 36.6 and 22.8.
+bool adapt_few(int64_t Nt) { return Nt <= 512; }
 
 FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk) {
-  (void)Nt;
   FewPlan f = {};
   f.blocks = (int32_t)((Nk + kSumFeatures - 1) / kSumFeatures);
-  // slices of k: a workgroup for each CU, of 256 values of k at least
+  f.rtiles = Nt <= 32 ? 1 : (int32_t)((Nt + 63) / 64);
+  // slices of k: a workgroup for each CU, of some 200 values of k at least
   f.ks = 1;
-  while (f.ks < 8 && f.ks * f.blocks < 256 && Nc >= 512 * f.ks) f.ks *= 2;
+  while (f.ks < 8 && f.ks * f.blocks * f.rtiles < 256 && Nc >= 384 * f.ks) f.ks *= 2;
   f.kh = Nc >= 1024 ? 4 : 1;
   return f;
 }

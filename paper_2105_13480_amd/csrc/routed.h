@@ -44,7 +44,7 @@ struct AdaptArgs {
 
 // How an adapted product of few rows is split.
 struct FewPlan {
-  int32_t blocks;  // of features
+  int32_t blocks, rtiles;  // of features and of rows
   int32_t ks, kh;  // slices of k of the projection and of H
   int32_t kslice, hslice, q, downs;  // set by the launch: their lengths, and H's workgroups
 };
