@@ -652,24 +652,23 @@ __device__ __forceinline__ void store_parts(const GroupArgs& a, const AdaptArgs&
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int n = yrow(j) + (lane & 15);
-    if (n >= w.n_valid) continue;
-    T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(w.n0 + n) * ad.hl;
+    T* const row = reinterpret_cast<T*>(ad.Hp) + (int64_t)(w.n0 + min(n, w.n_valid - 1)) * ad.hl;
+    const int ranks = n < w.n_valid ? ad.nlp : 0;  // a multiple of four
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int m = w.m0 + xrow(i) + 4 * (lane >> 4);
-      if (m >= ad.nlp) continue;  // a multiple of four
       float h[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = m + e < a.M ? acc[i][j][e] * scale : 0.f;
       if constexpr (sizeof(T) == 4) {
-        __builtin_memcpy(row + m, h, 16);
+        if (m < ranks) __builtin_memcpy(row + m, h, 16);
       } else {
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           bf16_t v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(__float_as_uint(bf16_part(h[e], p)) >> 16);
-          __builtin_memcpy(row + p * ad.nlp + m, v, 8);
+          if (m < ranks) __builtin_memcpy(row + p * ad.nlp + m, v, 8);
         }
       }
     }

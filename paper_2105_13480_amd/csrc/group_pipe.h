@@ -116,6 +116,7 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
 
   template <int PAR> __device__ __forceinline__ void read(uint32_t half, u32x4_t (&f)[NB][2]) const {
     if constexpr (KC) {
+#if defined(__HIP_DEVICE_COMPILE__)
       typedef const __attribute__((address_space(3))) char* lds_ptr;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
@@ -123,6 +124,7 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
         for (int i = 0; i < NB; ++i)
           f[i][ks] = *(const __attribute__((address_space(3))) u32x4_t*)(
               (lds_ptr)frag[PAR][ks] + (half + 2048 * i));
+#endif
     } else {
       uint32_t q[NB], first = frag[0][0];
       asm volatile("" : "+v"(first));  // made anew each time: registers are short

@@ -25,30 +25,20 @@ MAX_EXPERTS, MAX_CHOICES = 1024, 16
 _torch = None
 _types = None  # (operands' dtype, result's dtype) -> cnn_dtype
 _here = None
+_i32 = _f32 = None
 
 
 def _load():
-    global _torch, _types, _here
+    global _torch, _types, _here, _i32, _f32
     import torch
     _types = {(torch.float32, torch.float32): CNN_F32, (torch.bfloat16, torch.float32): CNN_BF16,
               (torch.bfloat16, torch.bfloat16): CNN_BF16_OBF16}
     # the current GPU's index, without the lazy initialisation's check where
     # torch offers that (a call on a small tensor is bound by the host)
     _here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _i32, _f32 = torch.int32, torch.float32
     _torch = torch
     return torch
-
-
-def _lib():
-    return cnn._lib or cnn.lib()
-
-
-def _same(here, *tensors):
-    """Whether all are contiguous tensors on GPU `here`."""
-    for t in tensors:
-        if t.get_device() != here or not t.is_contiguous():
-            return False
-    return True
 
 
 def _refuse(**tensors):
@@ -94,8 +84,11 @@ def _dtype(result, *operands):
     return dt
 
 
-def _ptr(t):
-    return 0 if t is None else t.data_ptr()
+def _order(offsets, rows, Np, Ng):
+    _shape("offsets", offsets, Ng + 1)
+    _of(_i32, offsets=offsets, rows=rows)
+    if rows is not None:
+        _shape("rows", rows, Np)
 
 
 def _enter():
@@ -126,7 +119,7 @@ class Routing:
         _enter()
         torch = _torch
         n = i64()
-        _check(_lib().cnn_route_ws(Nt, Ng, Kt, ctypes.byref(n)))
+        _check(cnn.lib().cnn_route_ws(Nt, Ng, Kt, ctypes.byref(n)))
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
         self.Nt, self.Ng, self.Kt = Nt, Ng, Kt
         self.choice = torch.empty((Nt, Kt), dtype=torch.int32, device=device)
@@ -135,6 +128,7 @@ class Routing:
         self.rows = torch.empty(Nt * Kt, dtype=torch.int32, device=device)
         self.slots = torch.empty((Nt, Kt), dtype=torch.int32, device=device)
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+        self.shape, self.ws_bytes = (Nt, Ng), n.value
 
 
 def route(Logits, routing: Routing, over: str = "chosen", stream=None) -> Routing:
@@ -143,17 +137,20 @@ def route(Logits, routing: Routing, over: str = "chosen", stream=None) -> Routin
     the weights are a softmax over "all" allowed experts or over the "chosen"
     ones.  Experts with logit -inf or NaN are never chosen."""
     r = routing
-    if not _same(_enter(), Logits, r.choice):
-        _refuse(Logits=Logits, routing=r.choice)
-    _shape("Logits", Logits, r.Nt, r.Ng)
-    if over not in OVER:
+    here = _enter()
+    choice = r.choice
+    if not (Logits.get_device() == here == choice.get_device() and Logits.is_contiguous()
+            and Logits.shape == r.shape and over in OVER):
+        _refuse(Logits=Logits, routing=choice)
+        _shape("Logits", Logits, r.Nt, r.Ng)
         raise ValueError(f"over must be one of {sorted(OVER)}")
-    dt = _dtype(Logits, Logits)
-    ws = r.ws
-    st = _lib().cnn_route(Logits.data_ptr(), r.choice.data_ptr(), r.gates.data_ptr(),
-                          r.offsets.data_ptr(), r.rows.data_ptr(), r.slots.data_ptr(), r.Nt, r.Ng,
-                          r.Kt, dt, OVER[over], _ptr(ws), 0 if ws is None else ws.numel(),
-                          _raw(stream))
+    dt = _types.get((Logits.dtype, Logits.dtype))
+    if dt is None:
+        raise ValueError("Logits must be float32 or bfloat16")
+    st = (cnn._lib or cnn.lib()).cnn_route(
+        Logits.data_ptr(), choice.data_ptr(), r.gates.data_ptr(), r.offsets.data_ptr(),
+        r.rows.data_ptr(), r.slots.data_ptr(), r.Nt, r.Ng, r.Kt, dt, OVER[over],
+        0 if r.ws is None else r.ws.data_ptr(), r.ws_bytes, _raw(stream))
     if st:
         _check(st)
     return r
@@ -162,22 +159,28 @@ def route(Logits, routing: Routing, over: str = "chosen", stream=None) -> Routin
 def route_bwd(Logits, choice, gates, dGates, dLogits, over: str = "chosen", stream=None):
     """dLogits from dGates, for the choice and gates that ``route`` gave with
     the same ``over``."""
-    if not _same(_enter(), Logits, choice, gates, dGates, dLogits):
-        _refuse(Logits=Logits, choice=choice, gates=gates, dGates=dGates, dLogits=dLogits)
+    here = _enter()
     Nt, Ng = _dims("Logits", Logits, 2)
-    Kt = _dims("choice", choice, 2)[1]
-    _shape("choice", choice, Nt, Kt)
-    _shape("gates", gates, Nt, Kt)
-    _shape("dGates", dGates, Nt, Kt)
-    _shape("dLogits", dLogits, Nt, Ng)
-    _of(_torch.int32, choice=choice)
-    _of(_torch.float32, gates=gates, dGates=dGates)
-    if over not in OVER:
+    pairs = choice.shape
+    if not (Logits.get_device() == here == choice.get_device() == gates.get_device() ==
+            dGates.get_device() == dLogits.get_device() and Logits.is_contiguous()
+            and choice.is_contiguous() and gates.is_contiguous() and dGates.is_contiguous()
+            and dLogits.is_contiguous() and len(pairs) == 2 and pairs[0] == Nt
+            and gates.shape == pairs == dGates.shape and dLogits.shape == Logits.shape
+            and choice.dtype is _i32 and gates.dtype is _f32 is dGates.dtype and over in OVER):
+        _refuse(Logits=Logits, choice=choice, gates=gates, dGates=dGates, dLogits=dLogits)
+        Kt = _dims("choice", choice, 2)[1]
+        _shape("choice", choice, Nt, Kt)
+        _shape("gates", gates, Nt, Kt)
+        _shape("dGates", dGates, Nt, Kt)
+        _shape("dLogits", dLogits, Nt, Ng)
+        _of(_i32, choice=choice)
+        _of(_f32, gates=gates, dGates=dGates)
         raise ValueError(f"over must be one of {sorted(OVER)}")
     dt = _dtype(dLogits, Logits)
-    st = _lib().cnn_route_bwd(Logits.data_ptr(), choice.data_ptr(), gates.data_ptr(),
-                              dGates.data_ptr(), dLogits.data_ptr(), Nt, Ng, Kt, dt, OVER[over],
-                              _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_route_bwd(
+        Logits.data_ptr(), choice.data_ptr(), gates.data_ptr(), dGates.data_ptr(),
+        dLogits.data_ptr(), Nt, Ng, pairs[1], dt, OVER[over], _raw(stream))
     if st:
         _check(st)
     return dLogits
@@ -187,18 +190,23 @@ def combine(In, Out, slots, gates=None, stream=None):
     """Out[t] = sum_j gates[t, j] In[slots[t, j]] (gates None: ones; slot -1
     adds nothing).  Without gates it sums dIn of ``group_bwd_in`` over a row's
     places: the gradient of the gather."""
-    if not _same(_enter(), In, Out, slots, slots if gates is None else gates):
-        _refuse(In=In, Out=Out, slots=slots, gates=gates)
+    here = _enter()
     Np, Nk = _dims("In", In, 2)
     Nt, Kt = _dims("slots", slots, 2)
-    _shape("Out", Out, Nt, Nk)
-    _of(_torch.int32, slots=slots)
-    if gates is not None:
+    if not (In.get_device() == here == Out.get_device() == slots.get_device()
+            and In.is_contiguous() and Out.is_contiguous() and slots.is_contiguous()
+            and Out.shape == (Nt, Nk) and slots.dtype is _i32
+            and (gates is None or (gates.get_device() == here and gates.is_contiguous()
+                                   and gates.shape == slots.shape and gates.dtype is _f32))):
+        _refuse(In=In, Out=Out, slots=slots, gates=gates)
+        _shape("Out", Out, Nt, Nk)
+        _of(_i32, slots=slots)
         _shape("gates", gates, Nt, Kt)
-        _of(_torch.float32, gates=gates)
+        _of(_f32, gates=gates)
     dt = _dtype(Out, In)
-    st = _lib().cnn_combine(In.data_ptr(), slots.data_ptr(), _ptr(gates), Out.data_ptr(), Nt, Kt,
-                            Np, Nk, dt, _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_combine(
+        In.data_ptr(), slots.data_ptr(), 0 if gates is None else gates.data_ptr(), Out.data_ptr(),
+        Nt, Kt, Np, Nk, dt, _raw(stream))
     if st:
         _check(st)
     return Out
@@ -206,52 +214,62 @@ def combine(In, Out, slots, gates=None, stream=None):
 
 def combine_bwd(dOut, In, dIn, dGates, slots, rows, gates=None, stream=None):
     """dIn[p] = gate dOut[t] and dGates[t, j] = dOut[t] . In[p] for p =
-    slots[t, j]; dIn is zero at the places without a pair (rows[p] < 0).
-    dGates None: not wanted."""
-    if not _same(_enter(), dOut, In, dIn, slots, rows, slots if gates is None else gates,
-                 slots if dGates is None else dGates):
-        _refuse(dOut=dOut, In=In, dIn=dIn, dGates=dGates, slots=slots, rows=rows, gates=gates)
+    slots[t, j], t = rows[p]; dIn is zero at the places without a pair (rows[p]
+    < 0), dGates for the choices without a place.  dGates None: not wanted."""
+    here = _enter()
     Np, Nk = _dims("In", In, 2)
     Nt, Kt = _dims("slots", slots, 2)
-    _shape("dOut", dOut, Nt, Nk)
-    _shape("dIn", dIn, Np, Nk)
-    _shape("rows", rows, Np)
-    _of(_torch.int32, slots=slots, rows=rows)
-    for name, t in (("gates", gates), ("dGates", dGates)):
-        if t is not None:
-            _shape(name, t, Nt, Kt)
-            _of(_torch.float32, **{name: t})
+    if not (dOut.get_device() == here == In.get_device() == dIn.get_device() == slots.get_device() ==
+            rows.get_device() and dOut.is_contiguous() and In.is_contiguous()
+            and dIn.is_contiguous() and slots.is_contiguous() and rows.is_contiguous()
+            and dOut.shape == (Nt, Nk) and dIn.shape == In.shape and rows.shape == (Np,)
+            and slots.dtype is _i32 is rows.dtype
+            and (gates is None or (gates.get_device() == here and gates.is_contiguous()
+                                   and gates.shape == slots.shape and gates.dtype is _f32))
+            and (dGates is None or (dGates.get_device() == here and dGates.is_contiguous()
+                                    and dGates.shape == slots.shape and dGates.dtype is _f32))):
+        _refuse(dOut=dOut, In=In, dIn=dIn, dGates=dGates, slots=slots, rows=rows, gates=gates)
+        _shape("dOut", dOut, Nt, Nk)
+        _shape("dIn", dIn, Np, Nk)
+        _shape("rows", rows, Np)
+        _of(_i32, slots=slots, rows=rows)
+        for name, t in (("gates", gates), ("dGates", dGates)):
+            if t is not None:
+                _shape(name, t, Nt, Kt)
+                _of(_f32, **{name: t})
     dt = _dtype(dIn, dOut, In)
-    st = _lib().cnn_combine_bwd(dOut.data_ptr(), In.data_ptr(), slots.data_ptr(), rows.data_ptr(),
-                                _ptr(gates), dIn.data_ptr(), _ptr(dGates), Nt, Kt, Np, Nk, dt,
-                                _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_combine_bwd(
+        dOut.data_ptr(), In.data_ptr(), slots.data_ptr(), rows.data_ptr(),
+        0 if gates is None else gates.data_ptr(), dIn.data_ptr(),
+        0 if dGates is None else dGates.data_ptr(), Nt, Kt, Np, Nk, dt, _raw(stream))
     if st:
         _check(st)
     return dIn, dGates
-
-
-def _group(offsets, rows, Np, Ng):
-    _shape("offsets", offsets, Ng + 1)
-    _of(_torch.int32, offsets=offsets, rows=rows)
-    if rows is not None:
-        _shape("rows", rows, Np)
 
 
 def group_fwd(In, Ker, Out, offsets, rows=None, stream=None):
     """Out[p] = In[rows[p]] Ker[g]^T for the places p of group g
     ([offsets[g], offsets[g+1])): In [Nt, Nc], Ker [Ng, Nk, Nc], Out [Np, Nk].
     rows None: In is in grouped order.  Places past offsets[Ng] get zeros."""
-    if not _same(_enter(), In, Ker, Out, offsets, offsets if rows is None else rows):
-        _refuse(In=In, Ker=Ker, Out=Out, offsets=offsets, rows=rows)
+    here = _enter()
     Nt, Nc = _dims("In", In, 2)
-    Ng, Nk, _ = _dims("Ker", Ker, 3)
-    Np = _dims("Out", Out, 2)[0]
-    _shape("Ker", Ker, Ng, Nk, Nc)
-    _shape("Out", Out, Np if rows is not None else Nt, Nk)
-    _group(offsets, rows, Np, Ng)
+    Ng, Nk, C = _dims("Ker", Ker, 3)
+    Np, K = _dims("Out", Out, 2)
+    if not (In.get_device() == here == Ker.get_device() == Out.get_device() == offsets.get_device()
+            and In.is_contiguous() and Ker.is_contiguous() and Out.is_contiguous()
+            and offsets.is_contiguous() and C == Nc and K == Nk and offsets.shape == (Ng + 1,)
+            and offsets.dtype is _i32
+            and (Np == Nt if rows is None else
+                 rows.get_device() == here and rows.is_contiguous() and rows.dtype is _i32
+                 and rows.shape == (Np,))):
+        _refuse(In=In, Ker=Ker, Out=Out, offsets=offsets, rows=rows)
+        _shape("Ker", Ker, Ng, Nk, Nc)
+        _shape("Out", Out, Nt if rows is None else Np, Nk)
+        _order(offsets, rows, Np, Ng)
     dt = _dtype(Out, In, Ker)
-    st = _lib().cnn_group_fwd(In.data_ptr(), Ker.data_ptr(), Out.data_ptr(), offsets.data_ptr(),
-                              _ptr(rows), Nt, Np, Ng, Nc, Nk, dt, _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_group_fwd(
+        In.data_ptr(), Ker.data_ptr(), Out.data_ptr(), offsets.data_ptr(),
+        0 if rows is None else rows.data_ptr(), Nt, Np, Ng, Nc, Nk, dt, _raw(stream))
     if st:
         _check(st)
     return Out
@@ -261,16 +279,21 @@ def group_bwd_in(dOut, Ker, dIn, offsets, stream=None):
     """dIn[p] = dOut[p] Ker[g], in grouped order: dOut [Np, Nk], Ker
     [Ng, Nk, Nc], dIn [Np, Nc].  ``combine`` without gates adds up a gathered
     row's places."""
-    if not _same(_enter(), dOut, Ker, dIn, offsets):
-        _refuse(dOut=dOut, Ker=Ker, dIn=dIn, offsets=offsets)
+    here = _enter()
     Np, Nk = _dims("dOut", dOut, 2)
-    Ng, _, Nc = _dims("Ker", Ker, 3)
-    _shape("Ker", Ker, Ng, Nk, Nc)
-    _shape("dIn", dIn, Np, Nc)
-    _group(offsets, None, Np, Ng)
+    Ng, K, Nc = _dims("Ker", Ker, 3)
+    if not (dOut.get_device() == here == Ker.get_device() == dIn.get_device() == offsets.get_device()
+            and dOut.is_contiguous() and Ker.is_contiguous() and dIn.is_contiguous()
+            and offsets.is_contiguous() and K == Nk and dIn.shape == (Np, Nc)
+            and offsets.shape == (Ng + 1,) and offsets.dtype is _i32):
+        _refuse(dOut=dOut, Ker=Ker, dIn=dIn, offsets=offsets)
+        _shape("Ker", Ker, Ng, Nk, Nc)
+        _shape("dIn", dIn, Np, Nc)
+        _order(offsets, None, Np, Ng)
     dt = _dtype(dIn, dOut, Ker)
-    st = _lib().cnn_group_bwd_in(dOut.data_ptr(), Ker.data_ptr(), dIn.data_ptr(),
-                                 offsets.data_ptr(), Np, Ng, Nc, Nk, dt, _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_group_bwd_in(dOut.data_ptr(), Ker.data_ptr(), dIn.data_ptr(),
+                                                  offsets.data_ptr(), Np, Ng, Nc, Nk, dt,
+                                                  _raw(stream))
     if st:
         _check(st)
     return dIn
@@ -279,19 +302,25 @@ def group_bwd_in(dOut, Ker, dIn, offsets, stream=None):
 def group_bwd_ker(dOut, In, dKer, offsets, rows=None, stream=None):
     """dKer[g] = sum over group g's places p of dOut[p]^T In[rows[p]]: dOut
     [Np, Nk], In [Nt, Nc], dKer [Ng, Nk, Nc]; zeros for an empty group."""
-    if not _same(_enter(), dOut, In, dKer, offsets, offsets if rows is None else rows):
-        _refuse(dOut=dOut, In=In, dKer=dKer, offsets=offsets, rows=rows)
+    here = _enter()
     Np, Nk = _dims("dOut", dOut, 2)
     Nt, Nc = _dims("In", In, 2)
-    Ng = _dims("dKer", dKer, 3)[0]
-    _shape("dKer", dKer, Ng, Nk, Nc)
-    if rows is None:
-        _shape("In", In, Np, Nc)
-    _group(offsets, rows, Np, Ng)
+    Ng, K, C = _dims("dKer", dKer, 3)
+    if not (dOut.get_device() == here == In.get_device() == dKer.get_device() == offsets.get_device()
+            and dOut.is_contiguous() and In.is_contiguous() and dKer.is_contiguous()
+            and offsets.is_contiguous() and K == Nk and C == Nc and offsets.shape == (Ng + 1,)
+            and offsets.dtype is _i32
+            and (Np == Nt if rows is None else
+                 rows.get_device() == here and rows.is_contiguous() and rows.dtype is _i32
+                 and rows.shape == (Np,))):
+        _refuse(dOut=dOut, In=In, dKer=dKer, offsets=offsets, rows=rows)
+        _shape("dKer", dKer, Ng, Nk, Nc)
+        _shape("In", In, Np if rows is None else Nt, Nc)
+        _order(offsets, rows, Np, Ng)
     dt = _dtype(dKer, dOut, In)
-    st = _lib().cnn_group_bwd_ker(dOut.data_ptr(), In.data_ptr(), dKer.data_ptr(),
-                                  offsets.data_ptr(), _ptr(rows), Nt, Np, Ng, Nc, Nk, dt,
-                                  _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_group_bwd_ker(
+        dOut.data_ptr(), In.data_ptr(), dKer.data_ptr(), offsets.data_ptr(),
+        0 if rows is None else rows.data_ptr(), Nt, Np, Ng, Nc, Nk, dt, _raw(stream))
     if st:
         _check(st)
     return dKer
@@ -310,10 +339,9 @@ def _adapt_dims(In, Ker, A, Out):
 def adapt_workspace(In, Ker, A, Out):
     """A workspace for ``adapt_fwd`` on tensors of these shapes."""
     _enter()
-    torch = _torch
     n = i64()
-    _check(_lib().cnn_adapt_ws(*_adapt_dims(In, Ker, A, Out), ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=In.device)
+    _check(cnn.lib().cnn_adapt_ws(*_adapt_dims(In, Ker, A, Out), ctypes.byref(n)))
+    return _torch.empty(n.value, dtype=_torch.uint8, device=In.device)
 
 
 def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
@@ -321,21 +349,28 @@ def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
     (outside [0, Na): no adapter): In [Nt, Nc], Ker [Nk, Nc], A [Na, Nl, Nc],
     B [Na, Nk, Nl], scales [Na] float32 (None: ones).  ws: the tensor that
     ``adapt_workspace`` gives, kept by the caller."""
-    if not _same(_enter(), In, Ker, A, B, ids, Out, ids if scales is None else scales,
-                 ids if ws is None else ws):
-        _refuse(In=In, Ker=Ker, A=A, B=B, ids=ids, Out=Out, scales=scales, ws=ws)
+    here = _enter()
     Nt, Nc, Nk, Na, Nl = _adapt_dims(In, Ker, A, Out)
-    _shape("B", B, Na, Nk, Nl)
-    _shape("ids", ids, Nt)
-    _of(_torch.int32, ids=ids)
-    if scales is not None:
+    if not (In.get_device() == here == Ker.get_device() == A.get_device() == B.get_device() ==
+            ids.get_device() == Out.get_device() and In.is_contiguous() and Ker.is_contiguous()
+            and A.is_contiguous() and B.is_contiguous() and ids.is_contiguous()
+            and Out.is_contiguous() and B.shape == (Na, Nk, Nl) and ids.shape == (Nt,)
+            and ids.dtype is _i32
+            and (scales is None or (scales.get_device() == here and scales.is_contiguous()
+                                    and scales.shape == (Na,) and scales.dtype is _f32))
+            and (ws is None or (ws.get_device() == here and ws.is_contiguous()))):
+        _refuse(In=In, Ker=Ker, A=A, B=B, ids=ids, Out=Out, scales=scales, ws=ws)
+        _shape("B", B, Na, Nk, Nl)
+        _shape("ids", ids, Nt)
+        _of(_i32, ids=ids)
         _shape("scales", scales, Na)
-        _of(_torch.float32, scales=scales)
+        _of(_f32, scales=scales)
     dt = _dtype(Out, In, Ker, A, B)
-    st = _lib().cnn_adapt_fwd(In.data_ptr(), Ker.data_ptr(), A.data_ptr(), B.data_ptr(),
-                              ids.data_ptr(), _ptr(scales), Out.data_ptr(), Nt, Nc, Nk, Na, Nl, dt,
-                              _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                              _raw(stream))
+    st = (cnn._lib or cnn.lib()).cnn_adapt_fwd(
+        In.data_ptr(), Ker.data_ptr(), A.data_ptr(), B.data_ptr(), ids.data_ptr(),
+        0 if scales is None else scales.data_ptr(), Out.data_ptr(), Nt, Nc, Nk, Na, Nl, dt,
+        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
+        _raw(stream))
     if st:
         _check(st)
     return Out
