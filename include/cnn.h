@@ -527,10 +527,11 @@ int cnn_combine(const void* In, const int32_t* Slots, const float* Gates, void* 
 /*
  * Its gradient: for each pair with a place p = Slots[t][j],
  * dIn[p] = Gates[t][j] dOut[t] and dGates[t][j] = sum_k dOut[t][k] In[p][k] (0
- * without a place).  Rows names the places without a pair (Rows[p] < 0), whose
- * dIn is zero.  A place must belong to one pair, as cnn_route makes them.
- * Gates may be NULL (ones), dGates may be NULL (not wanted).  dOut and In have
- * the operands' type, dIn the result's.
+ * without a place).  It goes through the places p, whose row Rows[p] leads to
+ * Slots: the two must name each other, as cnn_route makes them (Rows[Slots[t][j]]
+ * = t, a place belongs to one pair; Rows[p] < 0, a place without a pair, whose
+ * dIn is zero).  Gates may be NULL (ones), dGates may be NULL (not wanted).
+ * dOut and In have the operands' type, dIn the result's.
  */
 int cnn_combine_bwd(const void* dOut, const void* In, const int32_t* Slots, const int32_t* Rows,
                     const float* Gates, void* dIn, float* dGates, int64_t Nt, int64_t Kt,
