@@ -135,6 +135,99 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
   }
 };
 
+// The low-rank part of an adapted tile, added to acc, by runs of 64 of k as in
+// the main loop (the same places in LDS, two runs at a time): adapter by
+// adapter of the tile's rows, which are in the adapters' order, the rows of B
+// (its parts' ranks over again) and the rows of H.  Only the adapter's own rows
+// take its products, so what is not finite in B stays in them.
+template <typename TO>
+__device__ __forceinline__ void pipe_low_rank(const GroupArgs& a, const AdaptArgs& ad,
+                                              const Tile<bf16_t, TO>& w, int tid, int lane, int wave,
+                                              u32x4_t* lds, uint32_t lds0, f32x4_t (&acc)[8][4]) {
+  const int wm = wave >> 2, wn = wave & 3, l16 = lane & 15;
+  const int r0 = tid >> 3, c8 = 8 * ((tid & 7) ^ ((r0 >> 1) & 7));
+  PipeOperand<true, false, 4> X;
+  PipeOperand<true, false, 2> Y;
+  X.init(tid, nullptr, 0, 1, 0, nullptr, 0, wm * 64, lane, lds0);
+  Y.init(tid, nullptr, 0, 1, 0, nullptr, 0, wn * 32, lane, lds0);
+  const bf16_t* const H = reinterpret_cast<const bf16_t*>(ad.Hp) + (int64_t)w.n0 * ad.hl;
+  for (int pos = 0; pos < w.n_valid;) {
+    // the adapter of row `pos`, and the rows from there on that have it
+    const int id = __builtin_amdgcn_readfirstlane(ad.ids[w.n0 + pos]);
+    if (id < 0 || id >= ad.Na) break;  // rows without an adapter are last
+    int end = pos;
+    for (int b = pos & ~63; b < w.n_valid; b += 64) {
+      const int n = b + lane;
+      end += __popcll(__ballot(n >= pos && n < w.n_valid && ad.ids[w.n0 + min(n, w.n_valid - 1)] == id));
+    }
+    const bf16_t* const B = reinterpret_cast<const bf16_t*>(ad.B) + ((int64_t)id * a.M + w.m0) * ad.Nl;
+    for (int k0 = 0; k0 < ad.hl; k0 += 128) {
+      __syncthreads();  // every wave is done with what is there
+#pragma unroll
+      for (int par = 0; par < 2; ++par) {
+        if (k0 + 64 * par >= ad.hl) break;
+        const int k = k0 + 64 * par + c8;
+        const bool ok = k < ad.hl;
+        const int rank = k % ad.nlp;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // half q / 2, its rows from 64 (q % 2) on
+          const int row = 64 * q + r0;
+          u32x4_t* const dst = lds + par * 4 * kPipeHalf + 64 * wave + 512 * (q & 1);
+          const bf16_t* const bx = B + min(row, w.m_valid - 1) * ad.Nl + rank;
+          const bf16_t* const hy = H + min(row, w.n_valid - 1) * ad.hl + k;
+          const char* const zero = reinterpret_cast<const char*>(zero_unit);
+          copy16_lds(ok ? reinterpret_cast<const char*>(bx) : zero, dst + (q < 2 ? kX0 : kX1) * kPipeHalf);
+          copy16_lds(ok ? reinterpret_cast<const char*>(hy) : zero, dst + (q < 2 ? kY0 : kY1) * kPipeHalf);
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      auto products = [&](auto par) __attribute__((always_inline)) {
+#pragma unroll
+        for (int hm = 0; hm < 2; ++hm) {
+          u32x4_t xf[4][2];
+          X.template read<par.value>((hm ? kX1 : kX0) * kPipeHalf * 16, xf);
+#pragma unroll
+          for (int hn = 0; hn < 2; ++hn) {
+            const int n0 = hn * 128 + wn * 32;  // this wave's rows of the half
+            if (n0 >= end || n0 + 32 <= pos) continue;
+            u32x4_t yf[2][2];
+            Y.template read<par.value>((hn ? kY1 : kY0) * kPipeHalf * 16, yf);
+            const bool all = n0 >= pos && min(n0 + 32, w.n_valid) <= end;
+            if (all) {
+#pragma unroll
+              for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                  for (int j = 0; j < 2; ++j)
+                    acc[4 * hm + i][2 * hn + j] = mma<bf16_t>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const int n = n0 + 16 * j + l16;
+                const bool own = n >= pos && n < end;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  f32x4_t sum = acc[4 * hm + i][2 * hn + j];
+#pragma unroll
+                  for (int ks = 0; ks < 2; ++ks) sum = mma<bf16_t>(xf[i][ks], yf[j][ks], sum);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    acc[4 * hm + i][2 * hn + j][e] = own ? sum[e] : acc[4 * hm + i][2 * hn + j][e];
+                }
+              }
+            }
+          }
+        }
+      };
+      products(std::integral_constant<int, 0>{});
+      if (k0 + 64 < ad.hl) products(std::integral_constant<int, 1>{});
+    }
+    pos = end;
+  }
+}
+
 template <typename TO, int MODE>
 __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, int band) {
   typedef bf16_t T;
@@ -289,7 +382,7 @@ __global__ __launch_bounds__(512, 2) void group_pipe(GroupArgs a, AdaptArgs ad, 
     if (!gather_k) break;
   }
 
-  if constexpr (MODE == kAdapt) low_rank<T, TO, true>(a, ad, w, lane, acc, xrow, yrow);
+  if constexpr (MODE == kAdapt) pipe_low_rank<TO>(a, ad, w, tid, lane, wave, lds, lds0, acc);
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 

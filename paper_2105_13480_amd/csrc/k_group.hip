@@ -85,7 +85,8 @@ template <typename T, typename TO, int MODE, bool WHOLE>
 hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   constexpr bool XKC = MODE == kFwd || MODE >= kAdapt, YKC = MODE != kBwdKer;
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
-  const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE);
+  const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE) &&
+                    (MODE != kAdapt || ((uintptr_t)ad.B & 3) == 0);
   const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1);
   if constexpr (sizeof(T) == 2 && WHOLE)
     if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
