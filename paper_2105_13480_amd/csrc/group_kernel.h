@@ -23,6 +23,8 @@
 // that the 16 lanes of a read meet all 64 banks once.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 #include "routed.h"
 
@@ -787,7 +789,10 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
 
 // TM x TN results by WM x WN waves.  DEPTH > 0: both operands are copied
 // straight to LDS (rows on 4-byte boundaries), DEPTH - 1 stages ahead in a ring
-// of DEPTH; where K ends inside a unit, its last stage goes through registers.
+// of DEPTH.  AHEAD: a wave reads a stage while it multiplies the one before, and
+// the copies are a stage further ahead (64 x 64 and less: 3 to 11 % less time in
+// the forward product at 100 to 3000 rows; 128 x 128 has no registers for it, and
+// the transposing reads of bf16 are waited for where they are made).  Where K ends inside a unit, its last stage goes through registers.
 // DEPTH 0: through registers, at any alignment, two stages.  WHOLE: see low_rank.
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
@@ -797,6 +802,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
   constexpr int CE = 16 / (int)sizeof(T), TK = 8 * CE;
   constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
   constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
+  constexpr bool AHEAD = TM < 128 && YKC && (XKC || sizeof(T) == 4);
 
   extern __shared__ __attribute__((aligned(16))) char smem[];
   u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
@@ -822,16 +828,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
-    u32x4_t xf[NI][2], yf[NJ][2];
-    rx.read(buf, xf);
-    ry.read(buf + XU, yf);
+  auto multiply = [&](const u32x4_t(&xf)[NI][2], const u32x4_t(&yf)[NJ][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i][ks], yf[j][ks], acc[i][j]);
+  };
+  auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
+    u32x4_t xf[NI][2], yf[NJ][2];
+    rx.read(buf, xf);
+    ry.read(buf + XU, yf);
+    multiply(xf, yf);
   };
   auto load = [&](int s) __attribute__((always_inline)) {
     sx.load(s * TK, a.ldx, w.K, xrows, a.Nsrc);
@@ -862,12 +871,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
       };
 #pragma unroll
       for (int s = 0; s < DEPTH - 1; ++s) copy(s);
-      for (int s = 0; s < n_st; ++s) {
-        // this wave's copies of stage s have landed (the later ones' may be in
-        // flight), then every wave's; every wave is done with stage s - 1
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
-        copy(s + DEPTH - 1);
-        compute(ring + (s % DEPTH) * STAGE);
+      if constexpr (AHEAD) {
+        copy(DEPTH - 1);
+        u32x4_t xf[2][NI][2], yf[2][NJ][2];  // of this stage and the next
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 1)) : "memory");
+        rx.read(ring, xf[0]);
+        ry.read(ring + XU, yf[0]);
+        auto step = [&](auto at, int s) __attribute__((always_inline)) {
+          // this wave's copies of stage s + 1 have landed (the later ones' may
+          // be in flight) and it holds stage s; then every wave
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
+          copy(s + DEPTH);
+          const u32x4_t* const next = ring + (s + 1) % DEPTH * STAGE;
+          rx.read(next, xf[1 - at]);
+          ry.read(next + XU, yf[1 - at]);
+          __builtin_amdgcn_sched_barrier(0);  // reads before the products that hide them
+          multiply(xf[at], yf[at]);
+        };
+        int s = 0;
+        for (; s + 2 <= n_st; s += 2) {
+          step(std::integral_constant<int, 0>{}, s);
+          step(std::integral_constant<int, 1>{}, s + 1);
+        }
+        if (s < n_st) step(std::integral_constant<int, 0>{}, s);
+      } else {
+        for (int s = 0; s < n_st; ++s) {
+          // this wave's copies of stage s have landed (the later ones' may be in
+          // flight), then every wave's; every wave is done with stage s - 1
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
+          copy(s + DEPTH - 1);
+          compute(ring + (s % DEPTH) * STAGE);
+        }
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
       if (ends_inside && n_st * TK < w.K) {

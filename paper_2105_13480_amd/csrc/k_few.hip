@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
     f32x4_t acc[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // as in group_tiles; where k ends inside a unit, its last stage goes through
+    // as in group_tiles (AHEAD); where k ends inside a unit, its last stage goes through
     // registers
     const bool ends_inside = K % (16 / (int)sizeof(T)) != 0;
     const int n_st = ends_inside ? K / TK : (K + TK - 1) / TK;
@@ -244,22 +244,34 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
       sx.copy(tid, dst, s * TK, a.ldx, s < n_st ? K : 0, nullptr, 0);
       sy.copy(tid, dst + XU, s * TK, a.ldy, s < n_st ? K : 0, nullptr, 0);
     };
-    auto compute = [&](const u32x4_t* stage) __attribute__((always_inline)) {
-      u32x4_t xf[1][2], yf[RB][2];
-      rx.read(stage, xf);
-      ry.read(stage + XU, yf);
+    u32x4_t xf[2][1][2], yf[2][RB][2];  // of this stage and the next
+    auto read = [&](int at, const u32x4_t* stage) __attribute__((always_inline)) {
+      rx.read(stage, xf[at]);
+      ry.read(stage + XU, yf[at]);
+    };
+    auto multiply = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int b = 0; b < RB; ++b) acc[b] = mma<T>(xf[0][ks], yf[b][ks], acc[b]);
+        for (int b = 0; b < RB; ++b) acc[b] = mma<T>(xf[at][0][ks], yf[at][b][ks], acc[b]);
     };
 #pragma unroll
-    for (int s = 0; s < kSumDepth - 1; ++s) copy(s);
-    for (int s = 0; s < n_st; ++s) {
+    for (int s = 0; s < kSumDepth; ++s) copy(s);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 1)) : "memory");
+    read(0, ring);
+    auto step = [&](auto at, int s) __attribute__((always_inline)) {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 2)) : "memory");
-      copy(s + kSumDepth - 1);
-      compute(ring + s % kSumDepth * STAGE);
+      copy(s + kSumDepth);
+      read(1 - at, ring + (s + 1) % kSumDepth * STAGE);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(at);
+    };
+    int s = 0;
+    for (; s + 2 <= n_st; s += 2) {
+      step(std::integral_constant<int, 0>{}, s);
+      step(std::integral_constant<int, 1>{}, s + 1);
     }
+    if (s < n_st) step(std::integral_constant<int, 0>{}, s);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
     if (ends_inside && n_st * TK < K) {
       sx.load(n_st * TK, a.ldx, K, nullptr, 0);
@@ -268,7 +280,8 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
       sx.commit(tid, ring);
       sy.commit(tid, ring + XU);
       __syncthreads();
-      compute(ring);
+      read(0, ring);
+      multiply(0);
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
@@ -325,15 +338,27 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
     const float* const H = ad.H + (int64_t)n * ad.Nl;
     const int64_t hz = (int64_t)a.N * ad.Nl;
     f32x4_t d = {0.f, 0.f, 0.f, 0.f};
-    int r = 0;
-#pragma unroll 2
-    for (; r + 8 <= ad.Nl; r += 8) {
+    auto ranks = [&](int r, int n) __attribute__((always_inline)) {  // n of 8 from r on
       float p[KH][8];
       T b[4][8];
 #pragma unroll
-      for (int z = 0; z < KH; ++z) __builtin_memcpy(p[z], H + z * hz + r, sizeof(p[z]));
+      for (int z = 0; z < KH; ++z)
+        if (n == 8) {
+          __builtin_memcpy(p[z], H + z * hz + r, sizeof(p[z]));
+        } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) __builtin_memcpy(b[e], B + (int64_t)min(e, left) * ad.Nl + r, sizeof(b[e]));
+          for (int t = 0; t < 8; ++t) p[z][t] = t < n ? H[z * hz + r + min(t, n - 1)] : 0.f;
+        }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const T* const row = B + (int64_t)min(e, left) * ad.Nl + r;
+        if (n == 8) {
+          __builtin_memcpy(b[e], row, sizeof(b[e]));
+        } else {
+#pragma unroll
+          for (int t = 0; t < 8; ++t) b[e][t] = t < n ? row[min(t, n - 1)] : (T)0;
+        }
+      }
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         float h = p[0][t];
@@ -342,14 +367,11 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
 #pragma unroll
         for (int e = 0; e < 4; ++e) d[e] += h * to_f32(b[e][t]);
       }
-    }
-    for (; r < ad.Nl; ++r) {
-      float h = 0.f;
-#pragma unroll
-      for (int z = 0; z < KH; ++z) h += H[z * hz + r];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) d[e] += h * to_f32(B[(int64_t)min(e, left) * ad.Nl + r]);
-    }
+    };
+    int r = 0;
+#pragma unroll 2
+    for (; r + 8 <= ad.Nl; r += 8) ranks(r, 8);
+    if (r < ad.Nl) ranks(r, ad.Nl - r);
     const float s = ad.scales ? ad.scales[id] : 1.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += s * d[e];
@@ -373,8 +395,7 @@ template <typename T, int DF, int TN>
 void launch_sums(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipStream_t stream) {
   const dim3 grid((uint32_t)(f.downs + f.blocks * f.rtiles * f.ks)), block(64 * kSumWaves);
   const int red = 16 * 64 * kSumWaves * (DF > TN / 8 ? DF : TN / 8);
-  const bool ring = (((uintptr_t)a.X | (uintptr_t)a.Y) & 3) == 0 && a.K * sizeof(T) % 4 == 0;
-  if (ring) {
+  if (adapt_few_ring(a.X, a.Y, a.K, sizeof(T))) {
     const int lds = kSumDepth * 8 * (kSumFeatures + TN) * 16;
     adapt_few_sums<T, DF, TN, true><<<grid, block, lds > red ? lds : red, stream>>>(a, ad, f);
   } else {
@@ -393,7 +414,7 @@ void launch_out(const GroupArgs& a, const AdaptArgs& ad, const FewPlan& f, hipSt
 template <typename T, typename TO>
 hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   constexpr int RUN = 256 / (int)sizeof(T);
-  FewPlan f = adapt_few_plan(a.N, a.K, a.M);
+  FewPlan f = adapt_few_plan(a.N, a.K, a.M, sizeof(T));
   // slices of k of whole runs; the last may be shorter or empty
   f.hslice = ((a.K + f.kh - 1) / f.kh + RUN - 1) / RUN * RUN;
   f.kslice = ((a.K + f.ks - 1) / f.ks + RUN - 1) / RUN * RUN;
@@ -437,18 +458,34 @@ hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
   }
 }
 
-// At 269 rows (1024 x 512, rank 8) 12.3 us this way and 17.7 in the order of the
-// adapters, at 512 (768 x 768, rank 8) 12.0 and 17.7, at 771 (fp32, 264 x 637,
-// rank 32, mixed) 36.6 and 22.8.
-bool adapt_few(int64_t Nt) { return Nt <= 512; }
+// bf16 / fp32, us, rows as they come against the order of the adapters: 256 rows of
+// 4096 x 4096, rank 16, 29 / 95 and 36 / 122; 400 rows 44 / 173 and 42 / 182; 333 of
+// 2048 x 2048, rank 32, 25 / 66 and 27 / 68; 512 rows 32 / 83 and 27 / 77, but of
+// 512 x 512, rank 8, 9.2 / 14 and 14 / 20.  Rows that are on no 4-byte boundary go
+// straight to the registers: 1001 x 1537, rank 12, in bf16 at 128 rows 18 and 22, at
+// 256 28 and 23.
+bool adapt_few(int64_t Nt, int64_t Nc, int64_t Nk, bool ring) {
+  if (!ring) return Nt <= 192;
+  return Nt <= 352 || (Nt <= kFewRows && Nc * Nk <= 1 << 20);
+}
+bool adapt_few_ring(const void* Ker, const void* In, int64_t Nc, int es) {
+  return (((uintptr_t)Ker | (uintptr_t)In) & 3) == 0 && Nc * es % 4 == 0;
+}
 
-FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk) {
+FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk, int es) {
   FewPlan f = {};
   f.blocks = (int32_t)((Nk + kSumFeatures - 1) / kSumFeatures);
   f.rtiles = Nt <= 32 ? 1 : (int32_t)((Nt + 63) / 64);
-  // slices of k: a workgroup for each CU, of some 200 values of k at least
+  // slices of k, of some 200 values at least: a workgroup for each CU, or two of
+  // slices that still have 16 stages, since the adapters' workgroups leave the
+  // CUs unequal shares (256 workgroups of whole rows of 4096 in fp32: 156 us, two
+  // slices 92; in bf16 32 and 27; short slices cost more than they even out:
+  // 128 rows of 2048 x 2048 in bf16 15.2 us by four, 17.8 by eight)
   f.ks = 1;
-  while (f.ks < 8 && f.ks * f.blocks * f.rtiles < 256 && Nc >= 384 * f.ks) f.ks *= 2;
+  const int64_t wgs = (int64_t)f.blocks * f.rtiles;
+  while (f.ks < 8 && Nc >= 384 * f.ks &&
+         (f.ks * wgs < 256 || (f.ks * wgs < 512 && Nc * es >= 4096 * f.ks)))
+    f.ks *= 2;
   f.kh = Nc >= 1024 ? 4 : 1;
   return f;
 }

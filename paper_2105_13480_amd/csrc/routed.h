@@ -99,8 +99,10 @@ bool group_few_fits(const GroupArgs& a, int dtype);
 hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream);
 // Whether an adapted product of Nt rows runs the few-rows kernels, which take
 // the rows as they come.
-bool adapt_few(int64_t Nt);
-FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk);
+constexpr int64_t kFewRows = 512;  // at most
+bool adapt_few(int64_t Nt, int64_t Nc, int64_t Nk, bool ring);
+bool adapt_few_ring(const void* Ker, const void* In, int64_t Nc, int es);  // rows on 4-byte boundaries
+FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk, int es);
 hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 // Rows in the order of their adapters (a.off, a.rows, ad.ids).
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);

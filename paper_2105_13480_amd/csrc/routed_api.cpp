@@ -140,23 +140,27 @@ int64_t route_ws_bytes(int64_t Nt, int64_t Ng) {
 // The adapted projection's workspace: few rows, the slices' sums; many, H and
 // the order of the rows.
 struct AdaptWs {
-  int64_t h, part, counts, off, rows, keys, total;
+  int64_t few_h, h, counts, off, rows, total;
 };
+// For every type and alignment: whichever way the rows are taken, it fits.
 AdaptWs adapt_ws(int64_t Nt, int64_t Nc, int64_t Nk, int64_t Na, int64_t Nl) {
   AdaptWs w = {};
-  if (adapt_few(Nt)) {
-    const FewPlan f = adapt_few_plan(Nt, Nc, Nk);
-    w.h = round16(f.kh * Nt * Nl * 4);
-    w.part = round16(f.ks * Nt * Nk * 4);
-  } else {
+  int64_t few = 0, ordered = 0;
+  if (Nt <= kFewRows) {
+    const FewPlan f = adapt_few_plan(Nt, Nc, Nk, 4);  // bf16 has no more slices
+    w.few_h = round16(f.kh * Nt * Nl * 4);
+    few = w.few_h + round16(f.ks * Nt * Nk * 4);
+  }
+  if (!adapt_few(Nt, Nc, Nk, true) || !adapt_few(Nt, Nc, Nk, false)) {
     int32_t chunk, nblocks;
     order_blocks(Nt, &chunk, &nblocks);
     w.h = round16(Nt * adapt_nlp(Nl, CNN_BF16) * 6);  // three bf16 parts, or fp32
     w.counts = round16((int64_t)nblocks * Na * 4);
     w.off = round16((Na + 1) * 4);
-    w.rows = w.keys = round16(Nt * 4);
+    w.rows = round16(Nt * 4);
+    ordered = w.h + w.counts + w.off + 2 * w.rows;
   }
-  w.total = w.h + w.part + w.counts + w.off + w.rows + w.keys;
+  w.total = few > ordered ? few : ordered;
   return w;
 }
 
@@ -381,9 +385,9 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     AdaptArgs ad = {};
     ad.A = A; ad.B = B; ad.ids = Ids; ad.scales = Scales;
     ad.Na = (int32_t)Na; ad.Nl = (int32_t)Nl;
-    if (adapt_few(Nt)) {
+    if (adapt_few(Nt, Nc, Nk, adapt_few_ring(Ker, In, Nc, es))) {
       ad.H = (float*)p;
-      ad.part = (float*)(p + w.h);
+      ad.part = (float*)(p + w.few_h);
       return launched(launch_adapt_few(a, ad, dtype, (hipStream_t)stream));
     }
     ad.Hp = p;
