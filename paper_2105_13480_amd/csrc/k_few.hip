@@ -338,29 +338,16 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
     const float* const H = ad.H + (int64_t)n * ad.Nl;
     const int64_t hz = (int64_t)a.N * ad.Nl;
     f32x4_t d = {0.f, 0.f, 0.f, 0.f};
-    auto ranks = [&](int r, int n) __attribute__((always_inline)) {  // n of 8 from r on
-      float p[KH][8];
-      T b[4][8];
+    auto ranks = [&](auto count, int r) __attribute__((always_inline)) {
+      constexpr int R = count.value;
+      float p[KH][R];
+      T b[4][R];
 #pragma unroll
-      for (int z = 0; z < KH; ++z)
-        if (n == 8) {
-          __builtin_memcpy(p[z], H + z * hz + r, sizeof(p[z]));
-        } else {
+      for (int z = 0; z < KH; ++z) __builtin_memcpy(p[z], H + z * hz + r, sizeof(p[z]));
 #pragma unroll
-          for (int t = 0; t < 8; ++t) p[z][t] = t < n ? H[z * hz + r + min(t, n - 1)] : 0.f;
-        }
+      for (int e = 0; e < 4; ++e) __builtin_memcpy(b[e], B + (int64_t)min(e, left) * ad.Nl + r, sizeof(b[e]));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const T* const row = B + (int64_t)min(e, left) * ad.Nl + r;
-        if (n == 8) {
-          __builtin_memcpy(b[e], row, sizeof(b[e]));
-        } else {
-#pragma unroll
-          for (int t = 0; t < 8; ++t) b[e][t] = t < n ? row[min(t, n - 1)] : (T)0;
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
+      for (int t = 0; t < R; ++t) {
         float h = p[0][t];
 #pragma unroll
         for (int z = 1; z < KH; ++z) h += p[z][t];
@@ -370,8 +357,16 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
     };
     int r = 0;
 #pragma unroll 2
-    for (; r + 8 <= ad.Nl; r += 8) ranks(r, 8);
-    if (r < ad.Nl) ranks(r, ad.Nl - r);
+    for (; r + 8 <= ad.Nl; r += 8) ranks(std::integral_constant<int, 8>{}, r);
+    if (r + 4 <= ad.Nl) {
+      ranks(std::integral_constant<int, 4>{}, r);
+      r += 4;
+    }
+    if (r + 2 <= ad.Nl) {
+      ranks(std::integral_constant<int, 2>{}, r);
+      r += 2;
+    }
+    if (r < ad.Nl) ranks(std::integral_constant<int, 1>{}, r);
     const float s = ad.scales ? ad.scales[id] : 1.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += s * d[e];
