@@ -787,6 +787,21 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
   }
 }
 
+// The order of what follows the last wait: between a stage's MFMAS matrix
+// instructions, its reads (two at a time), copies and their addresses, which a
+// wave alone on its SIMD has nothing else to hide behind.  With more of the
+// addresses to an instruction in bf16, whose are a quarter as many: 1000 rows of
+// 2048 x 2048 16.5 us, in this order 16.0; fp32, 100 rows of 1024 x 1024 10.4 and 9.6.
+template <typename T, int MFMAS> __device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < MFMAS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                        // matrix
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);                      // LDS reads
+    __builtin_amdgcn_sched_group_barrier(0x6, sizeof(T) == 4 ? 2 : 8, 0);  // vector, scalar
+    __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);                       // copies
+  }
+}
+
 // TM x TN results by WM x WN waves.  DEPTH > 0: both operands are copied
 // straight to LDS (rows on 4-byte boundaries), DEPTH - 1 stages ahead in a ring
 // of DEPTH.  AHEAD: a wave reads a stage while it multiplies the one before, and
@@ -881,12 +896,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
           // this wave's copies of stage s + 1 have landed (the later ones' may
           // be in flight) and it holds stage s; then every wave
           asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
-          copy(s + DEPTH);
           const u32x4_t* const next = ring + (s + 1) % DEPTH * STAGE;
           rx.read(next, xf[1 - at]);
           ry.read(next + XU, yf[1 - at]);
-          __builtin_amdgcn_sched_barrier(0);  // reads before the products that hide them
+          copy(s + DEPTH);
           multiply(xf[at], yf[at]);
+          interleave<T, NI * NJ * 2 * (sizeof(T) == 4 ? 4 : 1)>();
         };
         int s = 0;
         for (; s + 2 <= n_st; s += 2) {

@@ -261,10 +261,10 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
     read(0, ring);
     auto step = [&](auto at, int s) __attribute__((always_inline)) {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (kSumDepth - 2)) : "memory");
-      copy(s + kSumDepth);
       read(1 - at, ring + (s + 1) % kSumDepth * STAGE);
-      __builtin_amdgcn_sched_barrier(0);
+      copy(s + kSumDepth);
       multiply(at);
+      interleave<T, RB * 2 * (sizeof(T) == 4 ? 4 : 1)>();
     };
     int s = 0;
     for (; s + 2 <= n_st; s += 2) {
