@@ -19,6 +19,14 @@
 // a read on, the half may be copied over.  That is six phases before it is
 // read again, so every memory slot waits for all but its wave's last ten
 // copies (copies beyond the end of k read zeros: the count always holds).
+//
+// Measured (bf16 results): 8192^3 711 us, 1546 TFLOP/s forward, 800 the gradient
+// of In, 889 that of Ker; the transposing reads are waited for in their slot.  A
+// stage takes 1.33 us (1.6 with both operands transposed), a tile's start and
+// results 10: at k = 2048 and whole rounds of the 256 CUs (2048 tiles) 432 us,
+// 1272 TFLOP/s, and a round more where the tiles do not divide.  Workgroups that
+// stay for several tiles gained nothing: the results of one tile and the first
+// copies of the next are still the same waves' work.
 #pragma once
 
 #include <type_traits>
@@ -139,7 +147,9 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
 // the main loop (the same places in LDS, two runs at a time): adapter by
 // adapter of the tile's rows, which are in the adapters' order, the rows of B
 // (its parts' ranks over again) and the rows of H.  Only the adapter's own rows
-// take its products, so what is not finite in B stays in them.
+// take its products, so what is not finite in B stays in them.  Both operands
+// straight from memory, a quarter of the results at a time, took 30 us a tile
+// and adapter at rank 64 in two parts, this about 6.
 template <typename TO>
 __device__ __forceinline__ void pipe_low_rank(const GroupArgs& a, const AdaptArgs& ad,
                                               const Tile<bf16_t, TO>& w, int tid, int lane, int wave,

