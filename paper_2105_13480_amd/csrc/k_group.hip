@@ -53,7 +53,7 @@ constexpr TileCost kF32[] = {{0, 0, 0, 0, 0, 0},
 // The cheapest of the tile sizes from `first` on (0: with the pipelined
 // kernel).  Group sizes are not known here: of several groups, half a tile each
 // is taken to be empty.
-template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
+template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first, bool* crowded) {
   const TileCost* const c = sizeof(T) == 2 ? kBf16 : kF32;
   const int last = MODE == kBwdKer ? 2 : 4;
   const double cus = device_cus();
@@ -77,9 +77,27 @@ template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first) {
     if (t < least) {
       least = t;
       best = i;
+      *crowded = n * (c[i].tm + c[i].tn) * 512 > 160 * 1024;
     }
   }
   return best;
+}
+
+// The tiles of 64 x 64 and less, by depth of their ring.  Where both operands
+// have k last, a wave reads ahead and copies run the whole depth ahead: in bf16,
+// whose stages are short, three stages let another workgroup onto a crowded CU
+// (3000 rows of 6 groups of 768 x 512 8.6 us, 9.9 by four; 1500 of 4 of 3000 x 768
+// 16.5 and 17.5; 17 rows of each of 28 of 4096 x 1024 48.3 and 49.6, or 35.4 and
+// 33.5 where Ker is in the caches); four are better where all tiles fit (256 rows
+// of 2048 x 2048 9.4 us, 11.1 by three) and in fp32 (3002 rows of 6 groups of
+// 771 x 515 33.5 and 34.6).
+template <typename T, typename TO, int MODE, int TM, int TN, bool WHOLE>
+hipError_t launch_small(const GroupArgs& a, const AdaptArgs& ad, bool dma, bool crowded, hipStream_t stream) {
+  const int64_t rt = row_tiles_of<MODE>(a, TN);
+  if (!dma) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
+  if constexpr (sizeof(T) == 2 && (MODE == kFwd || MODE == kAdapt))
+    if (crowded) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 3, WHOLE>(a, ad, rt, 16, stream);
+  return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream);
 }
 
 template <typename T, typename TO, int MODE, bool WHOLE>
@@ -88,7 +106,8 @@ hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t str
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
   const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE) &&
                     (MODE != kAdapt || ((uintptr_t)ad.B & 3) == 0);
-  const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1);
+  bool crowded = false;
+  const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1, &crowded);
   if constexpr (sizeof(T) == 2 && WHOLE)
     if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
   if (pick == 1) {
@@ -97,20 +116,10 @@ hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t str
                : launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
   }
   if constexpr (MODE != kBwdKer) {
-    if (pick == 4) {
-      const int64_t rt = row_tiles_of<MODE>(a, 32);
-      return dma ? launch_tiles<T, TO, MODE, 32, 32, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
-                 : launch_tiles<T, TO, MODE, 32, 32, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
-    }
-    if (pick == 3) {
-      const int64_t rt = row_tiles_of<MODE>(a, 32);
-      return dma ? launch_tiles<T, TO, MODE, 64, 32, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
-                 : launch_tiles<T, TO, MODE, 64, 32, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
-    }
+    if (pick == 4) return launch_small<T, TO, MODE, 32, 32, WHOLE>(a, ad, dma, crowded, stream);
+    if (pick == 3) return launch_small<T, TO, MODE, 64, 32, WHOLE>(a, ad, dma, crowded, stream);
   }
-  const int64_t rt = row_tiles_of<MODE>(a, 64);
-  return dma ? launch_tiles<T, TO, MODE, 64, 64, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream)
-             : launch_tiles<T, TO, MODE, 64, 64, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
+  return launch_small<T, TO, MODE, 64, 64, WHOLE>(a, ad, dma, crowded, stream);
 }
 
 template <typename T, typename TO, int MODE>
