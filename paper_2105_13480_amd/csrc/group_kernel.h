@@ -73,6 +73,34 @@ template <typename T> __device__ __forceinline__ u32x4_t load_unit(const T* p, i
   return v;
 }
 
+// A unit without its first `e` elements, zeros after the others.
+template <typename T> __device__ __forceinline__ u32x4_t drop_first(u32x4_t v, int e) {
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  const int bits = e * 8 * (int)sizeof(T);
+  if (bits >= 128) return u32x4_t{0u, 0u, 0u, 0u};
+  if (bits >= 64) {
+    lo = hi >> (bits - 64);
+    hi = 0;
+  } else if (bits > 0) {
+    lo = lo >> bits | hi << (64 - bits);
+    hi >>= bits;
+  }
+  return u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// The unit from element k on of a row of n elements; zeros past its end.  Where
+// the end is inside the unit, one load of the row's last 16 bytes (by elements,
+// each load waited for before the next, it took a stage of its own: 28 groups of
+// 17 rows of 4097 by 1023 features in bf16, gradient of In, 245 us).
+template <typename T> __device__ __forceinline__ u32x4_t load_end(const T* row, int k, int n) {
+  constexpr int CE = 16 / (int)sizeof(T);
+  if (n < CE) return load_unit(row + k, n - k);
+  const int start = min(k, n - CE);
+  u32x4_t v;
+  __builtin_memcpy(&v, row + start, 16);
+  return drop_first<T>(v, k - start);
+}
+
 // Where unit `c` (16 bytes) of row `r` of an operand's stage lies.  KC: 8
 // units a row, 16 rows of one unit column hit 16 distinct 16-byte columns.
 // MC: R * sizeof(T) / 16 units a row of k; bf16 keeps pairs of units (the 32
@@ -107,14 +135,17 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
   const T* p[NU];  // the unit's first element at k = 0, or (rows of k) of a row
   int at[NU];      // KC: the unit's first k within a stage; else its row of k
   int lim[KC ? 1 : NU];  // elements of the row from the unit's first
+  bool wide;             // !KC: the row holds a unit; p is at most its last
   int src[GATHER && !KC ? NU : 1];
-  u32x4_t reg[NU];
+  u32x4_t regs[2][NU];
+  uint32_t there[2];     // !KC: whether unit j's row of k is (bit j), of each set
 
   // base: the tensor at its first k; rows [i0, i0 + n) of the tile index are
   // there; ld: elements from row to row; index: source rows of a gathered
   // KC operand.
   __device__ __forceinline__ void init(int tid, const T* base, int64_t ld, int64_t i0, int n,
                                        const int32_t* index, int nsrc) {
+    wide = i0 + n >= CE;
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
       const int u = j * NT + tid;
@@ -132,7 +163,7 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
       } else {
         at[j] = r;
         lim[j] = n - c * CE;
-        p[j] = base + i0 + (lim[j] > 0 ? c * CE : 0);
+        p[j] = base + i0 + (wide ? min(c * CE, n - CE) : lim[j] > 0 ? c * CE : 0);
       }
     }
   }
@@ -182,33 +213,41 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     }
   }
 
-  // Through registers, at any alignment: loads, and later the LDS writes.
+  // Through registers (one of two sets), at any alignment: loads, and later the
+  // LDS writes.
+  template <int SET = 0>
   __device__ __forceinline__ void load(int k0, int64_t ld, int nk, const int32_t* index, int nsrc) {
+    u32x4_t(&reg)[NU] = regs[SET];
     if constexpr (KC) {
       if (k0 + TK <= nk) {  // the whole stage lies within K
 #pragma unroll
         for (int j = 0; j < NU; ++j) __builtin_memcpy(&reg[j], p[j] + k0, 16);
       } else {
 #pragma unroll
-        for (int j = 0; j < NU; ++j) reg[j] = load_unit(p[j] + k0, nk - k0 - at[j]);
+        for (int j = 0; j < NU; ++j) reg[j] = load_end(p[j] - at[j], k0 + at[j], nk);
       }
     } else {
-      int64_t row[NU];
-      bool ok[NU];
+      // what is to be cut off or cleared is so when the loads are waited for
+      there[SET] = 0;
 #pragma unroll
       for (int j = 0; j < NU; ++j) {
-        ok[j] = row_of(j, k0, nk, index, nsrc, &row[j]);
-        reg[j] = u32x4_t{0u, 0u, 0u, 0u};
-        if (lim[j] >= CE) __builtin_memcpy(&reg[j], p[j] + row[j] * ld, 16);
-        else reg[j] = load_unit(p[j] + row[j] * ld, lim[j]);
+        int64_t row;
+        there[SET] |= (uint32_t)row_of(j, k0, nk, index, nsrc, &row) << j;
+        if (wide) __builtin_memcpy(&reg[j], p[j] + row * ld, 16);
+        else reg[j] = load_unit(p[j] + row * ld, lim[j]);
       }
-#pragma unroll
-      for (int j = 0; j < NU; ++j) reg[j] = ok[j] ? reg[j] : u32x4_t{0u, 0u, 0u, 0u};
     }
   }
-  __device__ __forceinline__ void commit(int tid, u32x4_t* lds) const {
+  template <int SET = 0> __device__ __forceinline__ void commit(int tid, u32x4_t* lds) const {
 #pragma unroll
-    for (int j = 0; j < NU; ++j) lds[j * NT + tid] = reg[j];
+    for (int j = 0; j < NU; ++j) {
+      u32x4_t v = regs[SET][j];
+      if constexpr (!KC) {
+        if (wide && lim[j] < CE) v = drop_first<T>(v, CE - lim[j]);
+        if (!(there[SET] >> j & 1)) v = u32x4_t{0u, 0u, 0u, 0u};
+      }
+      lds[j * NT + tid] = v;
+    }
   }
 };
 
@@ -813,7 +852,7 @@ template <typename T, int MFMAS> __device__ __forceinline__ void interleave() {
 // the copies are a stage further ahead (64 x 64 and less: 3 to 11 % less time in
 // the forward product at 100 to 3000 rows; 128 x 128 has no registers for it, and
 // the transposing reads of bf16 are waited for where they are made).  Where K ends inside a unit, its last stage goes through registers.
-// DEPTH 0: through registers, at any alignment, two stages.  WHOLE: see low_rank.
+// DEPTH 0: through registers, at any alignment, two stages in LDS and, in small tiles, two ahead.  WHOLE: see low_rank.
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, AdaptArgs ad, int band) {
   constexpr int NT = 64 * WM * WN;
@@ -862,15 +901,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
     ry.read(buf + XU, yf);
     multiply(xf, yf);
   };
-  auto load = [&](int s) __attribute__((always_inline)) {
-    sx.load(s * TK, a.ldx, w.K, xrows, a.Nsrc);
+  auto load = [&](auto set, int s) __attribute__((always_inline)) {
+    sx.template load<set.value>(s * TK, a.ldx, w.K, xrows, a.Nsrc);
     sx.fetch((s + 1) * TK, w.K, xrows);
-    sy.load(s * TK, a.ldy, w.K, nullptr, 0);
+    sy.template load<set.value>(s * TK, a.ldy, w.K, nullptr, 0);
   };
-  auto commit = [&](int s) __attribute__((always_inline)) {
-    sx.commit(tid, ring + (s & 1) * STAGE);
-    sy.commit(tid, ring + (s & 1) * STAGE + XU);
+  auto commit = [&](auto set, int s) __attribute__((always_inline)) {
+    sx.template commit<set.value>(tid, ring + (s & 1) * STAGE);
+    sy.template commit<set.value>(tid, ring + (s & 1) * STAGE + XU);
   };
+  constexpr std::integral_constant<int, 0> even;
+  constexpr std::integral_constant<int, 1> odd;
 
   if (w.K > 0) {
     sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, nullptr, 0);
@@ -910,10 +951,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
         };
         int s = 0;
         for (; s + 2 <= n_st; s += 2) {
-          step(std::integral_constant<int, 0>{}, s);
-          step(std::integral_constant<int, 1>{}, s + 1);
+          step(even, s);
+          step(odd, s + 1);
         }
-        if (s < n_st) step(std::integral_constant<int, 0>{}, s);
+        if (s < n_st) step(even, s);
       } else {
         for (int s = 0; s < n_st; ++s) {
           // this wave's copies of stage s have landed (the later ones' may be in
@@ -925,21 +966,38 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
       if (ends_inside && n_st * TK < w.K) {
-        load(n_st);
+        load(even, n_st);
         __syncthreads();
-        commit(0);
+        commit(even, 0);
         __syncthreads();
         compute(ring);
       }
     } else {
       const int n_st = (w.K + TK - 1) / TK;
-      load(0);
-      commit(0);
-      for (int s = 0; s < n_st; ++s) {
-        __syncthreads();  // stage s is there; every wave is done with stage s - 1
-        if (s + 1 < n_st) load(s + 1);
-        compute(ring + (s & 1) * STAGE);
-        if (s + 1 < n_st) commit(s + 1);
+      load(even, 0);
+      if constexpr (TM < 128) {  // two stages in flight, one in each set of registers
+        if (n_st > 1) load(odd, 1);
+        commit(even, 0);
+        auto step = [&](auto set, auto other, int s) __attribute__((always_inline)) {
+          __syncthreads();  // stage s is there; every wave is done with stage s - 1
+          if (s + 2 < n_st) load(set, s + 2);
+          compute(ring + (s & 1) * STAGE);
+          if (s + 1 < n_st) commit(other, s + 1);
+        };
+        int s = 0;
+        for (; s + 2 <= n_st; s += 2) {
+          step(even, odd, s);
+          step(odd, even, s + 1);
+        }
+        if (s < n_st) step(even, odd, s);
+      } else {
+        commit(even, 0);
+        for (int s = 0; s < n_st; ++s) {
+          __syncthreads();
+          if (s + 1 < n_st) load(even, s + 1);
+          compute(ring + (s & 1) * STAGE);
+          if (s + 1 < n_st) commit(even, s + 1);
+        }
       }
     }
   }

@@ -82,9 +82,9 @@ __device__ __forceinline__ void few_rows_dot(const T* const (&x)[FB], const T* c
     for (int i = 0; i < 4; ++i) {
       const int k = k0 + (4 * i + G) * R::CE;
 #pragma unroll
-      for (int f = 0; f < FB; ++f) a.x[f][i] = load_unit(x[f] + k, K - k);
+      for (int f = 0; f < FB; ++f) a.x[f][i] = load_end(x[f], k, K);
 #pragma unroll
-      for (int b = 0; b < RB; ++b) a.y[b][i] = load_unit(y[b] + k, K - k);
+      for (int b = 0; b < RB; ++b) a.y[b][i] = load_end(y[b], k, K);
     }
     a.multiply(acc);
   }
