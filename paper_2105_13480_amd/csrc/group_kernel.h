@@ -218,32 +218,44 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
   template <int SET = 0>
   __device__ __forceinline__ void load(int k0, int64_t ld, int nk, const int32_t* index, int nsrc) {
     u32x4_t(&reg)[NU] = regs[SET];
+    // what is to be cut off or cleared is so when the loads are waited for, and
+    // rows shorter than a unit are read only then
     if constexpr (KC) {
-      if (k0 + TK <= nk) {  // the whole stage lies within K
 #pragma unroll
-        for (int j = 0; j < NU; ++j) __builtin_memcpy(&reg[j], p[j] + k0, 16);
-      } else {
-#pragma unroll
-        for (int j = 0; j < NU; ++j) reg[j] = load_end(p[j] - at[j], k0 + at[j], nk);
+      for (int j = 0; j < NU; ++j) {
+        if (nk >= CE) __builtin_memcpy(&reg[j], p[j] - at[j] + min(k0 + at[j], nk - CE), 16);
       }
     } else {
-      // what is to be cut off or cleared is so when the loads are waited for
       there[SET] = 0;
 #pragma unroll
       for (int j = 0; j < NU; ++j) {
         int64_t row;
         there[SET] |= (uint32_t)row_of(j, k0, nk, index, nsrc, &row) << j;
         if (wide) __builtin_memcpy(&reg[j], p[j] + row * ld, 16);
-        else reg[j] = load_unit(p[j] + row * ld, lim[j]);
       }
     }
   }
-  template <int SET = 0> __device__ __forceinline__ void commit(int tid, u32x4_t* lds) const {
+  // Of the stage at k0, as it was loaded.
+  template <int SET = 0>
+  __device__ __forceinline__ void commit(int tid, u32x4_t* lds, int k0, int64_t ld, int nk,
+                                         const int32_t* index, int nsrc) const {
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
       u32x4_t v = regs[SET][j];
-      if constexpr (!KC) {
-        if (wide && lim[j] < CE) v = drop_first<T>(v, CE - lim[j]);
+      if constexpr (KC) {
+        if (nk < CE) v = load_unit(p[j] + k0, nk - k0 - at[j]);
+        else if (k0 + TK > nk) v = drop_first<T>(v, max(k0 + at[j] + CE - nk, 0));
+      } else {
+        if (!wide) {
+          int64_t row = max(min(k0 + at[j], nk - 1), 0);
+          if (GATHER && index) {
+            row = index[row];
+            if (row < 0 || row >= nsrc) row = 0;  // cleared below
+          }
+          v = load_unit(p[j] + row * ld, lim[j]);
+        } else if (lim[j] < CE) {
+          v = drop_first<T>(v, CE - lim[j]);
+        }
         if (!(there[SET] >> j & 1)) v = u32x4_t{0u, 0u, 0u, 0u};
       }
       lds[j * NT + tid] = v;
@@ -907,8 +919,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
     sy.template load<set.value>(s * TK, a.ldy, w.K, nullptr, 0);
   };
   auto commit = [&](auto set, int s) __attribute__((always_inline)) {
-    sx.template commit<set.value>(tid, ring + (s & 1) * STAGE);
-    sy.template commit<set.value>(tid, ring + (s & 1) * STAGE + XU);
+    u32x4_t* const dst = ring + (s & 1) * STAGE;
+    sx.template commit<set.value>(tid, dst, s * TK, a.ldx, w.K, xrows, a.Nsrc);
+    sy.template commit<set.value>(tid, dst + XU, s * TK, a.ldy, w.K, nullptr, 0);
   };
   constexpr std::integral_constant<int, 0> even;
   constexpr std::integral_constant<int, 1> odd;
@@ -968,7 +981,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
       if (ends_inside && n_st * TK < w.K) {
         load(even, n_st);
         __syncthreads();
-        commit(even, 0);
+        sx.commit(tid, ring, n_st * TK, a.ldx, w.K, xrows, a.Nsrc);
+        sy.commit(tid, ring + XU, n_st * TK, a.ldy, w.K, nullptr, 0);
         __syncthreads();
         compute(ring);
       }

@@ -281,8 +281,8 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
       sx.load(n_st * TK, a.ldx, K, nullptr, 0);
       sy.load(n_st * TK, a.ldy, K, nullptr, 0);
       __syncthreads();
-      sx.commit(tid, ring);
-      sy.commit(tid, ring + XU);
+      sx.commit(tid, ring, n_st * TK, a.ldx, K, nullptr, 0);
+      sy.commit(tid, ring + XU, n_st * TK, a.ldy, K, nullptr, 0);
       __syncthreads();
       read(0, ring);
       multiply(0);
