@@ -106,14 +106,19 @@ hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t str
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
   const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE) &&
                     (MODE != kAdapt || ((uintptr_t)ad.B & 3) == 0);
+  // fp32 through registers: 64 x 64 at most (gradient of In, 2000 rows of 2049 x
+  // 2047 172 us, by 128 x 128 220, the other products alike; in bf16 56 and 71 there
+  // but 187 and 162 at 8000 rows)
+  const int first = pipe ? 0 : dma || sizeof(T) == 2 ? 1 : 2;
   bool crowded = false;
-  const int pick = pick_tile<T, MODE>(a, pipe ? 0 : 1, &crowded);
+  const int pick = pick_tile<T, MODE>(a, first, &crowded);
   if constexpr (sizeof(T) == 2 && WHOLE)
     if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
   if (pick == 1) {
     const int64_t rt = row_tiles_of<MODE>(a, 128);
-    return dma ? launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, stream)
-               : launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
+    if constexpr (sizeof(T) == 2)
+      if (!dma) return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
+    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, stream);
   }
   if constexpr (MODE != kBwdKer) {
     if (pick == 4) return launch_small<T, TO, MODE, 32, 32, WHOLE>(a, ad, dma, crowded, stream);
