@@ -151,7 +151,10 @@ SIZES = [([9000, 4200], 2056, 2064, 0), ([5000, 0, 4201, 57, 1], 2056, 1544, 90)
          ([513, 300], 1032, 776, 0), ([40] * 70 + [300, 0, 1], 264, 200, 130),
          ([130, 0, 77, 250], 264, 640, 1), ([130, 0, 77, 250], 263, 129, 1),
          ([20, 9, 31, 0, 12], 136, 72, 2), ([20, 9, 31, 0, 12], 35, 71, 2),
-         ([3] * 9 + [7], 1032, 104, 0), ([33], 2048, 1, 0), ([0, 1, 0], 1, 512, 0)]
+         ([3] * 9 + [7], 1032, 104, 0), ([33], 2048, 1, 0), ([0, 1, 0], 1, 512, 0),
+         # rows shorter than 16 bytes, ends inside 16 bytes, odd sizes in large tiles
+         ([300, 0, 41], 5, 3, 4), ([300, 41], 7, 1023, 0), ([90] * 3, 1023, 5, 1), ([150, 80], 9, 11, 0),
+         ([700, 0, 400], 2047, 130, 3), ([1500, 300], 515, 2049, 0)]
 
 
 def _whole(gen, *shape, top=2, dtype=torch.float32):
@@ -255,7 +258,9 @@ def test_combine_gradients_differences(Nt, Ng, Kt, Nk, mode):
 @pytest.mark.parametrize("mode", ["f32", "bf16", "bf16_obf16"])
 @pytest.mark.parametrize("Nt,Nc,Nk,Na,Nl", [(1, 1032, 520, 3, 8), (40, 264, 72, 70, 16), (300, 2056, 328, 5, 12),
                                             (700, 520, 640, 3, 40), (600, 515, 131, 4, 7), (1500, 264, 328, 2, 16),
-                                            (4000, 264, 2080, 6, 8), (5000, 1032, 2048, 3, 16)])
+                                            (4000, 264, 2080, 6, 8), (5000, 1032, 2048, 3, 16),
+                                            (333, 1001, 153, 5, 12), (150, 1001, 77, 4, 9),
+                                            (450, 2048, 2048, 3, 8), (9, 5, 3, 2, 2), (700, 1003, 259, 3, 64)])
 def test_adapt_exact(Nt, Nc, Nk, Na, Nl, mode):
     """Whole numbers; A has few entries a row, so that every value of the low
     rank product has at most 16 bits (two parts in bf16) and no sum passes 2^24."""
