@@ -566,9 +566,9 @@ int cnn_group_bwd_ker(const void* dOut, const void* In, void* dKer, const int32_
  * In[Nt][Nc], Ker[Nk][Nc], A[Na][Nl][Nc], B[Na][Nk][Nl], Scales[Na] (NULL:
  * ones), Na <= 1024, Nl <= 4096.  A row whose Ids is outside [0, Na) has no
  * adapter.  Adapters of smaller rank are stored with zeros up to Nl.  The inner
- * sum is kept to fp32 (bf16 Out: to 2^-16 of itself).  For calls that serve;
- * gradients are those of cnn_group_* with the adapters as groups.  workspace:
- * cnn_adapt_ws bytes, 16-byte aligned.  Errors as cnn_route.
+ * sum is kept to fp32.  For calls that serve; gradients are those of
+ * cnn_group_* with the adapters as groups.  workspace: cnn_adapt_ws bytes,
+ * 16-byte aligned.  Errors as cnn_route.
  */
 int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
                   const int32_t* Ids, const float* Scales, void* Out, int64_t Nt, int64_t Nc,

@@ -719,12 +719,16 @@ __device__ __forceinline__ void store_tile(const GroupArgs& a, const Tile<T, TO>
 }
 
 // Rows of the low-rank operand from the results of In A^T: scaled, and in bf16
-// as the sum of PARTS bf16 values, each part nlp ranks (zeros past M).
+// as the sum of three bf16 values of 8 bits each, all 24 of the fp32 one, each
+// part nlp ranks (zeros past M).  Two parts, for a bf16 result, cut off up to
+// 2^-15 of a value, always with one sign: the result then was 1.0e-4 of its norm
+// from that of an fp32 factor (rank 64, 2048 features), where the order of the
+// sums makes 2e-5.
 template <typename T, typename TO, int NI, int NJ, typename XR, typename YR>
 __device__ __forceinline__ void store_parts(const GroupArgs& a, const AdaptArgs& ad,
                                             const Tile<T, TO>& w, int lane, f32x4_t (&acc)[NI][NJ],
                                             XR xrow, YR yrow) {
-  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(TO) == 2 ? 2 : 3;
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;
   const float scale = ad.scales ? ad.scales[w.g] : 1.f;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {

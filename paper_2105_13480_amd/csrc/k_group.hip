@@ -160,8 +160,7 @@ namespace {
 
 // Rows of the low-rank operand: the product grouped by adapter, whose ranks
 // are few: tiles of 64 or 16 ranks by 32 rows.
-template <typename T, typename TO>
-hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+template <typename T> hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
   GroupArgs h = a;
   h.X = ad.A;
   h.xgroup = (int64_t)ad.Nl * a.K;
@@ -170,18 +169,17 @@ hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stre
   const int64_t rt = row_tiles_of<kDown>(h, 32);
   const bool dma = copies_ok(h.X, h.ldx, h.M, true, sizeof(T)) && copies_ok(h.Y, h.ldy, h.N, true, sizeof(T));
   if (ad.Nl <= 16)
-    return dma ? launch_tiles<T, TO, kDown, 16, 32, 1, 2, 6>(h, ad, rt, 1, stream)
-               : launch_tiles<T, TO, kDown, 16, 32, 1, 2, 0>(h, ad, rt, 1, stream);
-  return dma ? launch_tiles<T, TO, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream)
-             : launch_tiles<T, TO, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
+    return dma ? launch_tiles<T, T, kDown, 16, 32, 1, 2, 6>(h, ad, rt, 1, stream)
+               : launch_tiles<T, T, kDown, 16, 32, 1, 2, 0>(h, ad, rt, 1, stream);
+  return dma ? launch_tiles<T, T, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream)
+             : launch_tiles<T, T, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
 }
 
 }  // namespace
 
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
-  const hipError_t e = dtype == CNN_F32    ? launch_down<float, float>(a, ad, stream)
-                       : dtype == CNN_BF16 ? launch_down<bf16_t, float>(a, ad, stream)
-                                           : launch_down<bf16_t, bf16_t>(a, ad, stream);
+  const hipError_t e =
+      dtype == CNN_F32 ? launch_down<float>(a, ad, stream) : launch_down<bf16_t>(a, ad, stream);
   if (e != hipSuccess) return e;
   GroupArgs g = a;
   g.off = nullptr;

@@ -33,8 +33,8 @@ struct AdaptArgs {
   const float* scales;   // [Na] or NULL
   int32_t Na, Nl;
   // Many rows, in the order of their adapters: scaled H as operand rows of
-  // `hl` elements, in bf16 the leading two or three bf16 parts of the fp32
-  // values, `nlp` ranks each (Nl up to a unit, zeros past it).
+  // `hl` elements, in bf16 the three bf16 parts of the fp32 values, `nlp` ranks
+  // each (Nl up to a unit, zeros past it).
   void* Hp;
   int32_t nlp, hl;
   // Few rows, as they come: partial sums over slices of k.
@@ -53,7 +53,7 @@ struct FewPlan {
 inline int adapt_nlp(int64_t Nl, int dtype) {
   return (int)(dtype == CNN_F32 ? (Nl + 3) & ~(int64_t)3 : (Nl + 7) & ~(int64_t)7);
 }
-inline int adapt_parts(int dtype) { return dtype == CNN_F32 ? 1 : dtype == CNN_BF16 ? 3 : 2; }
+inline int adapt_parts(int dtype) { return dtype == CNN_F32 ? 1 : 3; }
 
 // The rows of a problem in the order of a key (experts of (row, choice) pairs,
 // adapters of rows): a counting sort by workgroups of `chunk` rows.

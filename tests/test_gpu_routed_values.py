@@ -1,0 +1,59 @@
+"""Values that the routed contractions must keep: a low-rank factor of more bits
+than two bf16 values hold.
+
+Whole numbers throughout, small enough that every sum is exact in fp32 in any
+order: finite results are compared bit for bit."""
+import math
+
+import pytest
+import torch
+
+from gpu_helpers import say
+from paper_2105_13480_amd import routed
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": (torch.float32, torch.float32), "bf16": (torch.bfloat16, torch.float32),
+         "bf16_obf16": (torch.bfloat16, torch.bfloat16)}
+
+# rows, features in and out, adapters, ranks: rows as they come (100 rows), and in the
+# order of their adapters by small tiles (whole units of ranks, and not; rows on no
+# 4-byte boundary) and, in bf16, by 256 x 256 tiles
+ADAPTED = [(100, 264, 328, 3, 8), (700, 264, 328, 3, 8), (700, 264, 328, 3, 7), (600, 515, 131, 3, 7),
+           (5000, 1032, 2048, 3, 16)]
+
+
+def _whole(gen, lo, hi, *shape):
+    return torch.randint(lo, hi + 1, shape, generator=gen).float()
+
+
+def _adapt(In, Ker, A, B, ids, to, scales=None):
+    out = torch.full((In.shape[0], Ker.shape[0]), math.nan, dtype=to, device="cuda")
+    i, k, a, b = In.cuda(), Ker.cuda(), A.cuda(), B.cuda()
+    ws = routed.adapt_workspace(i, k, a, out)
+    ws.fill_(0xff)  # NaN in every type
+    routed.adapt_fwd(i, k, a, b, ids.cuda(), out, None if scales is None else scales.cuda(), ws)
+    return out.cpu()
+
+
+@pytest.mark.parametrize("mode", TYPES)
+@pytest.mark.parametrize("case", ADAPTED, ids=str)
+def test_low_rank_factor_in_full(case, mode):
+    """The inner sum has up to 23 bits and the projection takes all but a few of
+    them away again: what is left shows every bit that was not kept."""
+    say(f"[factor] {case} {mode}")
+    Nt, Nc, Nk, Na, Nl = case
+    ti, to = TYPES[mode]
+    gen = torch.Generator().manual_seed(Nt + Nl)
+    In, A = _whole(gen, 0, 255, Nt, Nc), _whole(gen, 0, 31, 1, Nl, Nc)
+    assert 255 * 32 * Nc < 1 << 24
+    r, c = torch.arange(Nk) % Nl, torch.randint(0, Nc, (Nk,), generator=gen)
+    Ker = -A[0][r]
+    Ker[torch.arange(Nk), c] += 1  # Out: one value of In
+    B = torch.zeros(Na, Nk, Nl)
+    B[:, torch.arange(Nk), r] = 1
+    ids = torch.randint(-1, Na, (Nt,), generator=gen).int()
+    assert float((In @ A[0].t()).max()) > 1 << 18  # more than 17 bits
+    want = torch.where((ids >= 0)[:, None], In[:, c], In @ Ker.t())
+    got = _adapt(In.to(ti), Ker.to(ti), A.expand(Na, Nl, Nc).contiguous().to(ti), B.to(ti), ids, to)
+    assert torch.equal(got, want.to(to))
