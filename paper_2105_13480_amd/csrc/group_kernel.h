@@ -595,6 +595,21 @@ __device__ __forceinline__ float bf16_part(float h, int part) {
   return v;
 }
 
+// B's values as the later parts of H meet them (bf16): infinities and
+// NaN are replaced by the type's largest value.  A later part may be zero, and
+// zero times infinity would be NaN; the first part, which is zero only where H
+// is, gives what is due.  Finite values stay, and so does all of a first part's.
+__device__ __forceinline__ u32x4_t met_by_part(u32x4_t b, bool later) {
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  const u16x2_t most = __builtin_bit_cast(u16x2_t, later ? 0x7f7f7f7fu : 0x7fff7fffu);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u16x2_t size = __builtin_bit_cast(u16x2_t, b[i] & 0x7fff7fffu);
+    b[i] = (b[i] & 0x80008000u) | __builtin_bit_cast(uint32_t, __builtin_elementwise_min(size, most));
+  }
+  return b;
+}
+
 // A workgroup's tile: its operands and result from the tile's (and, for the
 // gradient of Ker, the group's) start.
 template <typename T, typename TO> struct Tile {
@@ -829,6 +844,13 @@ __device__ __forceinline__ void low_rank(const GroupArgs& a, const AdaptArgs& ad
             }
           }
           __builtin_amdgcn_sched_barrier(0);
+          if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s)
+#pragma unroll
+              for (int i = 0; i < IB; ++i)
+                xf[s][i] = met_by_part(xf[s][i], k0 + s * STEP + CE * G >= ad.nlp);
+          }
 #pragma unroll
           for (int j = 0; j < JB; ++j)
 #pragma unroll

@@ -197,6 +197,14 @@ __device__ __forceinline__ void pipe_low_rank(const GroupArgs& a, const AdaptArg
         for (int hm = 0; hm < 2; ++hm) {
           u32x4_t xf[4][2];
           X.template read<par.value>((hm ? kX1 : kX0) * kPipeHalf * 16, xf);
+          const int k = k0 + 64 * par.value;
+          if (k + 64 > ad.nlp) {  // some of it meets later parts
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                xf[i][ks] = met_by_part(xf[i][ks], k + 32 * ks + 8 * (lane >> 4) >= ad.nlp);
+          }
 #pragma unroll
           for (int hn = 0; hn < 2; ++hn) {
             const int n0 = hn * 128 + wn * 32;  // this wave's rows of the half

@@ -1,5 +1,5 @@
 """Values that the routed contractions must keep: a low-rank factor of more bits
-than two bf16 values hold.
+than two bf16 values hold, and infinities that meet its parts.
 
 Whole numbers throughout, small enough that every sum is exact in fp32 in any
 order: finite results are compared bit for bit."""
@@ -15,6 +15,7 @@ pytestmark = pytest.mark.gpu
 
 TYPES = {"f32": (torch.float32, torch.float32), "bf16": (torch.bfloat16, torch.float32),
          "bf16_obf16": (torch.bfloat16, torch.bfloat16)}
+INF = math.inf
 
 # rows, features in and out, adapters, ranks: rows as they come (100 rows), and in the
 # order of their adapters by small tiles (whole units of ranks, and not; rows on no
@@ -57,3 +58,41 @@ def test_low_rank_factor_in_full(case, mode):
     want = torch.where((ids >= 0)[:, None], In[:, c], In @ Ker.t())
     got = _adapt(In.to(ti), Ker.to(ti), A.expand(Na, Nl, Nc).contiguous().to(ti), B.to(ti), ids, to)
     assert torch.equal(got, want.to(to))
+
+
+def _products(x, y):
+    """x y^T in 64 bits, infinities and NaN as each product gives them."""
+    return torch.cat([(t[:, None] * y[None]).sum(2) for t in x.split(32)]) if len(x) else x @ y.t()
+
+
+def _same(got, want):
+    """Bit for bit, NaN where NaN is due."""
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got, nan=0.0, posinf=INF, neginf=-INF),
+                       torch.nan_to_num(want, nan=0.0, posinf=INF, neginf=-INF))
+
+
+@pytest.mark.parametrize("mode", TYPES)
+@pytest.mark.parametrize("case", ADAPTED, ids=str)
+def test_adapters_of_infinite_weights(case, mode):
+    """An infinite B times a finite factor other than zero is infinite, times
+    zero NaN; an infinite factor is as the definition has it.  However many rows
+    the call has."""
+    say(f"[infinite] {case} {mode}")
+    Nt, Nc, Nk, Na, Nl = case
+    ti, to = TYPES[mode]
+    gen = torch.Generator().manual_seed(Nt * 3 + Nl)
+    In, Ker = _whole(gen, -2, 2, Nt, Nc), _whole(gen, -2, 2, Nk, Nc)
+    A, B = _whole(gen, -1, 1, Na, Nl, Nc), _whole(gen, -1, 1, Na, Nk, Nl)
+    B[0, 5, 2], B[0, 6, 0], B[0, 7, 1] = INF, -INF, math.nan
+    B[0, Nk - 1, 3], B[0, Nk - 1, 4] = INF, -INF
+    A[1, 3, 0] = INF      # the factor is infinite, or NaN where In[:, 0] is zero
+    B[1, 9, 3] = INF
+    B[1, 10] = 0
+    ids = torch.randint(-1, Na, (Nt,), generator=gen).int()
+    want = In.double() @ Ker.double().t()
+    for a in range(Na):
+        t = torch.nonzero(ids == a).reshape(-1)
+        want[t] += _products(_products(In[t].double(), A[a].double()), B[a].double())
+    got = _adapt(In.to(ti), Ker.to(ti), A.to(ti), B.to(ti), ids, to)
+    _same(got.double(), want.float().to(to).double())
