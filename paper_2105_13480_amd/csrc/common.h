@@ -74,6 +74,19 @@ __host__ __device__ __forceinline__ uint32_t last_index(int64_t elems_from_row) 
   return elems_from_row > 0x7fffffffLL ? 0x7fffffffu : (uint32_t)(elems_from_row - 1);
 }
 
+// Thread `thread` of workgroup `block` (256 threads) of a launch over `rows` rows
+// of `per` units each, row by row: its row and unit; false past the last.
+// Unsigned: a launch may have 2^31 threads and more, but fewer than 2^32.
+__host__ __device__ __forceinline__ bool unit_of_thread(uint32_t block, uint32_t thread, int rows,
+                                                        int per, int* row, int* unit) {
+  const uint32_t i = block * 256u + thread;
+  if (i >= (uint32_t)rows * (uint32_t)per) return false;
+  *row = (int)(i / (uint32_t)per);
+  *unit = (int)(i - (uint32_t)*row * (uint32_t)per);
+  return true;
+}
+constexpr int64_t kMostThreads = 0xffffffffLL;  // of a launch
+
 // The hardware hands consecutive workgroup ids to the 8 XCDs round-robin
 // (id % 8).  Renumber so that each XCD receives one contiguous run of
 // logical tiles: tiles that share input data (the k-tiles of one pixel tile)

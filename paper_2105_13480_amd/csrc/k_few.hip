@@ -318,10 +318,9 @@ __global__ __launch_bounds__(64 * kSumWaves) void adapt_few_sums(GroupArgs a, Ad
 // part in fp32; a thread has four features of a row.
 template <typename T, typename TO, int KS, int KH>
 __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) {
-  const int per = (a.M + 3) / 4;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= per * a.N) return;
-  const int n = i / per, m = 4 * (i - n * per);
+  int n, u;
+  if (!unit_of_thread(blockIdx.x, threadIdx.x, a.N, (a.M + 3) / 4, &n, &u)) return;
+  const int m = 4 * u;
   const int left = a.M - 1 - m;  // features after the first
   f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 
+#include "common.h"
 #include "routed.h"
 
 using namespace cnnlib;
@@ -386,6 +387,9 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     ad.A = A; ad.B = B; ad.ids = Ids; ad.scales = Scales;
     ad.Na = (int32_t)Na; ad.Nl = (int32_t)Nl;
     if (adapt_few(Nt, Nc, Nk, adapt_few_ring(Ker, In, Nc, es))) {
+      if (Nt * ((Nk + 3) / 4) + 255 > kMostThreads)
+        return fail(CNN_E_OVERFLOW, "Nt = %lld rows of Nk = %lld features are more threads than a launch holds",
+                    (long long)Nt, (long long)Nk);
       ad.H = (float*)p;
       ad.part = (float*)(p + w.few_h);
       return launched(launch_adapt_few(a, ad, dtype, (hipStream_t)stream));

@@ -1,0 +1,36 @@
+"""Sizes of the routed contractions past 32 bits, on a machine without a GPU: the
+index arithmetic of their kernels is compiled for the host and checked there, and
+calls that no launch holds are refused before any HIP call (the addresses are
+never read)."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2105_13480_amd import cnn
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+F32, BF16, OBF16 = cnn.CNN_F32, cnn.CNN_BF16, cnn.CNN_BF16_OBF16
+OVERFLOW = -4
+P = [i << 58 for i in range(1, 12)]  # addresses far from each other
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
+def test_threads_past_31_bits(tmp_path):
+    exe = str(tmp_path / "check")
+    res = subprocess.run([HIPCC, "-O2", "-std=c++17", "-x", "hip", "--offload-arch=gfx950",
+                          "-I", os.path.join(ROOT, "paper_2105_13480_amd", "csrc"),
+                          os.path.join(ROOT, "tests", "routed_host", "check_unit_of_thread.cpp"), "-o", exe],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-4000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "bad 0" in run.stdout, run.stdout + run.stderr
+
+
+def test_adapted_rows_past_a_launch():
+    """Few rows of so many features that the last launch would have 2^32 threads."""
+    for Nt, Nk in ((352, 48806447), (17, 1011000000), (64, 1 << 28)):
+        assert Nt * ((Nk + 3) // 4) >= 1 << 32
+        assert cnn.lib().cnn_adapt_fwd(*P[:7], Nt, 8, Nk, 2, 4, BF16, P[8], 1 << 57, None) == OVERFLOW, (Nt, Nk)
