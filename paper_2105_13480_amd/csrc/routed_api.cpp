@@ -67,6 +67,15 @@ int check_type(int dtype) {
   return CNN_OK;
 }
 
+// a b c of sizes >= 0, 2^62 where that or more is due: a product that wrapped
+// would pass for a small one.
+int64_t product(int64_t a, int64_t b, int64_t c) {
+  constexpr int64_t most = 1LL << 62;
+  int64_t r;
+  if (!a || !b || !c) return 0;
+  return __builtin_mul_overflow(a, b, &r) || __builtin_mul_overflow(r, c, &r) || r > most ? most : r;
+}
+
 // A tensor argument: NULL is allowed where it holds no element.
 struct Buf {
   const char* name;
@@ -288,7 +297,7 @@ int cnn_group_fwd(const void* In, const void* Ker, void* Out, const int32_t* Off
     if ((st = check_group(Nt, Np, Ng, Nc, Nk, Rows != nullptr)) || (st = check_type(dtype)) ||
         (st = check_tiles(Np, Ng, Nk)))
       return st;
-    const Buf in[] = {{"In", In, Nt * Nc, in_bytes(dtype)}, {"Ker", Ker, Ng * Nk * Nc, in_bytes(dtype)},
+    const Buf in[] = {{"In", In, Nt * Nc, in_bytes(dtype)}, {"Ker", Ker, product(Ng, Nk, Nc), in_bytes(dtype)},
                       {"Offsets", Offsets, Ng + 1, 4}, {"Rows", Rows, Rows ? Np : 0, 4}};
     const Buf out[] = {{"Out", Out, Np * Nk, out_bytes(dtype)}};
     if ((st = check_bufs(in, out))) return st;
@@ -311,7 +320,7 @@ int cnn_group_bwd_in(const void* dOut, const void* Ker, void* dIn, const int32_t
     if ((st = check_group(Np, Np, Ng, Nc, Nk, false)) || (st = check_type(dtype)) ||
         (st = check_tiles(Np, Ng, Nc)))
       return st;
-    const Buf in[] = {{"dOut", dOut, Np * Nk, in_bytes(dtype)}, {"Ker", Ker, Ng * Nk * Nc, in_bytes(dtype)},
+    const Buf in[] = {{"dOut", dOut, Np * Nk, in_bytes(dtype)}, {"Ker", Ker, product(Ng, Nk, Nc), in_bytes(dtype)},
                       {"Offsets", Offsets, Ng + 1, 4}};
     const Buf out[] = {{"dIn", dIn, Np * Nc, out_bytes(dtype)}};
     if ((st = check_bufs(in, out))) return st;
@@ -333,11 +342,11 @@ int cnn_group_bwd_ker(const void* dOut, const void* In, void* dKer, const int32_
   return guarded([&] {
     int st;
     if ((st = check_group(Nt, Np, Ng, Nc, Nk, Rows != nullptr)) || (st = check_type(dtype)) ||
-        (st = check_grid(Ng * ((Nk + 63) / 64) * ((Nc + 63) / 64))))
+        (st = check_grid(product(Ng, (Nk + 63) / 64, (Nc + 63) / 64))))
       return st;
     const Buf in[] = {{"dOut", dOut, Np * Nk, in_bytes(dtype)}, {"In", In, Nt * Nc, in_bytes(dtype)},
                       {"Offsets", Offsets, Ng + 1, 4}, {"Rows", Rows, Rows ? Np : 0, 4}};
-    const Buf out[] = {{"dKer", dKer, Ng * Nk * Nc, out_bytes(dtype)}};
+    const Buf out[] = {{"dKer", dKer, product(Ng, Nk, Nc), out_bytes(dtype)}};
     if ((st = check_bufs(in, out))) return st;
     GroupArgs a = {};
     a.X = In; a.Y = dOut; a.D = dKer;
@@ -371,8 +380,8 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
       return st;
     const AdaptWs w = adapt_ws(Nt, Nc, Nk, Na, Nl);
     const int es = in_bytes(dtype);
-    const Buf in[] = {{"In", In, Nt * Nc, es}, {"Ker", Ker, Nk * Nc, es}, {"A", A, Na * Nl * Nc, es},
-                      {"B", B, Na * Nk * Nl, es}, {"Ids", Ids, Nt, 4},
+    const Buf in[] = {{"In", In, Nt * Nc, es}, {"Ker", Ker, Nk * Nc, es}, {"A", A, product(Na, Nl, Nc), es},
+                      {"B", B, product(Na, Nk, Nl), es}, {"Ids", Ids, Nt, 4},
                       {"Scales", Scales, Scales ? Na : 0, 4}};
     const Buf out[] = {{"Out", Out, Nt * Nk, out_bytes(dtype)}, {"workspace", workspace, w.total, 1}};
     if ((st = check_ws(workspace, ws_bytes, w.total)) || (st = check_bufs(in, out))) return st;

@@ -34,3 +34,15 @@ def test_adapted_rows_past_a_launch():
     for Nt, Nk in ((352, 48806447), (17, 1011000000), (64, 1 << 28)):
         assert Nt * ((Nk + 3) // 4) >= 1 << 32
         assert cnn.lib().cnn_adapt_fwd(*P[:7], Nt, 8, Nk, 2, 4, BF16, P[8], 1 << 57, None) == OVERFLOW, (Nt, Nk)
+
+
+def test_products_of_sizes_that_wrap():
+    """Ker of 2^64 elements and more, which modulo 2^64 are none or few, and as many
+    tiles: refused, also where Ker is NULL as only an empty tensor may be."""
+    L = cnn.lib()
+    for Ng, Nk, Nc in ((64, 1 << 29, 1 << 29), (256, 1 << 29, 1 << 27), (65535, (1 << 30) - 1, (1 << 30) - 1),
+                       (32768, (1 << 30) - 1, (1 << 30) - 1)):
+        for ker in (P[1], None):
+            assert L.cnn_group_fwd(P[0], ker, P[2], P[3], P[4], 8, 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
+            assert L.cnn_group_bwd_in(P[0], ker, P[2], P[3], 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
+            assert L.cnn_group_bwd_ker(P[0], P[1], ker, P[3], P[4], 8, 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
