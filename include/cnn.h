@@ -463,7 +463,8 @@ int cnn_hbm_bytes(const cnn_plan_t* plan, int64_t xcds, int64_t l2_bytes, double
  * result's (CNN_BF16: bf16 operands, fp32 result); integers are int32, weights
  * and their gradients fp32.  Buffers may start at any element (fp32 at 4
  * bytes); 16-byte aligned rows are fastest.  Nt = 0 or Np = 0 is a call without
- * rows (tensors without elements may be NULL).  Results must not overlap any
+ * rows (tensors without elements may be NULL).  Sizes that need a launch of 2^32
+ * threads or more are refused (CNN_E_OVERFLOW).  Results must not overlap any
  * other argument (CNN_E_ALIAS).  Every sum has a fixed order: results do not
  * vary from call to call.
  *

@@ -85,7 +85,12 @@ __host__ __device__ __forceinline__ bool unit_of_thread(uint32_t block, uint32_t
   *unit = (int)(i - (uint32_t)*row * (uint32_t)per);
   return true;
 }
-constexpr int64_t kMostThreads = 0xffffffffLL;  // of a launch
+// hipErrorInvalidConfiguration where a grid has more threads than a launch holds:
+// the routed contractions' launchers look before they launch anything.
+constexpr int64_t kMostThreads = 0xffffffffLL;
+inline hipError_t grid_fits(int64_t blocks, int threads) {
+  return blocks * threads > kMostThreads ? hipErrorInvalidConfiguration : hipSuccess;
+}
 
 // The hardware hands consecutive workgroup ids to the 8 XCDs round-robin
 // (id % 8).  Renumber so that each XCD receives one contiguous run of

@@ -1051,15 +1051,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
 
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE = true>
 hipError_t launch_tiles(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
-                        hipStream_t stream) {
+                        Launch to) {
   auto* const k = group_tiles<T, TO, MODE, TM, TN, WM, WN, DEPTH, WHOLE>;
+  const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
+  const hipError_t fit = grid_fits(grid, 64 * WM * WN);
+  if (fit != hipSuccess || to.dry) return fit;
   const int lds = (DEPTH > 0 ? DEPTH : 2) * 8 * (TM + TN) * 16;
   if (lds > 64 * 1024) {
     const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
     if (e != hipSuccess) return e;
   }
-  const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
-  k<<<dim3((uint32_t)grid), dim3(64 * WM * WN), lds, stream>>>(a, ad, band);
+  k<<<dim3((uint32_t)grid), dim3(64 * WM * WN), lds, to.stream>>>(a, ad, band);
   return hipGetLastError();
 }
 

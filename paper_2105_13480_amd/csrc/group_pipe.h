@@ -413,13 +413,15 @@ inline bool pipe_fits(const GroupArgs& a, int mode) {
 
 template <typename TO, int MODE>
 hipError_t launch_pipe(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
-                       hipStream_t stream) {
+                       Launch to) {
   auto* const k = group_pipe<TO, MODE>;
+  const int64_t grid = row_tiles * ((a.M + 255) / 256);
+  const hipError_t fit = grid_fits(grid, 512);
+  if (fit != hipSuccess || to.dry) return fit;
   const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
   if (e != hipSuccess) return e;
-  const int64_t grid = row_tiles * ((a.M + 255) / 256);
   const int lds = kPipeLds + (MODE == kBwdKer && a.rows ? (kPipeRows + 192) * 4 : 0);
-  k<<<dim3((uint32_t)grid), dim3(512), lds, stream>>>(a, ad, band);
+  k<<<dim3((uint32_t)grid), dim3(512), lds, to.stream>>>(a, ad, band);
   return hipGetLastError();
 }
 

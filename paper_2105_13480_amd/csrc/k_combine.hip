@@ -145,8 +145,10 @@ hipError_t launch_fwd(const void* In, const int32_t* slots, const float* gates, 
                       int64_t Nt, int Kt, int64_t Np, int64_t Nk, hipStream_t stream) {
   constexpr int V = 16 / (int)sizeof(T);
   const int upr = (int)((Nk + V - 1) / V);
-  const int64_t units = Nt * upr;
-  combine_rows<T, TO, V><<<dim3((uint32_t)((units + 255) / 256)), dim3(256), 0, stream>>>(
+  const int64_t units = Nt * upr, blocks = (units + 255) / 256;
+  const hipError_t e = grid_fits(blocks, 256);
+  if (e != hipSuccess) return e;
+  combine_rows<T, TO, V><<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>(
       reinterpret_cast<const T*>(In), slots, gates, reinterpret_cast<TO*>(Out), units, upr, Kt, Np, Nk);
   return hipGetLastError();
 }
@@ -160,6 +162,8 @@ hipError_t launch_bwd(const void* dOut, const void* In, const int32_t* slots, co
   const int w = Nk <= 64 * V ? 1 : Nk <= 128 * V ? 2 : 4;
   const int64_t place_blocks = (Np * w + 3) / 4, clear_blocks = dGates ? (Nt * Kt + 255) / 256 : 0;
   if (!place_blocks && !clear_blocks) return hipSuccess;
+  const hipError_t e = grid_fits(place_blocks + clear_blocks, 256);
+  if (e != hipSuccess) return e;
   auto* const k = w == 1 ? combine_rows_bwd<T, TO, V, 1>
                   : w == 2 ? combine_rows_bwd<T, TO, V, 2> : combine_rows_bwd<T, TO, V, 4>;
   k<<<dim3((uint32_t)(place_blocks + clear_blocks)), dim3(256), 0, stream>>>(

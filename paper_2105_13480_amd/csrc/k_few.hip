@@ -380,8 +380,10 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
 template <typename T, typename TO, int FB, int RB, int NW>
 hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
   const int64_t mt = (a.M + 16 * FB - 1) / (16 * FB), parts = a.Ng + 1 < a.N ? a.Ng + 1 : a.N;
-  const dim3 grid((uint32_t)((a.N / (16 * RB) + parts) * mt)), block(64 * NW);
-  group_few<T, TO, FB, RB, NW><<<grid, block, 0, stream>>>(a);
+  const int64_t blocks = (a.N / (16 * RB) + parts) * mt;
+  const hipError_t e = grid_fits(blocks, 64 * NW);
+  if (e != hipSuccess) return e;
+  group_few<T, TO, FB, RB, NW><<<dim3((uint32_t)blocks), dim3(64 * NW), 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -418,6 +420,10 @@ hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream
   f.kslice = ((a.K + f.ks - 1) / f.ks + RUN - 1) / RUN * RUN;
   f.q = ad.Na < 16 ? ad.Na : 16;
   f.downs = (a.N + 15) / 16 * f.q * f.kh;
+  // both launches before the first
+  hipError_t e = grid_fits(f.downs + (int64_t)f.blocks * f.rtiles * f.ks, 64 * kSumWaves);
+  if (e == hipSuccess) e = grid_fits(((int64_t)a.N * ((a.M + 3) / 4) + 255) / 256, 256);
+  if (e != hipSuccess) return e;
   if (a.N <= 32) {
     if (ad.Nl <= 16) launch_sums<T, 1, 32>(a, ad, f, stream);
     else launch_sums<T, 4, 32>(a, ad, f, stream);
@@ -425,7 +431,7 @@ hipError_t launch_adapt_typed(const GroupArgs& a, const AdaptArgs& ad, hipStream
     if (ad.Nl <= 16) launch_sums<T, 1, 64>(a, ad, f, stream);
     else launch_sums<T, 4, 64>(a, ad, f, stream);
   }
-  const hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   switch (f.ks) {
     case 1: launch_out<T, TO, 1>(a, ad, f, stream); break;

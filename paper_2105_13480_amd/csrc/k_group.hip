@@ -92,16 +92,16 @@ template <typename T, int MODE> int pick_tile(const GroupArgs& a, int first, boo
 // of 2048 x 2048 9.4 us, 11.1 by three) and in fp32 (3002 rows of 6 groups of
 // 771 x 515 33.5 and 34.6).
 template <typename T, typename TO, int MODE, int TM, int TN, bool WHOLE>
-hipError_t launch_small(const GroupArgs& a, const AdaptArgs& ad, bool dma, bool crowded, hipStream_t stream) {
+hipError_t launch_small(const GroupArgs& a, const AdaptArgs& ad, bool dma, bool crowded, Launch to) {
   const int64_t rt = row_tiles_of<MODE>(a, TN);
-  if (!dma) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 0, WHOLE>(a, ad, rt, 16, stream);
+  if (!dma) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 0, WHOLE>(a, ad, rt, 16, to);
   if constexpr (sizeof(T) == 2 && (MODE == kFwd || MODE == kAdapt))
-    if (crowded) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 3, WHOLE>(a, ad, rt, 16, stream);
-  return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 4, WHOLE>(a, ad, rt, 16, stream);
+    if (crowded) return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 3, WHOLE>(a, ad, rt, 16, to);
+  return launch_tiles<T, TO, MODE, TM, TN, 2, 2, 4, WHOLE>(a, ad, rt, 16, to);
 }
 
 template <typename T, typename TO, int MODE, bool WHOLE>
-hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, Launch to) {
   constexpr bool XKC = MODE == kFwd || MODE >= kAdapt, YKC = MODE != kBwdKer;
   const bool dma = copies_ok(a.X, a.ldx, a.M, XKC, sizeof(T)) && copies_ok(a.Y, a.ldy, a.N, YKC, sizeof(T));
   const bool pipe = sizeof(T) == 2 && WHOLE && dma && (MODE == kBwdKer || a.K % 8 == 0) && pipe_fits(a, MODE) &&
@@ -113,33 +113,33 @@ hipError_t launch_sized(const GroupArgs& a, const AdaptArgs& ad, hipStream_t str
   bool crowded = false;
   const int pick = pick_tile<T, MODE>(a, first, &crowded);
   if constexpr (sizeof(T) == 2 && WHOLE)
-    if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, stream);
+    if (pick == 0) return launch_pipe<TO, MODE>(a, ad, row_tiles_of<MODE>(a, 256), 4, to);
   if (pick == 1) {
     const int64_t rt = row_tiles_of<MODE>(a, 128);
     if constexpr (sizeof(T) == 2)
-      if (!dma) return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, stream);
-    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, stream);
+      if (!dma) return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 0, WHOLE>(a, ad, rt, 8, to);
+    return launch_tiles<T, TO, MODE, 128, 128, 2, 2, 2, WHOLE>(a, ad, rt, 8, to);
   }
   if constexpr (MODE != kBwdKer) {
-    if (pick == 4) return launch_small<T, TO, MODE, 32, 32, WHOLE>(a, ad, dma, crowded, stream);
-    if (pick == 3) return launch_small<T, TO, MODE, 64, 32, WHOLE>(a, ad, dma, crowded, stream);
+    if (pick == 4) return launch_small<T, TO, MODE, 32, 32, WHOLE>(a, ad, dma, crowded, to);
+    if (pick == 3) return launch_small<T, TO, MODE, 64, 32, WHOLE>(a, ad, dma, crowded, to);
   }
-  return launch_small<T, TO, MODE, 64, 64, WHOLE>(a, ad, dma, crowded, stream);
+  return launch_small<T, TO, MODE, 64, 64, WHOLE>(a, ad, dma, crowded, to);
 }
 
 template <typename T, typename TO, int MODE>
-hipError_t launch_ranks(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+hipError_t launch_ranks(const GroupArgs& a, const AdaptArgs& ad, Launch to) {
   if constexpr (MODE == kAdapt)
-    if (ad.nlp != ad.Nl) return launch_sized<T, TO, MODE, false>(a, ad, stream);
-  return launch_sized<T, TO, MODE, true>(a, ad, stream);
+    if (ad.nlp != ad.Nl) return launch_sized<T, TO, MODE, false>(a, ad, to);
+  return launch_sized<T, TO, MODE, true>(a, ad, to);
 }
 
 template <int MODE>
-hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
+hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, Launch to) {
   switch (dtype) {
-    case CNN_F32: return launch_ranks<float, float, MODE>(a, ad, stream);
-    case CNN_BF16: return launch_ranks<bf16_t, float, MODE>(a, ad, stream);
-    default: return launch_ranks<bf16_t, bf16_t, MODE>(a, ad, stream);
+    case CNN_F32: return launch_ranks<float, float, MODE>(a, ad, to);
+    case CNN_BF16: return launch_ranks<bf16_t, float, MODE>(a, ad, to);
+    default: return launch_ranks<bf16_t, bf16_t, MODE>(a, ad, to);
   }
 }
 
@@ -147,20 +147,20 @@ hipError_t launch_typed(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipS
 
 hipError_t launch_group_fwd(const GroupArgs& a, int dtype, hipStream_t stream) {
   if (group_few_fits(a, dtype)) return launch_group_few(a, dtype, stream);
-  return launch_typed<kFwd>(a, AdaptArgs{}, dtype, stream);
+  return launch_typed<kFwd>(a, AdaptArgs{}, dtype, Launch{stream, false});
 }
 hipError_t launch_group_bwd_in(const GroupArgs& a, int dtype, hipStream_t stream) {
-  return launch_typed<kBwdIn>(a, AdaptArgs{}, dtype, stream);
+  return launch_typed<kBwdIn>(a, AdaptArgs{}, dtype, Launch{stream, false});
 }
 hipError_t launch_group_bwd_ker(const GroupArgs& a, int dtype, hipStream_t stream) {
-  return launch_typed<kBwdKer>(a, AdaptArgs{}, dtype, stream);
+  return launch_typed<kBwdKer>(a, AdaptArgs{}, dtype, Launch{stream, false});
 }
 
 namespace {
 
 // Rows of the low-rank operand: the product grouped by adapter, whose ranks
 // are few: tiles of 64 or 16 ranks by 32 rows.
-template <typename T> hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, hipStream_t stream) {
+template <typename T> hipError_t launch_down(const GroupArgs& a, const AdaptArgs& ad, Launch to) {
   GroupArgs h = a;
   h.X = ad.A;
   h.xgroup = (int64_t)ad.Nl * a.K;
@@ -169,22 +169,22 @@ template <typename T> hipError_t launch_down(const GroupArgs& a, const AdaptArgs
   const int64_t rt = row_tiles_of<kDown>(h, 32);
   const bool dma = copies_ok(h.X, h.ldx, h.M, true, sizeof(T)) && copies_ok(h.Y, h.ldy, h.N, true, sizeof(T));
   if (ad.Nl <= 16)
-    return dma ? launch_tiles<T, T, kDown, 16, 32, 1, 2, 6>(h, ad, rt, 1, stream)
-               : launch_tiles<T, T, kDown, 16, 32, 1, 2, 0>(h, ad, rt, 1, stream);
-  return dma ? launch_tiles<T, T, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, stream)
-             : launch_tiles<T, T, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, stream);
+    return dma ? launch_tiles<T, T, kDown, 16, 32, 1, 2, 6>(h, ad, rt, 1, to)
+               : launch_tiles<T, T, kDown, 16, 32, 1, 2, 0>(h, ad, rt, 1, to);
+  return dma ? launch_tiles<T, T, kDown, 64, 32, 2, 2, 4>(h, ad, rt, 1, to)
+             : launch_tiles<T, T, kDown, 64, 32, 2, 2, 0>(h, ad, rt, 1, to);
 }
 
 }  // namespace
 
-hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream) {
+hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, Launch to) {
   const hipError_t e =
-      dtype == CNN_F32 ? launch_down<float>(a, ad, stream) : launch_down<bf16_t>(a, ad, stream);
+      dtype == CNN_F32 ? launch_down<float>(a, ad, to) : launch_down<bf16_t>(a, ad, to);
   if (e != hipSuccess) return e;
   GroupArgs g = a;
   g.off = nullptr;
   g.Ng = 1;
-  return launch_typed<kAdapt>(g, ad, dtype, stream);
+  return launch_typed<kAdapt>(g, ad, dtype, to);
 }
 
 }  // namespace cnnlib

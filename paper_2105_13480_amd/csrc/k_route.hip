@@ -394,19 +394,14 @@ template <typename T, typename TO>
 hipError_t launch_bwd(const void* logits, const int32_t* choice, const float* gates,
                       const float* dgates, void* dlogits, int64_t Nt, int Ng, int Kt, int over_all,
                       hipStream_t stream) {
-  const dim3 block(256);
   const T* const l = reinterpret_cast<const T*>(logits);
   TO* const d = reinterpret_cast<TO*>(dlogits);
-  if (Ng <= 64) {
-    route_bwd<T, TO, 16, 4><<<dim3((uint32_t)((Nt + 15) / 16)), block, 0, stream>>>(
-        l, choice, gates, dgates, d, Nt, Ng, Kt, over_all);
-  } else if (Ng <= 256) {
-    route_bwd<T, TO, 16, 16><<<dim3((uint32_t)((Nt + 15) / 16)), block, 0, stream>>>(
-        l, choice, gates, dgates, d, Nt, Ng, Kt, over_all);
-  } else {
-    route_bwd<T, TO, 64, 16><<<dim3((uint32_t)((Nt + 3) / 4)), block, 0, stream>>>(
-        l, choice, gates, dgates, d, Nt, Ng, Kt, over_all);
-  }
+  const int rows = Ng <= 256 ? 16 : 4;  // of a workgroup
+  const int64_t blocks = (Nt + rows - 1) / rows;
+  const hipError_t e = grid_fits(blocks, 256);
+  if (e != hipSuccess) return e;
+  auto* const k = Ng <= 64 ? route_bwd<T, TO, 16, 4> : Ng <= 256 ? route_bwd<T, TO, 16, 16> : route_bwd<T, TO, 64, 16>;
+  k<<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>(l, choice, gates, dgates, d, Nt, Ng, Kt, over_all);
   return hipGetLastError();
 }
 

@@ -76,6 +76,12 @@ struct RouteArgs {
   int32_t over_all;     // weights over all allowed experts, not the chosen ones
 };
 
+// Where a launch goes; `dry`: it is only seen whether its grid fits.
+struct Launch {
+  hipStream_t stream;
+  bool dry;
+};
+
 // Rows of an ordering workgroup and the number of workgroups.
 void order_blocks(int64_t Nt, int32_t* chunk, int32_t* nblocks);
 
@@ -105,6 +111,6 @@ bool adapt_few_ring(const void* Ker, const void* In, int64_t Nc, int es);  // ro
 FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk, int es);
 hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 // Rows in the order of their adapters (a.off, a.rows, ad.ids).
-hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
+hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, Launch to);
 
 }  // namespace cnnlib

@@ -6,7 +6,6 @@
 
 #include <algorithm>
 
-#include "common.h"
 #include "routed.h"
 
 using namespace cnnlib;
@@ -25,6 +24,8 @@ int fail(int status, const char* fmt, ...) {
 
 int launched(hipError_t e) {
   if (e == hipSuccess) return CNN_OK;
+  if (e == hipErrorInvalidConfiguration)
+    return fail(CNN_E_OVERFLOW, "more threads than a launch holds");
   return fail(CNN_E_HIP, "kernel launch: %s", hipGetErrorString(e));
 }
 
@@ -396,9 +397,6 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     ad.A = A; ad.B = B; ad.ids = Ids; ad.scales = Scales;
     ad.Na = (int32_t)Na; ad.Nl = (int32_t)Nl;
     if (adapt_few(Nt, Nc, Nk, adapt_few_ring(Ker, In, Nc, es))) {
-      if (Nt * ((Nk + 3) / 4) + 255 > kMostThreads)
-        return fail(CNN_E_OVERFLOW, "Nt = %lld rows of Nk = %lld features are more threads than a launch holds",
-                    (long long)Nt, (long long)Nk);
       ad.H = (float*)p;
       ad.part = (float*)(p + w.few_h);
       return launched(launch_adapt_few(a, ad, dtype, (hipStream_t)stream));
@@ -406,6 +404,7 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     ad.Hp = p;
     ad.nlp = adapt_nlp(Nl, dtype);
     ad.hl = ad.nlp * adapt_parts(dtype);
+    if ((st = launched(launch_adapt(a, ad, dtype, Launch{nullptr, true})))) return st;
     OrderArgs o = {};
     o.key = Ids;
     o.counts = (int32_t*)(p += w.h);
@@ -421,7 +420,7 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
     a.off = o.off;
     a.rows = o.rows;
     ad.ids = o.keys;
-    return launched(launch_adapt(a, ad, dtype, (hipStream_t)stream));
+    return launched(launch_adapt(a, ad, dtype, Launch{(hipStream_t)stream, false}));
   });
 }
 

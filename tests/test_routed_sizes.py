@@ -46,3 +46,22 @@ def test_products_of_sizes_that_wrap():
             assert L.cnn_group_fwd(P[0], ker, P[2], P[3], P[4], 8, 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
             assert L.cnn_group_bwd_in(P[0], ker, P[2], P[3], 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
             assert L.cnn_group_bwd_ker(P[0], P[1], ker, P[3], P[4], 8, 16, Ng, Nc, Nk, BF16, None) == OVERFLOW
+
+
+def test_more_threads_than_a_launch_holds():
+    """2^32 threads: CNN_E_OVERFLOW, not an error of the launch.  The sizes fit the
+    GPU's memory, or each of them its limit."""
+    L, m = cnn.lib(), (1 << 30) - 1
+    assert L.cnn_combine(*P[:4], 1 << 23, 1, 1 << 23, 4096, OBF16, None) == OVERFLOW
+    assert L.cnn_combine(*P[:4], 1 << 24, 1, 1 << 23, 1024, F32, None) == OVERFLOW
+    assert L.cnn_combine_bwd(*P[:7], 1 << 24, 1, 1 << 24, 2048, OBF16, None) == OVERFLOW
+    assert L.cnn_combine_bwd(*P[:7], m, 4, 8, 2048, OBF16, None) == OVERFLOW  # weights' gradients alone
+    assert L.cnn_route_bwd(*P[:5], 1 << 28, 8, 2, F32, 0, None) == OVERFLOW
+    assert L.cnn_route_bwd(*P[:5], 1 << 26, 300, 2, F32, 0, None) == OVERFLOW
+    for dtype in (F32, BF16, OBF16):
+        for Nc in (8, 7):
+            assert L.cnn_group_fwd(*P[:5], m, m, 1, Nc, 16, dtype, None) == OVERFLOW
+            assert L.cnn_group_bwd_in(*P[:4], m, 1, 16, Nc, dtype, None) == OVERFLOW
+            assert L.cnn_adapt_fwd(*P[:7], m, Nc, 16, 2, 4, dtype, P[8], 1 << 57, None) == OVERFLOW
+        assert L.cnn_group_fwd(*P[:5], 65535, 65535, 65535, 1024, 8192, dtype, None) == OVERFLOW
+        assert L.cnn_group_bwd_ker(*P[:5], 65535, 65535, 65535, 5000, 5000, dtype, None) == OVERFLOW
