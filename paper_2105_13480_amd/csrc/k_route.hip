@@ -359,7 +359,7 @@ __global__ __launch_bounds__(256) void route_bwd(const T* logits, const int32_t*
   float d[E];
   bool some = false;
 #pragma unroll
-  for (int i = 0; i < E; ++i) d[i] = -p[i] * inner;
+  for (int i = 0; i < E; ++i) d[i] = p[i] != 0.f ? -p[i] * inner : 0.f;  // inner may be infinite
   for (int j = 0; j < Kt; ++j) {
     const int e = choice[row * Kt + j];
     if (e < 0 || e >= Ng) continue;

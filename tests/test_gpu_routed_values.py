@@ -1,5 +1,6 @@
 """Values that the routed contractions must keep: a low-rank factor of more bits
-than two bf16 values hold, and infinities that meet its parts.
+than two bf16 values hold, infinities that meet its parts, and gradients that are
+not finite.
 
 Whole numbers throughout, small enough that every sum is exact in fp32 in any
 order: finite results are compared bit for bit."""
@@ -96,3 +97,36 @@ def test_adapters_of_infinite_weights(case, mode):
         want[t] += _products(_products(In[t].double(), A[a].double()), B[a].double())
     got = _adapt(In.to(ti), Ker.to(ti), A.to(ti), B.to(ti), ids, to)
     _same(got.double(), want.float().to(to).double())
+
+
+@pytest.mark.parametrize("mode", TYPES)
+@pytest.mark.parametrize("over", ["all", "chosen"])
+@pytest.mark.parametrize("Nt,Ng,Kt", [(5, 6, 2), (40, 200, 4), (17, 700, 8)])
+def test_route_bwd_of_infinite_gradients(Nt, Ng, Kt, over, mode):
+    """A weight's gradient that is not finite reaches neither the experts that are
+    not allowed nor, over the chosen ones, those not chosen: theirs is zero."""
+    say(f"[route_bwd infinite] {Nt} {Ng} {Kt} {over} {mode}")
+    ti, to = TYPES[mode]
+    gen = torch.Generator().manual_seed(Ng)
+    logits = torch.randn((Nt, Ng), generator=gen).to(ti)
+    logits[torch.rand((Nt, Ng), generator=gen) < 0.2] = -INF
+    logits[1, : Ng // 2] = math.nan
+    logits[:3, -2:] = 0.5  # two allowed at least
+    barred = ~(logits.float() > -INF)
+    r = routed.route(logits.cuda(), routed.Routing(Nt, Ng, Kt), over=over)
+    choice = r.choice.cpu().long()
+    dG = torch.randn((Nt, Kt), generator=gen)
+    clean, dirty = (torch.full((Nt, Ng), math.nan, dtype=to, device="cuda") for _ in range(2))
+    routed.route_bwd(logits.cuda(), r.choice, r.gates, dG.cuda(), clean, over=over)
+    dG[0, 0], dG[1, 1], dG[2] = INF, math.nan, -INF
+    routed.route_bwd(logits.cuda(), r.choice, r.gates, dG.cuda(), dirty, over=over)
+    clean, dirty = clean.float().cpu(), dirty.float().cpu()
+    outside = barred
+    if over == "chosen":
+        outside = torch.ones((Nt, Ng), dtype=torch.bool)
+        outside.scatter_(1, choice.clamp(min=0), False)  # every row has a choice
+    for d in (clean, dirty):
+        assert (d[outside] == 0).all()
+        assert not torch.signbit(d[outside]).any()  # not -0 either
+    assert torch.equal(clean[3:], dirty[3:])
+    assert not torch.isfinite(dirty[:3]).all(1).any()
