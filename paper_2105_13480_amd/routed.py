@@ -344,11 +344,22 @@ def adapt_workspace(In, Ker, A, Out):
     return _torch.empty(n.value, dtype=_torch.uint8, device=In.device)
 
 
+def _adapt_own_workspace(In, Ker, A, Out, stream):
+    """One for a single call, of the memory of the stream that the call runs on:
+    it is free for that stream's later work only."""
+    if stream is None:
+        return adapt_workspace(In, Ker, A, Out)
+    raw = _stream(stream)
+    with _torch.cuda.stream(_torch.cuda.ExternalStream(raw) if raw else _torch.cuda.default_stream()):
+        return adapt_workspace(In, Ker, A, Out)
+
+
 def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
     """Out[t] = In[t] Ker^T + scales[a] (In[t] A[a]^T) B[a]^T with a = ids[t]
     (outside [0, Na): no adapter): In [Nt, Nc], Ker [Nk, Nc], A [Na, Nl, Nc],
     B [Na, Nk, Nl], scales [Na] float32 (None: ones).  ws: the tensor that
-    ``adapt_workspace`` gives, kept by the caller."""
+    ``adapt_workspace`` gives, kept by the caller (None: one of its own for
+    this call)."""
     here = _enter()
     Nt, Nc, Nk, Na, Nl = _adapt_dims(In, Ker, A, Out)
     if not (In.get_device() == here == Ker.get_device() == A.get_device() == B.get_device() ==
@@ -366,11 +377,12 @@ def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
         _shape("scales", scales, Na)
         _of(_f32, scales=scales)
     dt = _dtype(Out, In, Ker, A, B)
+    if ws is None:
+        ws = _adapt_own_workspace(In, Ker, A, Out, stream)
     st = (cnn._lib or cnn.lib()).cnn_adapt_fwd(
         In.data_ptr(), Ker.data_ptr(), A.data_ptr(), B.data_ptr(), ids.data_ptr(),
         0 if scales is None else scales.data_ptr(), Out.data_ptr(), Nt, Nc, Nk, Na, Nl, dt,
-        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
-        _raw(stream))
+        ws.data_ptr(), ws.numel() * ws.element_size(), _raw(stream))
     if st:
         _check(st)
     return Out
