@@ -1,5 +1,6 @@
 // The pipelined tile kernel of the grouped products: 256 x 256 results of
-// bf16 operands with 16-byte aligned rows.
+// bf16 operands with rows on 4-byte boundaries, k (or, where it is last, the
+// operand's own index) of whole units of 16 bytes.
 //
 // Eight waves of 128 (m) x 64 (n) results, two on each SIMD.  A stage is 64 of
 // k: 64 KB of LDS in four halves (128 rows of Y, 128 of X, the other 128 of

@@ -1,8 +1,8 @@
-// Products of few rows: grouped products with a few rows a group, and adapted
-// projections of up to a few dozen rows (serving steps).
+// Products of few rows: grouped products with a few rows a group (serving
+// steps), and adapted projections of up to some hundred rows (adapt_few).
 //
-// Such a product is bound by reading Ker once: a workgroup takes 16 FB features
-// by 16 RB rows, its waves share the contraction (wave w takes every NW-th
+// Such a product is bound by reading Ker once: a workgroup takes some 16 features
+// by 16 rows, its waves share the contraction (each of four takes every fourth
 // 256-byte run of k), and both operands go straight from memory to the MFMA
 // registers, no LDS and no barrier until the waves' sums meet: 16 rows of 64
 // bytes a load, four loads a run.  Rows beyond a tile's last read a row that
@@ -123,44 +123,34 @@ __device__ __forceinline__ void clear(f32x4_t (&acc)[FB][RB]) {
     for (int b = 0; b < RB; ++b) acc[f][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 }
 
-template <typename T, typename TO, int FB, int RB, int NW>
-__global__ __launch_bounds__(64 * NW) void group_few(GroupArgs a) {
-  __shared__ f32x4_t red[NW * FB * RB * 64];
+// A tile of 16 features by 16 rows of a group.
+constexpr int kFewWaves = 4;
+
+template <typename T, typename TO>
+__global__ __launch_bounds__(64 * kFewWaves) void group_few(GroupArgs a) {
+  constexpr int NW = kFewWaves;
+  __shared__ f32x4_t red[NW * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int MT = (a.M + 16 * FB - 1) / (16 * FB);
   RowTile t;
-  if (!find_tile<16 * RB>(a.off, a.Ng, a.N, MT, blockIdx.x, 1, &t)) return;
-  const int l16 = lane & 15, G = lane >> 4;
-  const int m0 = 16 * FB * t.mt, n_valid = min(t.n1 - t.n0, 16 * RB);
+  if (!find_tile<16>(a.off, a.Ng, a.N, (a.M + 15) / 16, blockIdx.x, 1, &t)) return;
+  const int l16 = lane & 15;
+  const int m0 = 16 * t.mt, n_valid = min(t.n1 - t.n0, 16);
   const bool live = t.g < a.Ng;
 
-  const T* const X = reinterpret_cast<const T*>(a.X) + (live ? t.g : 0) * a.xgroup;
-  const T* x[FB];
-  feature_rows<T, FB>(X, a.ldx, m0, a.M, l16, x);
-  const T* y[RB];
-  uint32_t none = 0;  // blocks whose row of this lane is no row of In
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    int64_t r = t.n0 + min(16 * b + l16, n_valid - 1);
-    if (a.rows) r = a.rows[r];
-    if (r < 0 || r >= a.Nsrc) {
-      none |= 1u << b;
-      r = 0;
-    }
-    y[b] = reinterpret_cast<const T*>(a.Y) + r * a.ldy;
-  }
-  f32x4_t acc[FB][RB];
+  const T* x[1];
+  feature_rows<T, 1>(reinterpret_cast<const T*>(a.X) + (live ? t.g : 0) * a.xgroup, a.ldx, m0, a.M, l16, x);
+  int64_t r = t.n0 + min(l16, n_valid - 1);
+  if (a.rows) r = a.rows[r];
+  const bool there = r >= 0 && r < a.Nsrc;  // this lane's row is one of In
+  const T* const y[1] = {reinterpret_cast<const T*>(a.Y) + (there ? r : 0) * a.ldy};
+  f32x4_t acc[1][1];
   clear(acc);
-  if (live) few_rows_dot<T, FB, RB>(x, y, a.K, wave, NW, lane, acc);
+  if (live) few_rows_dot<T, 1, 1>(x, y, a.K, wave, NW, lane, acc);
   leave_sums(red, acc, wave, NW, lane);
-
-  for (int blk = wave; blk < FB * RB; blk += NW) {
-    const int b = blk % RB, n = 16 * b + l16, m = m0 + 16 * (blk / RB) + 4 * G;
-    if (n >= n_valid) continue;
-    f32x4_t s = block_sum(red, blk, NW, lane);
-    if (!live || (none >> b & 1)) s = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    store4(reinterpret_cast<TO*>(a.D) + (t.n0 + n) * a.ldd, m, a.M, s);
-  }
+  if (wave != 0 || l16 >= n_valid) return;
+  f32x4_t s = block_sum(red, 0, NW, lane);
+  if (!live || !there) s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  store4(reinterpret_cast<TO*>(a.D) + (t.n0 + l16) * a.ldd, m0 + 4 * (lane >> 4), a.M, s);
 }
 
 // Few adapted rows, first launch: partial sums of both products that read In.
@@ -377,18 +367,13 @@ __global__ __launch_bounds__(256) void adapt_few_out(GroupArgs a, AdaptArgs ad) 
   store4(reinterpret_cast<TO*>(a.D) + (int64_t)n * a.ldd, m, a.M, sum);
 }
 
-template <typename T, typename TO, int FB, int RB, int NW>
-hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
-  const int64_t mt = (a.M + 16 * FB - 1) / (16 * FB), parts = a.Ng + 1 < a.N ? a.Ng + 1 : a.N;
-  const int64_t blocks = (a.N / (16 * RB) + parts) * mt;
-  const hipError_t e = grid_fits(blocks, 64 * NW);
+template <typename T, typename TO> hipError_t launch_few(const GroupArgs& a, hipStream_t stream) {
+  const int64_t mt = (a.M + 15) / 16, parts = a.Ng + 1 < a.N ? a.Ng + 1 : a.N;
+  const int64_t blocks = (a.N / 16 + parts) * mt;
+  const hipError_t e = grid_fits(blocks, 64 * kFewWaves);
   if (e != hipSuccess) return e;
-  group_few<T, TO, FB, RB, NW><<<dim3((uint32_t)blocks), dim3(64 * NW), 0, stream>>>(a);
+  group_few<T, TO><<<dim3((uint32_t)blocks), dim3(64 * kFewWaves), 0, stream>>>(a);
   return hipGetLastError();
-}
-
-template <typename T, typename TO> hipError_t launch_few_typed(const GroupArgs& a, hipStream_t stream) {
-  return launch_few<T, TO, 1, 1, 4>(a, stream);
 }
 
 template <typename T, int DF, int TN>
@@ -456,9 +441,9 @@ bool group_few_fits(const GroupArgs& a, int dtype) {
 
 hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
   switch (dtype) {
-    case CNN_F32: return launch_few_typed<float, float>(a, stream);
-    case CNN_BF16: return launch_few_typed<bf16_t, float>(a, stream);
-    default: return launch_few_typed<bf16_t, bf16_t>(a, stream);
+    case CNN_F32: return launch_few<float, float>(a, stream);
+    case CNN_BF16: return launch_few<bf16_t, float>(a, stream);
+    default: return launch_few<bf16_t, bf16_t>(a, stream);
   }
 }
 

@@ -216,7 +216,7 @@ int cnn_route(const void* Logits, int32_t* Choice, float* Gates, int32_t* Offset
     const Buf in[] = {{"Logits", Logits, Nt * Ng, in_bytes(dtype)}};
     const Buf out[] = {{"Choice", Choice, Nt * Kt, 4}, {"Gates", Gates, Nt * Kt, 4},
                        {"Offsets", Offsets, Ng + 1, 4}, {"Rows", Rows, Nt * Kt, 4},
-                       {"Slots", Slots, Nt * Kt, 4}, {"workspace", workspace, need ? need : 0, 1}};
+                       {"Slots", Slots, Nt * Kt, 4}, {"workspace", workspace, need, 1}};
     if ((st = check_ws(workspace, ws_bytes, need)) || (st = check_bufs(in, out))) return st;
     OrderArgs o = {};
     o.key = Choice;
