@@ -567,7 +567,8 @@ int cnn_group_bwd_ker(const void* dOut, const void* In, void* dKer, const int32_
  * In[Nt][Nc], Ker[Nk][Nc], A[Na][Nl][Nc], B[Na][Nk][Nl], Scales[Na] (NULL:
  * ones), Na <= 1024, Nl <= 4096.  A row whose Ids is outside [0, Na) has no
  * adapter.  Adapters of smaller rank are stored with zeros up to Nl.  The inner
- * sum is kept to fp32.  For calls that serve; gradients are those of
+ * sum is kept to fp32 (of many rows, its product with Scales: an infinity there
+ * is one before the sum over r).  For calls that serve; gradients are those of
  * cnn_group_* with the adapters as groups.  workspace: cnn_adapt_ws bytes,
  * 16-byte aligned.  Errors as cnn_route.
  */

@@ -598,7 +598,7 @@ __device__ __forceinline__ float bf16_part(float h, int part) {
 // B's values as the later parts of H meet them (bf16): infinities and
 // NaN are replaced by the type's largest value.  A later part may be zero, and
 // zero times infinity would be NaN; the first part, which is zero only where H
-// is, gives what is due.  Finite values stay, and so does all of a first part's.
+// is (to 2^-133), gives what is due.  Finite values stay, and so does all of a first part's.
 __device__ __forceinline__ u32x4_t met_by_part(u32x4_t b, bool later) {
   typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
   const u16x2_t most = __builtin_bit_cast(u16x2_t, later ? 0x7f7f7f7fu : 0x7fff7fffu);

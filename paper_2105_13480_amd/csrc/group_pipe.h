@@ -148,9 +148,10 @@ template <bool KC, bool GATHER, int NB> struct PipeOperand {
 // the main loop (the same places in LDS, two runs at a time): adapter by
 // adapter of the tile's rows, which are in the adapters' order, the rows of B
 // (its parts' ranks over again) and the rows of H.  Only the adapter's own rows
-// take its products, so what is not finite in B stays in them.  Both operands
-// straight from memory, a quarter of the results at a time, took 30 us a tile
-// and adapter at rank 64 in two parts, this about 6.
+// take its products, so what is not finite in B stays in them.  H in three parts
+// takes 13 us a tile at rank 64 and 8 at rank 16 (8192 rows of 2048 x 4096, one
+// adapter a tile; two 18 and 9).  In two parts, straight from memory, a quarter of
+// the results at a time, it was 30 at rank 64.
 template <typename TO>
 __device__ __forceinline__ void pipe_low_rank(const GroupArgs& a, const AdaptArgs& ad,
                                               const Tile<bf16_t, TO>& w, int tid, int lane, int wave,

@@ -450,7 +450,8 @@ hipError_t launch_group_few(const GroupArgs& a, int dtype, hipStream_t stream) {
 // bf16 / fp32, us, rows as they come against the order of the adapters: 256 rows of
 // 4096 x 4096, rank 16, 29 / 95 and 36 / 122; 400 rows 44 / 173 and 42 / 182; 333 of
 // 2048 x 2048, rank 32, 25 / 66 and 27 / 68; 512 rows 32 / 83 and 27 / 77, but of
-// 512 x 512, rank 8, 9.2 / 14 and 14 / 20.  Rows that are on no 4-byte boundary go
+// 512 x 512, rank 8, 9.2 / 14 and 14 / 20.  Higher ranks were not measured and are
+// no part of the rule.  Rows that are on no 4-byte boundary go
 // straight to the registers: 1001 x 1537, rank 12, in bf16 at 128 rows 18 and 22, at
 // 256 28 and 23.
 bool adapt_few(int64_t Nt, int64_t Nc, int64_t Nk, bool ring) {

@@ -7,9 +7,10 @@
 // maximum over the lanes by data-parallel moves, so every lane knows it: in
 // bf16 of (16-bit key, ~expert) as one value, in fp32 of the key and then of
 // the lowest expert that has it; ties go to the lowest expert.  Four rows a
-// wave.  Bound by the latency of Kt dependent maxima (16384 rows of 128 experts,
-// eight choices, bf16: 7.6 us for 4 MB of logits) and, for few rows, by the
-// launch: up to 64 rows are chosen and ordered in one (16 rows of 32: 3.7 us).
+// wave.  Bound by its instructions, some 70 a choice (16384 rows of 128 experts,
+// eight choices, bf16: 7.6 to 8.8 us for 4 MB of logits, half of it issuing them on
+// four waves a SIMD) and, for few rows, by the launch: up to 64 rows are chosen and
+// ordered in one (16 rows of 32: 4 us).
 //
 // Order: a counting sort, stable.  A workgroup owns a chunk of rows; the
 // chunk's counts per expert go to the workspace, then every workgroup adds up
