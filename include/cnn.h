@@ -580,6 +580,94 @@ int cnn_adapt_fwd(const void* In, const void* Ker, const void* A, const void* B,
 /* Bytes of cnn_adapt_fwd's workspace (host only). */
 int cnn_adapt_ws(int64_t Nt, int64_t Nc, int64_t Nk, int64_t Na, int64_t Nl, int64_t* ws_bytes);
 
+/*
+ * The router's balance: how often each expert is chosen, and the losses that a
+ * router is trained with beside its own.  Bounds[Ns + 1]: sequence s has the rows
+ * [Bounds[s], Bounds[s + 1]), non-decreasing, in [0, Nt]; rows outside all of them
+ * are padding.  Bounds NULL: one sequence of all rows (Ns = 1).
+ *
+ * A row takes part if it has a choice (Choice[Nt][Kt], outside [0, Ng): none) and
+ * a logit that is allowed (neither -inf nor NaN); p is the softmax over its
+ * allowed logits and z the logarithm of their exponentials' sum.  Then
+ *   Counts[s][e]  the choices of expert e in sequence s (whole numbers)
+ *   Tokens[s]     the rows of s that take part
+ *   Loss[0]       mean over the sequences with Tokens > 0 of
+ *                 Ng sum_e (Counts[s][e] / sum Counts[s]) (sum_t p[t][e] / Tokens[s])
+ *   Loss[1]       sum_t z[t]^2 / sum Tokens
+ * Loss[0] is 1 where choices or weights are even; both are 0 without a row.  dtype
+ * is the logits' (CNN_F32, else bf16).  Bounds that are no such order leave the
+ * result unspecified.  workspace: cnn_balance_ws bytes (0 for one sequence of few
+ * rows), 16-byte aligned.  Limits and errors as cnn_route; Ns <= 2^20.
+ */
+int cnn_balance(const void* Logits, const int32_t* Choice, const int32_t* Bounds, int32_t* Counts,
+                int32_t* Tokens, float* Loss, int64_t Nt, int64_t Ng, int64_t Kt, int64_t Ns, int dtype,
+                void* workspace, int64_t ws_bytes, void* stream);
+
+/* Bytes of cnn_balance's workspace (host only). */
+int cnn_balance_ws(int64_t Nt, int64_t Ng, int64_t Ns, int64_t* ws_bytes);
+
+/*
+ * Its gradient: dLogits of dLoss[0] Loss[0] + dLoss[1] Loss[1] (dLoss on the
+ * device), with Counts and Tokens as cnn_balance gave them; Counts are taken as
+ * constants, and may have been summed over processes since.  Zero for rows that
+ * do not take part and for experts without weight.  add != 0: on top of what
+ * dLogits holds (the router's own gradient), else dLogits is overwritten.
+ */
+int cnn_balance_bwd(const void* Logits, const int32_t* Choice, const int32_t* Bounds,
+                    const int32_t* Counts, const int32_t* Tokens, const float* dLoss, void* dLogits,
+                    int64_t Nt, int64_t Ng, int64_t Kt, int64_t Ns, int dtype, int add, void* stream);
+
+/*
+ * ---- 4 bits with a shared scale -------------------------------------------
+ *
+ * A row of Nc values is ceil(Nc / 32) blocks of 32.  A block has a scale byte s,
+ * 2^(s - 127) (255: the block is NaN), and 16 bytes of codes, two values each, the
+ * first in the low half: bit 3 the sign, bits 0..2 the size 0, 1/2, 1, 3/2, 2, 3,
+ * 4 or 6 times the scale.  Codes past the row's end are zeros.  A tensor's codes are
+ * [rows][blocks][16] on a 16-byte boundary (else CNN_E_SHAPE), its scales
+ * [rows][blocks].
+ */
+
+/* The scale of a block whose largest magnitude is a, 2^x <= a < 2^(x + 1). */
+typedef enum cnn_scale {
+  CNN_SCALE_FLOOR = 0, /* 2^(x - 2): a is below 8 scales, above 6 it becomes 6            */
+  CNN_SCALE_UP = 1     /* the least power of two of which a is at most 6 times: none is cut */
+} cnn_scale;
+
+/*
+ * Rows In[Nt][Nc] (dtype CNN_F32, else bf16) to 4 bits: to nearest, ties to the even
+ * code, the sign kept.  Scales are at least 2^-127; a block that holds an infinity
+ * or NaN gets scale 255.
+ */
+int cnn_quantize4(const void* In, uint8_t* Codes, uint8_t* Scales, int64_t Nt, int64_t Nc, int dtype,
+                  int rule, void* stream);
+
+/*
+ * The values again, Out[Nt][Nc] (dtype CNN_F32, else bf16): exact in both, but for
+ * sizes of 2^128 and more, which are infinite.
+ */
+int cnn_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void* Out, int64_t Nt, int64_t Nc,
+                    int dtype, void* stream);
+
+/*
+ * cnn_group_fwd of a Ker in 4 bits along c: Ker [Ng][Nk][blocks][16], KerScales
+ * [Ng][Nk][blocks].  InScales NULL: In[Nt][Nc] is bf16; else In is in 4 bits too,
+ * codes [Nt][blocks][16] and InScales [Nt][blocks], as cnn_quantize4 makes them of
+ * the rows.  Products are of the exact values, sums fp32.  dtype: CNN_BF16 (fp32
+ * Out) or CNN_BF16_OBF16 (CNN_F32: CNN_E_UNSUPPORTED).
+ */
+int cnn_group_fwd4(const void* In, const uint8_t* InScales, const uint8_t* Ker, const uint8_t* KerScales,
+                   void* Out, const int32_t* Offsets, const int32_t* Rows, int64_t Nt, int64_t Np,
+                   int64_t Ng, int64_t Nc, int64_t Nk, int dtype, void* stream);
+
+/*
+ * Its gradient in In, in grouped order, through the same Ker: dIn[p][c] = sum_k
+ * dOut[p][k] Ker[g][k][c], dOut bf16.
+ */
+int cnn_group_bwd_in4(const void* dOut, const uint8_t* Ker, const uint8_t* KerScales, void* dIn,
+                      const int32_t* Offsets, int64_t Np, int64_t Ng, int64_t Nc, int64_t Nk, int dtype,
+                      void* stream);
+
 /* Budget of HIP device `device` (CU count, LDS per CU, accumulator regs). */
 int cnn_device_budget(int device, cnn_budget* budget);
 

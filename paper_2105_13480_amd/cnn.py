@@ -39,7 +39,8 @@ EXPORTS = ["cnn_fwd", "cnn_plan", "cnn_plan_candidates", "cnn_variants", "cnn_pl
            "cnn_strerror", "cnn_last_error", "cnn_abi_version",
            "cnn_route", "cnn_route_ws", "cnn_route_bwd", "cnn_combine", "cnn_combine_bwd",
            "cnn_group_fwd", "cnn_group_bwd_in", "cnn_group_bwd_ker", "cnn_adapt_fwd",
-           "cnn_adapt_ws"]
+           "cnn_adapt_ws", "cnn_balance", "cnn_balance_ws", "cnn_balance_bwd", "cnn_quantize4",
+           "cnn_dequantize4", "cnn_group_fwd4", "cnn_group_bwd_in4"]
 
 i64 = ctypes.c_int64
 
@@ -148,7 +149,14 @@ def lib():
                     ("cnn_group_bwd_in", [vp] * 4 + [i64] * 4 + [ci, vp]),
                     ("cnn_group_bwd_ker", [vp] * 5 + [i64] * 5 + [ci, vp]),
                     ("cnn_adapt_fwd", [vp] * 7 + [i64] * 5 + [ci, vp, i64, vp]),
-                    ("cnn_adapt_ws", [i64] * 5 + [lp])):
+                    ("cnn_adapt_ws", [i64] * 5 + [lp]),
+                    ("cnn_balance", [vp] * 6 + [i64] * 4 + [ci, vp, i64, vp]),
+                    ("cnn_balance_ws", [i64] * 3 + [lp]),
+                    ("cnn_balance_bwd", [vp] * 7 + [i64] * 4 + [ci, ci, vp]),
+                    ("cnn_quantize4", [vp] * 3 + [i64] * 2 + [ci, ci, vp]),
+                    ("cnn_dequantize4", [vp] * 3 + [i64] * 2 + [ci, vp]),
+                    ("cnn_group_fwd4", [vp] * 7 + [i64] * 5 + [ci, vp]),
+                    ("cnn_group_bwd_in4", [vp] * 5 + [i64] * 4 + [ci, vp])):
         getattr(L, f).argtypes = args
         getattr(L, f).restype = ci
     _lib = L

@@ -1,0 +1,337 @@
+// Tile kernels of the grouped products whose Ker lies in 4 bits (gfx950): blocks
+// of 32 values of c with a scale byte each, see k_block4.hip.
+//
+// With bf16 rows (group4_tiles) Ker's values become bf16 on their way into LDS,
+// which is exact (a code has two significant bits, and its scale is a power of
+// two), and are then what the bf16 kernel multiplies; both directions, since the
+// conversion is the same whether c is summed over or is the result's index:
+//   forward       X = Ker[g], rows of features, k = c
+//   gradient, In  X = Ker[g], rows of k = features, the tile's index c
+#pragma once
+
+#include "group_kernel.h"
+
+namespace cnnlib {
+namespace group {
+
+// 2^(s - 127) as the conversions take it: they read the exponent field alone, 0 is
+// 2^-127 and 255 NaN.
+__device__ __forceinline__ float scale4(uint32_t s) { return __uint_as_float(s << 23); }
+
+// Eight values from a word of codes, as bf16.
+__device__ __forceinline__ u32x4_t bf16_of4(uint32_t code, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3))};
+#else
+  (void)code;
+  (void)scale;
+  return u32x4_t{0u, 0u, 0u, 0u};
+#endif
+}
+
+// Stages R rows of features by 64 of k (KC) or 64 rows of k by R of c of a Ker in
+// 4 bits as bf16: a thread takes half blocks (8 bytes, 16 values).
+template <bool KC, int R, int NT> struct Stager4 {
+  static constexpr int ALL = 4 * R, NU = (ALL + NT - 1) / NT;
+  static constexpr int U = KC ? 4 : R / 16;  // half blocks of a row of the stage
+  const uint8_t* codes[NU];
+  const uint8_t* scales[NU];
+  int at[NU];        // KC: the half block's first k within a stage; else its row of k
+  bool there[NU];    // !KC: the half block is one of the row's
+  u32x2_t code[2][NU];
+  uint32_t scale[2][NU];
+  uint32_t gone[2];  // bit j: half block j of the set is not there
+
+  // codes, scales: the group's; rows of Nb blocks; rows (KC) or c (else) [i0, i0 + n) are there.
+  __device__ __forceinline__ void init(int tid, const uint8_t* c4, const uint8_t* s4, int Nb, int i0, int n) {
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      const int u = min(j * NT + tid, ALL - 1), r = u / U, q = u % U;
+      if constexpr (KC) {
+        const int64_t row = i0 + min(r, n - 1);
+        at[j] = 16 * q;
+        codes[j] = c4 + row * 16 * Nb + 8 * q;
+        scales[j] = s4 + row * Nb + (q >> 1);
+        there[j] = true;
+      } else {
+        at[j] = r;
+        there[j] = i0 + 16 * q < 32 * Nb;
+        codes[j] = c4 + (there[j] ? i0 / 2 + 8 * q : 0);
+        scales[j] = s4 + (there[j] ? (i0 + 16 * q) / 32 : 0);
+      }
+    }
+  }
+  // nk: values of k (KC: of whole blocks).  What is not there is cleared when the
+  // loads are waited for.
+  template <int SET> __device__ __forceinline__ void load(int k0, int Nb, int nk) {
+    gone[SET] = 0u;
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      const bool in = k0 + at[j] < nk;
+      gone[SET] |= (in && there[j] ? 0u : 1u) << j;
+      if constexpr (KC) {
+        const int k = in ? k0 : 0;
+        __builtin_memcpy(&code[SET][j], codes[j] + (k >> 1), 8);
+        scale[SET][j] = scales[j][k >> 5];
+      } else {
+        const int64_t k = min(k0 + at[j], nk - 1);
+        __builtin_memcpy(&code[SET][j], codes[j] + k * 16 * Nb, 8);
+        scale[SET][j] = scales[j][k * Nb];
+      }
+    }
+  }
+  template <int SET> __device__ __forceinline__ void commit(int tid, u32x4_t* lds) const {
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      const int u = j * NT + tid, r = u / U, q = u % U;
+      if (ALL % NT != 0 && u >= ALL) break;
+      const bool in = !(gone[SET] >> j & 1);
+      const float s = scale4(in ? scale[SET][j] : 0u);
+      lds[unit_at<bf16_t, KC, R>(r, 2 * q)] = bf16_of4(in ? code[SET][j][0] : 0u, s);
+      lds[unit_at<bf16_t, KC, R>(r, 2 * q + 1)] = bf16_of4(in ? code[SET][j][1] : 0u, s);
+    }
+  }
+};
+
+// TM x TN results by 2 x 2 waves, both operands through registers at any
+// alignment of the rows, two stages in LDS and two in flight.
+template <typename TO, int MODE, int TM, int TN>
+__global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b, int band) {
+  typedef bf16_t T;
+  constexpr int NT = 256, WM = 2, WN = 2, TK = 64;
+  constexpr bool XKC = MODE == kFwd, YG = MODE == kFwd;
+  constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
+  constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  auto xrow = [&](int i) { return wm * (TM / WM) + 16 * i; };
+  auto yrow = [&](int j) { return wn * (TN / WN) + 16 * j; };
+
+  Tile<T, TO> w;
+  if (!setup_tile<T, TO, MODE, TM, TN>(a, band, &w)) return;
+  const int64_t g = w.g < a.Ng ? w.g : 0;
+  const int rows_x = XKC ? a.M : a.K;  // rows of one group's Ker
+  Stager4<XKC, TM, NT> sx;
+  Stager<T, true, TN, NT, YG> sy;
+  Reader<T, XKC, TM, NI> rx;
+  Reader<T, true, TN, NJ> ry;
+  rx.init(xrow(0), lane);
+  ry.init(yrow(0), lane);
+
+  f32x4_t acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  if (w.K > 0) {
+    const uint8_t* const codes = reinterpret_cast<const uint8_t*>(a.X) + g * rows_x * 16 * b.Nb;
+    sx.init(tid, codes, b.xs + g * rows_x * b.Nb, b.Nb, w.m0, w.m_valid);
+    sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, YG ? w.rows : nullptr, a.Nsrc);
+    const int xk = XKC ? 32 * b.Nb : w.K;
+    const int n_st = (w.K + TK - 1) / TK;
+    auto load = [&](auto set, int s) __attribute__((always_inline)) {
+      sx.template load<set.value>(s * TK, b.Nb, xk);
+      sy.template load<set.value>(s * TK, a.ldy, w.K, nullptr, 0);
+    };
+    auto commit = [&](auto set, int s) __attribute__((always_inline)) {
+      u32x4_t* const dst = ring + (s & 1) * STAGE;
+      sx.template commit<set.value>(tid, dst);
+      sy.template commit<set.value>(tid, dst + XU, s * TK, a.ldy, w.K, nullptr, 0);
+    };
+    auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
+      u32x4_t xf[NI][2], yf[NJ][2];
+      rx.read(buf, xf);
+      ry.read(buf + XU, yf);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i][ks], yf[j][ks], acc[i][j]);
+    };
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    load(even, 0);
+    if (n_st > 1) load(odd, 1);
+    commit(even, 0);
+    auto step = [&](auto set, auto other, int s) __attribute__((always_inline)) {
+      __syncthreads();  // stage s is there; every wave is done with stage s - 1
+      if (s + 2 < n_st) load(set, s + 2);
+      compute(ring + (s & 1) * STAGE);
+      if (s + 1 < n_st) commit(other, s + 1);
+    };
+    int s = 0;
+    for (; s + 2 <= n_st; s += 2) {
+      step(even, odd, s);
+      step(odd, even, s + 1);
+    }
+    if (s < n_st) step(even, odd, s);
+  }
+  store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
+}
+
+template <typename TO, int MODE, int TM, int TN>
+hipError_t launch_tiles4(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
+  auto* const k = group4_tiles<TO, MODE, TM, TN>;
+  const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
+  const hipError_t fit = grid_fits(grid, 256);
+  if (fit != hipSuccess) return fit;
+  const int lds = 2 * 8 * (TM + TN) * 16;
+  k<<<dim3((uint32_t)grid), dim3(256), lds, stream>>>(a, b, band);
+  return hipGetLastError();
+}
+
+// Both operands in 4 bits: a block of 32 is 16 bytes, which is what one lane gives
+// the scaled matrix instruction (128 values of k by 16 rows: lane l has row l % 16,
+// block l / 16 and its scale).  So rows of codes are staged as rows of eight bf16
+// values a block are, straight to LDS, and a stage of 128 bytes holds 256 values.
+// Lane l takes blocks 2 (l / 16) and the next, whose two scales it loads at once;
+// the other operand's lane takes the same.
+template <int NB> struct Scales4 {
+  const uint8_t* p[NB];  // this lane's rows
+
+  // Scales of blocks `at` and the next of rows of Nb; past their end 2^-127 (the
+  // codes there are zeros).
+  __device__ __forceinline__ void load(int at, int Nb, uint32_t (&s)[NB]) const {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (at + 1 < Nb) {
+        uint16_t v;
+        __builtin_memcpy(&v, p[i] + at, 2);
+        s[i] = v;
+      } else {
+        s[i] = at < Nb ? p[i][at] : 0u;
+      }
+    }
+  }
+};
+
+template <int KS>
+__device__ __forceinline__ f32x4_t mma4(u32x4_t x, u32x4_t y, f32x4_t acc, uint32_t sx, uint32_t sy) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef int i32x8_t __attribute__((ext_vector_type(8)));
+  const i32x8_t p = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
+  const i32x8_t q = {(int)y[0], (int)y[1], (int)y[2], (int)y[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, acc, 4, 4, KS, (int)sx, KS, (int)sy);
+#else
+  (void)x;
+  (void)y;
+  (void)sx;
+  (void)sy;
+  return acc;
+#endif
+}
+
+template <typename TO, int TM, int TN, int WM, int WN, int DEPTH>
+__global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Group4Args b, int band) {
+  typedef bf16_t T;
+  constexpr int NT = 64 * WM * WN, TK = 64;  // of 16-bit words: 256 values
+  constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
+  constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, G = lane >> 4;
+  const int wm = wave % WM, wn = wave / WM;
+  auto xrow = [&](int i) { return wm * (TM / WM) + 16 * i; };
+  auto yrow = [&](int j) { return wn * (TN / WN) + 16 * j; };
+
+  Tile<T, TO> w;
+  if (!setup_tile<T, TO, kFwd, TM, TN>(a, band, &w)) return;
+  const int64_t g = w.g < a.Ng ? w.g : 0;
+  Stager<T, true, TM, NT, false> sx;
+  Stager<T, true, TN, NT, true> sy;
+  Scales4<NI> px;
+  Scales4<NJ> py;
+
+  f32x4_t acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  if (w.K > 0) {
+    sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, nullptr, 0);
+    sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, w.rows, a.Nsrc);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      px.p[i] = b.xs + (g * a.M + w.m0 + min(xrow(i) + l16, w.m_valid - 1)) * b.Nb;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      int64_t r = w.n0 + min(yrow(j) + l16, w.n_valid - 1);
+      if (w.rows) {
+        r = w.rows[r];
+        if (r < 0 || r >= a.Nsrc) r = 0;
+      }
+      py.p[j] = b.ys + r * b.Nb;
+    }
+    constexpr int COPIES = sx.NU + sy.NU;
+    const int n_st = (w.K + TK - 1) / TK;
+    auto copy = [&](int s) __attribute__((always_inline)) {
+      u32x4_t* const dst = ring + (s % DEPTH) * STAGE;
+      const int K = s < n_st ? w.K : 0;
+      sx.copy(tid, dst, s * TK, a.ldx, K, nullptr, 0);
+      sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
+    };
+    uint32_t at[2][2];  // LDS bytes of this lane's units, by sub-step
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      at[0][ks] = 16 * unit_at<T, true, TM>(xrow(0) + l16, 2 * G + ks);
+      at[1][ks] = 16 * unit_at<T, true, TN>(yrow(0) + l16, 2 * G + ks);
+    }
+#pragma unroll
+    for (int s = 0; s < DEPTH - 1; ++s) copy(s);
+    for (int s = 0; s < n_st; ++s) {
+      uint32_t fx[NI], fy[NJ];
+      px.load(8 * s + 2 * G, b.Nb, fx);
+      py.load(8 * s + 2 * G, b.Nb, fy);
+      // stage s has landed (the later ones' copies and the scales may be in flight);
+      // every wave is done with stage s - 1
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
+      copy(s + DEPTH - 1);
+      const char* const buf = reinterpret_cast<const char*>(ring + (s % DEPTH) * STAGE);
+      u32x4_t xf[NI][2], yf[NJ][2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) xf[i][ks] = *reinterpret_cast<const u32x4_t*>(buf + at[0][ks] + 2048 * i);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) yf[j][ks] = *reinterpret_cast<const u32x4_t*>(buf + 16 * XU + at[1][ks] + 2048 * j);
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          acc[i][j] = mma4<0>(xf[i][0], yf[j][0], acc[i][j], fx[i], fy[j]);
+          acc[i][j] = mma4<1>(xf[i][1], yf[j][1], acc[i][j], fx[i], fy[j]);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
+  }
+  store_tile<T, TO, kFwd, true>(a, w, lane, acc, xrow, yrow);
+}
+
+template <typename TO, int TM, int TN, int WM, int WN, int DEPTH>
+hipError_t launch_tiles44(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
+  auto* const k = group44_tiles<TO, TM, TN, WM, WN, DEPTH>;
+  const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
+  const hipError_t fit = grid_fits(grid, 64 * WM * WN);
+  if (fit != hipSuccess) return fit;
+  const int lds = DEPTH * 8 * (TM + TN) * 16;
+  if (lds > 64 * 1024) {
+    const hipError_t e = allow_max_lds(reinterpret_cast<const void*>(k));
+    if (e != hipSuccess) return e;
+  }
+  k<<<dim3((uint32_t)grid), dim3(64 * WM * WN), lds, stream>>>(a, b, band);
+  return hipGetLastError();
+}
+
+}  // namespace group
+}  // namespace cnnlib

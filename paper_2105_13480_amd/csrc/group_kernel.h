@@ -1049,6 +1049,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_tiles(GroupArgs a, Adap
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 
+// Tiles that the worst split of Np rows into Ng groups and the rows past them
+// needs: each non-empty group may leave one tile partly filled.
+inline int64_t row_tiles(int64_t Np, int64_t Ng, bool groups, int TN) {
+  if (!groups) return (Np + TN - 1) / TN;
+  const int64_t parts = Ng + 1 < Np ? Ng + 1 : Np;
+  return Np / TN + parts;
+}
+
 template <typename T, typename TO, int MODE, int TM, int TN, int WM, int WN, int DEPTH, bool WHOLE = true>
 hipError_t launch_tiles(const GroupArgs& a, const AdaptArgs& ad, int64_t row_tiles, int band,
                         Launch to) {

@@ -14,14 +14,6 @@ bool copies_ok(const void* p, int64_t ld, int64_t extent, bool kc, int esize) {
   return ((uintptr_t)p & 3) == 0 && (ld * esize) % 4 == 0 && (kc || (extent * esize) % 16 == 0);
 }
 
-// Tiles that the worst split of Np rows into Ng groups and the rows past them
-// needs: each non-empty group may leave one tile partly filled.
-int64_t row_tiles(int64_t Np, int64_t Ng, bool groups, int TN) {
-  if (!groups) return (Np + TN - 1) / TN;
-  const int64_t parts = Ng + 1 < Np ? Ng + 1 : Np;
-  return Np / TN + parts;
-}
-
 // Row tiles of TN rows of a launch.
 template <int MODE> int64_t row_tiles_of(const GroupArgs& a, int TN) {
   if (MODE == kBwdKer) return (int64_t)a.Ng * ((a.N + TN - 1) / TN);

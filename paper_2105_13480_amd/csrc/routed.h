@@ -76,6 +76,31 @@ struct RouteArgs {
   int32_t over_all;     // weights over all allowed experts, not the chosen ones
 };
 
+// A Ker in 4 bits beside GroupArgs, whose X then points to its codes: rows of Nb
+// blocks of 16 bytes, and a scale byte each.
+struct Group4Args {
+  const uint8_t* xs;  // scales of X's blocks
+  const uint8_t* ys;  // of Y's, if it is in 4 bits too; else NULL
+  int32_t Nb;
+};
+
+// The router's balance.
+struct BalanceArgs {
+  const void* logits;     // [Nt][Ng]
+  const int32_t* choice;  // [Nt][Kt]
+  const int32_t* bounds;  // [Ns + 1], NULL: one sequence of all rows
+  int32_t* counts;        // [Ns][Ng]
+  int32_t* tokens;        // [Ns]
+  float* loss;            // [2]
+  const float* dloss;     // [2]
+  void* dlogits;          // [Nt][Ng]
+  void* ws;
+  int32_t Nt, Ng, Kt, Ns;
+  int32_t chunk, nblocks; // rows of a workgroup, workgroups
+};
+// Rows of one sequence that a single workgroup takes.
+constexpr int64_t kBalanceOne = 256;
+
 // Where a launch goes; `dry`: it is only seen whether its grid fits.
 struct Launch {
   hipStream_t stream;
@@ -112,5 +137,15 @@ FewPlan adapt_few_plan(int64_t Nt, int64_t Nc, int64_t Nk, int es);
 hipError_t launch_adapt_few(const GroupArgs& a, const AdaptArgs& ad, int dtype, hipStream_t stream);
 // Rows in the order of their adapters (a.off, a.rows, ad.ids).
 hipError_t launch_adapt(const GroupArgs& a, const AdaptArgs& ad, int dtype, Launch to);
+
+int64_t balance_ws_bytes(int64_t Nt, int64_t Ng, int64_t Ns);
+hipError_t launch_balance(const BalanceArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_balance_bwd(const BalanceArgs& a, int dtype, bool add, hipStream_t stream);
+hipError_t launch_quantize4(const void* In, uint8_t* Codes, uint8_t* Scales, int64_t Nt, int64_t Nc,
+                            bool bf16, bool up, hipStream_t stream);
+hipError_t launch_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void* Out, int64_t Nt,
+                              int64_t Nc, bool bf16, hipStream_t stream);
+hipError_t launch_group_fwd4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream);
+hipError_t launch_group_bwd_in4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream);
 
 }  // namespace cnnlib

@@ -60,6 +60,7 @@ constexpr int64_t kGroups = 65535;
 constexpr int64_t kExperts = 1024;         // experts of a router, adapters of a projection
 constexpr int64_t kChoices = 16;
 constexpr int64_t kRank = 4096;
+constexpr int64_t kSequences = 1 << 20;
 constexpr int64_t kGrid = 0x7fffffff;
 
 int check_type(int dtype) {
@@ -137,6 +138,30 @@ int check_route(int64_t Nt, int64_t Ng, int64_t Kt) {
 int check_over(int over) {
   if (over != CNN_OVER_ALL && over != CNN_OVER_CHOSEN)
     return fail(CNN_E_UNSUPPORTED, "unknown weights %d", over);
+  return CNN_OK;
+}
+
+// Tensors in 4 bits: the blocks of a row, codes on 16-byte boundaries.
+int64_t blocks4(int64_t Nc) { return (Nc + 31) / 32; }
+int check_codes(const char* name, const void* p) {
+  if ((uintptr_t)p & 15) return fail(CNN_E_SHAPE, "%s must be 16-byte aligned", name);
+  return CNN_OK;
+}
+// Products of Ker in 4 bits: bf16 rows (or rows in 4 bits), either result.
+int check_type4(int dtype) {
+  const int st = check_type(dtype);
+  if (st) return st;
+  if (dtype == CNN_F32) return fail(CNN_E_UNSUPPORTED, "no product of fp32 rows and a Ker in 4 bits");
+  return CNN_OK;
+}
+
+int check_balance(int64_t Nt, int64_t Ng, int64_t Kt, int64_t Ns, bool bounds) {
+  const int st = check_route(Nt, Ng, Kt);
+  if (st) return st;
+  const Size s[] = {{"Ns", Ns, 1, kSequences}};
+  const int su = check_sizes(s);
+  if (su) return su;
+  if (!bounds && Ns != 1) return fail(CNN_E_SHAPE, "without Bounds, Ns = %lld must be 1", (long long)Ns);
   return CNN_OK;
 }
 
@@ -357,6 +382,145 @@ int cnn_group_bwd_ker(const void* dOut, const void* In, void* dKer, const int32_
     a.M = (int32_t)Nc; a.N = (int32_t)Nk; a.K = (int32_t)Np;
     a.Ng = (int32_t)Ng; a.Nsrc = (int32_t)Nt;
     return launched(launch_group_bwd_ker(a, dtype, (hipStream_t)stream));
+  });
+}
+
+int cnn_quantize4(const void* In, uint8_t* Codes, uint8_t* Scales, int64_t Nt, int64_t Nc, int dtype,
+                  int rule, void* stream) {
+  return guarded([&] {
+    const Size s[] = {{"Nt", Nt, 0, kRows}, {"Nc", Nc, 1, kFeatures}};
+    int st;
+    if ((st = check_sizes(s)) || (st = check_type(dtype))) return st;
+    if (rule != CNN_SCALE_FLOOR && rule != CNN_SCALE_UP) return fail(CNN_E_UNSUPPORTED, "unknown rule %d", rule);
+    const Buf in[] = {{"In", In, Nt * Nc, in_bytes(dtype)}};
+    const Buf out[] = {{"Codes", Codes, Nt * blocks4(Nc), 16}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
+    if ((st = check_codes("Codes", Codes)) || (st = check_bufs(in, out))) return st;
+    if (!Nt) return (int)CNN_OK;
+    return launched(launch_quantize4(In, Codes, Scales, Nt, Nc, dtype != CNN_F32, rule == CNN_SCALE_UP,
+                                     (hipStream_t)stream));
+  });
+}
+
+int cnn_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void* Out, int64_t Nt, int64_t Nc,
+                    int dtype, void* stream) {
+  return guarded([&] {
+    const Size s[] = {{"Nt", Nt, 0, kRows}, {"Nc", Nc, 1, kFeatures}};
+    int st;
+    if ((st = check_sizes(s)) || (st = check_type(dtype))) return st;
+    const Buf in[] = {{"Codes", Codes, Nt * blocks4(Nc), 16}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
+    const Buf out[] = {{"Out", Out, Nt * Nc, in_bytes(dtype)}};
+    if ((st = check_codes("Codes", Codes)) || (st = check_bufs(in, out))) return st;
+    if (!Nt) return (int)CNN_OK;
+    return launched(launch_dequantize4(Codes, Scales, Out, Nt, Nc, dtype != CNN_F32, (hipStream_t)stream));
+  });
+}
+
+int cnn_group_fwd4(const void* In, const uint8_t* InScales, const uint8_t* Ker, const uint8_t* KerScales,
+                   void* Out, const int32_t* Offsets, const int32_t* Rows, int64_t Nt, int64_t Np,
+                   int64_t Ng, int64_t Nc, int64_t Nk, int dtype, void* stream) {
+  return guarded([&] {
+    int st;
+    if ((st = check_group(Nt, Np, Ng, Nc, Nk, Rows != nullptr)) || (st = check_type4(dtype)) ||
+        (st = check_tiles(Np, Ng, Nk)))
+      return st;
+    const int64_t Nb = blocks4(Nc);
+    const Buf in[] = {{"In", In, InScales ? Nt * Nb : Nt * Nc, InScales ? 16 : 2},
+                      {"InScales", InScales, InScales ? Nt * Nb : 0, 1},
+                      {"Ker", Ker, product(Ng, Nk, Nb), 16}, {"KerScales", KerScales, product(Ng, Nk, Nb), 1},
+                      {"Offsets", Offsets, Ng + 1, 4}, {"Rows", Rows, Rows ? Np : 0, 4}};
+    const Buf out[] = {{"Out", Out, Np * Nk, out_bytes(dtype)}};
+    if ((st = check_codes("Ker", Ker)) || (InScales && (st = check_codes("In", In))) ||
+        (st = check_bufs(in, out)))
+      return st;
+    if (!Np) return (int)CNN_OK;
+    GroupArgs a = {};
+    a.X = Ker; a.Y = In; a.D = Out;
+    a.off = Offsets; a.rows = Rows;
+    a.ldx = 8 * Nb; a.ldy = InScales ? 8 * Nb : Nc; a.ldd = Nk;  // codes as 16-bit words
+    a.xgroup = Nk * 8 * Nb;
+    a.M = (int32_t)Nk; a.N = (int32_t)Np; a.K = (int32_t)(InScales ? 8 * Nb : Nc);
+    a.Ng = (int32_t)Ng; a.Nsrc = (int32_t)Nt;
+    const Group4Args b = {KerScales, InScales, (int32_t)Nb};
+    return launched(launch_group_fwd4(a, b, dtype == CNN_BF16_OBF16, (hipStream_t)stream));
+  });
+}
+
+int cnn_group_bwd_in4(const void* dOut, const uint8_t* Ker, const uint8_t* KerScales, void* dIn,
+                      const int32_t* Offsets, int64_t Np, int64_t Ng, int64_t Nc, int64_t Nk, int dtype,
+                      void* stream) {
+  return guarded([&] {
+    int st;
+    if ((st = check_group(Np, Np, Ng, Nc, Nk, false)) || (st = check_type4(dtype)) ||
+        (st = check_tiles(Np, Ng, Nc)))
+      return st;
+    const int64_t Nb = blocks4(Nc);
+    const Buf in[] = {{"dOut", dOut, Np * Nk, 2}, {"Ker", Ker, product(Ng, Nk, Nb), 16},
+                      {"KerScales", KerScales, product(Ng, Nk, Nb), 1}, {"Offsets", Offsets, Ng + 1, 4}};
+    const Buf out[] = {{"dIn", dIn, Np * Nc, out_bytes(dtype)}};
+    if ((st = check_codes("Ker", Ker)) || (st = check_bufs(in, out))) return st;
+    if (!Np) return (int)CNN_OK;
+    GroupArgs a = {};
+    a.X = Ker; a.Y = dOut; a.D = dIn;
+    a.off = Offsets;
+    a.ldx = 8 * Nb; a.ldy = Nk; a.ldd = Nc;
+    a.xgroup = Nk * 8 * Nb;
+    a.M = (int32_t)Nc; a.N = (int32_t)Np; a.K = (int32_t)Nk;
+    a.Ng = (int32_t)Ng; a.Nsrc = (int32_t)Np;
+    const Group4Args b = {KerScales, nullptr, (int32_t)Nb};
+    return launched(launch_group_bwd_in4(a, b, dtype == CNN_BF16_OBF16, (hipStream_t)stream));
+  });
+}
+
+int cnn_balance_ws(int64_t Nt, int64_t Ng, int64_t Ns, int64_t* ws_bytes) {
+  return guarded([&] {
+    if (!ws_bytes) return fail(CNN_E_NULL, "ws_bytes must be non-NULL");
+    const int st = check_balance(Nt, Ng, 1, Ns, true);
+    if (st) return st;
+    *ws_bytes = balance_ws_bytes(Nt, Ng, Ns);
+    return (int)CNN_OK;
+  });
+}
+
+int cnn_balance(const void* Logits, const int32_t* Choice, const int32_t* Bounds, int32_t* Counts,
+                int32_t* Tokens, float* Loss, int64_t Nt, int64_t Ng, int64_t Kt, int64_t Ns, int dtype,
+                void* workspace, int64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    int st;
+    if ((st = check_balance(Nt, Ng, Kt, Ns, Bounds != nullptr)) || (st = check_type(dtype))) return st;
+    const int64_t need = balance_ws_bytes(Nt, Ng, Ns);
+    const Buf in[] = {{"Logits", Logits, Nt * Ng, in_bytes(dtype)}, {"Choice", Choice, Nt * Kt, 4},
+                      {"Bounds", Bounds, Bounds ? Ns + 1 : 0, 4}};
+    const Buf out[] = {{"Counts", Counts, Ns * Ng, 4}, {"Tokens", Tokens, Ns, 4}, {"Loss", Loss, 2, 4},
+                       {"workspace", workspace, need, 1}};
+    if ((st = check_ws(workspace, ws_bytes, need)) || (st = check_bufs(in, out))) return st;
+    BalanceArgs a = {};
+    a.logits = Logits; a.choice = Choice; a.bounds = Bounds;
+    a.counts = Counts; a.tokens = Tokens; a.loss = Loss;
+    a.ws = workspace;
+    a.Nt = (int32_t)Nt; a.Ng = (int32_t)Ng; a.Kt = (int32_t)Kt; a.Ns = (int32_t)Ns;
+    order_blocks(Nt, &a.chunk, &a.nblocks);
+    return launched(launch_balance(a, dtype != CNN_F32, (hipStream_t)stream));
+  });
+}
+
+int cnn_balance_bwd(const void* Logits, const int32_t* Choice, const int32_t* Bounds,
+                    const int32_t* Counts, const int32_t* Tokens, const float* dLoss, void* dLogits,
+                    int64_t Nt, int64_t Ng, int64_t Kt, int64_t Ns, int dtype, int add, void* stream) {
+  return guarded([&] {
+    int st;
+    if ((st = check_balance(Nt, Ng, Kt, Ns, Bounds != nullptr)) || (st = check_type(dtype))) return st;
+    const Buf in[] = {{"Logits", Logits, Nt * Ng, in_bytes(dtype)}, {"Choice", Choice, Nt * Kt, 4},
+                      {"Bounds", Bounds, Bounds ? Ns + 1 : 0, 4}, {"Counts", Counts, Ns * Ng, 4},
+                      {"Tokens", Tokens, Ns, 4}, {"dLoss", dLoss, 2, 4}};
+    const Buf out[] = {{"dLogits", dLogits, Nt * Ng, out_bytes(dtype)}};
+    if ((st = check_bufs(in, out))) return st;
+    if (!Nt) return (int)CNN_OK;
+    BalanceArgs a = {};
+    a.logits = Logits; a.choice = Choice; a.bounds = Bounds;
+    a.counts = const_cast<int32_t*>(Counts); a.tokens = const_cast<int32_t*>(Tokens);
+    a.dloss = dLoss; a.dlogits = dLogits;
+    a.Nt = (int32_t)Nt; a.Ng = (int32_t)Ng; a.Kt = (int32_t)Kt; a.Ns = (int32_t)Ns;
+    return launched(launch_balance_bwd(a, dtype, add != 0, (hipStream_t)stream));
   });
 }
 

@@ -4,7 +4,10 @@ depends on the row.
 A router chooses experts for each row (``route``), the rows are multiplied by
 their experts' Kers group by group (``group_fwd``), and the results return to
 their rows (``combine``); each has its gradient.  ``adapt_fwd`` is a shared
-projection with a low-rank adapter for each row.
+projection with a low-rank adapter for each row.  ``balance`` counts the router's
+choices and gives the losses that keep them even.  ``quantize4`` puts rows into 4
+bits with a scale for every 32 values, and ``group_fwd4`` and ``group_bwd_in4``
+are the groups' products with such a Ker.
 
 Argument marshalling only, as in ``cnn``: tensors are contiguous torch tensors
 on the current GPU, results are the caller's tensors, every call is
@@ -20,23 +23,24 @@ from . import cnn
 from .cnn import CNN_BF16, CNN_BF16_OBF16, CNN_F32, _check, _stream, i64
 
 OVER = {"all": 0, "chosen": 1}
+RULES = {"floor": 0, "up": 1}  # how a block's scale is chosen
 MAX_EXPERTS, MAX_CHOICES = 1024, 16
 
 _torch = None
 _types = None  # (operands' dtype, result's dtype) -> cnn_dtype
 _here = None
-_i32 = _f32 = None
+_i32 = _f32 = _u8 = None
 
 
 def _load():
-    global _torch, _types, _here, _i32, _f32
+    global _torch, _types, _here, _i32, _f32, _u8
     import torch
     _types = {(torch.float32, torch.float32): CNN_F32, (torch.bfloat16, torch.float32): CNN_BF16,
               (torch.bfloat16, torch.bfloat16): CNN_BF16_OBF16}
     # the current GPU's index, without the lazy initialisation's check where
     # torch offers that (a call on a small tensor is bound by the host)
     _here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    _i32, _f32 = torch.int32, torch.float32
+    _i32, _f32, _u8 = torch.int32, torch.float32, torch.uint8
     _torch = torch
     return torch
 
@@ -344,14 +348,14 @@ def adapt_workspace(In, Ker, A, Out):
     return _torch.empty(n.value, dtype=_torch.uint8, device=In.device)
 
 
-def _adapt_own_workspace(In, Ker, A, Out, stream):
+def _own_workspace(make, stream):
     """One for a single call, of the memory of the stream that the call runs on:
     it is free for that stream's later work only."""
     if stream is None:
-        return adapt_workspace(In, Ker, A, Out)
+        return make()
     raw = _stream(stream)
     with _torch.cuda.stream(_torch.cuda.ExternalStream(raw) if raw else _torch.cuda.default_stream()):
-        return adapt_workspace(In, Ker, A, Out)
+        return make()
 
 
 def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
@@ -378,7 +382,7 @@ def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
         _of(_f32, scales=scales)
     dt = _dtype(Out, In, Ker, A, B)
     if ws is None:
-        ws = _adapt_own_workspace(In, Ker, A, Out, stream)
+        ws = _own_workspace(lambda: adapt_workspace(In, Ker, A, Out), stream)
     st = (cnn._lib or cnn.lib()).cnn_adapt_fwd(
         In.data_ptr(), Ker.data_ptr(), A.data_ptr(), B.data_ptr(), ids.data_ptr(),
         0 if scales is None else scales.data_ptr(), Out.data_ptr(), Nt, Nc, Nk, Na, Nl, dt,
@@ -386,3 +390,217 @@ def adapt_fwd(In, Ker, A, B, ids, Out, scales=None, ws=None, stream=None):
     if st:
         _check(st)
     return Out
+
+
+def balance_workspace(Nt: int, Ng: int, Ns: int = 1, device=None):
+    """A workspace for ``balance`` of Nt rows, Ng experts and Ns sequences (None
+    where it needs none)."""
+    _enter()
+    n = i64()
+    _check(cnn.lib().cnn_balance_ws(Nt, Ng, Ns, ctypes.byref(n)))
+    device = _torch.device("cuda", _torch.cuda.current_device()) if device is None else device
+    return _torch.empty(n.value, dtype=_u8, device=device) if n.value else None
+
+
+def _balance_check(Logits, choice, counts, tokens, bounds, **more):
+    """Of balance and balance_bwd: Nt, Ng, Kt, Ns."""
+    here = _here()
+    Nt, Ng = _dims("Logits", Logits, 2)
+    _, Kt = _dims("choice", choice, 2)
+    Ns, _ = _dims("counts", counts, 2)
+    if not (Logits.get_device() == here == choice.get_device() == counts.get_device() == tokens.get_device()
+            and Logits.is_contiguous() and choice.is_contiguous() and counts.is_contiguous()
+            and tokens.is_contiguous() and choice.shape == (Nt, Kt) and counts.shape == (Ns, Ng)
+            and tokens.shape == (Ns,) and choice.dtype is _i32 is counts.dtype and tokens.dtype is _i32
+            and (bounds is None or (bounds.get_device() == here and bounds.is_contiguous()
+                                    and bounds.shape == (Ns + 1,) and bounds.dtype is _i32))):
+        _refuse(Logits=Logits, choice=choice, counts=counts, tokens=tokens, bounds=bounds)
+        _shape("choice", choice, Nt, Kt)
+        _shape("counts", counts, Ns, Ng)
+        _shape("tokens", tokens, Ns)
+        _of(_i32, choice=choice, counts=counts, tokens=tokens, bounds=bounds)
+        _shape("bounds", bounds, Ns + 1)
+    for name, t in more.items():
+        if not (t.get_device() == here and t.is_contiguous() and t.shape == (2,) and t.dtype is _f32):
+            _refuse(**{name: t})
+            _shape(name, t, 2)
+            _of(_f32, **{name: t})
+    return Nt, Ng, Kt, Ns
+
+
+def balance(Logits, choice, counts, tokens, loss, bounds=None, ws=None, stream=None):
+    """The choices of each expert and the losses that keep them even: for Logits
+    [Nt, Ng], the choice [Nt, Kt] that ``route`` made of them and sequences of the
+    rows [bounds[s], bounds[s + 1]) (bounds [Ns + 1] int32; None: one of all
+    rows), counts [Ns, Ng] and tokens [Ns] int32 (rows with a choice) and loss [2]
+    float32: the balance loss, 1 where the choices are even, and the mean square
+    of the rows' log-sum-exp.  ws: the tensor that ``balance_workspace`` gives,
+    kept by the caller (None: one of its own for this call, if it needs any)."""
+    here = _enter()
+    Nt, Ng, Kt, Ns = _balance_check(Logits, choice, counts, tokens, bounds, loss=loss)
+    dt = _types.get((Logits.dtype, Logits.dtype))
+    if dt is None:
+        raise ValueError("Logits must be float32 or bfloat16")
+    if ws is None:
+        ws = _own_workspace(lambda: balance_workspace(Nt, Ng, Ns), stream)
+    elif ws.get_device() != here or not ws.is_contiguous():
+        _refuse(ws=ws)
+    st = (cnn._lib or cnn.lib()).cnn_balance(
+        Logits.data_ptr(), choice.data_ptr(), 0 if bounds is None else bounds.data_ptr(),
+        counts.data_ptr(), tokens.data_ptr(), loss.data_ptr(), Nt, Ng, Kt, Ns, dt,
+        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
+        _raw(stream))
+    if st:
+        _check(st)
+    return loss
+
+
+def balance_bwd(Logits, choice, counts, tokens, dLoss, dLogits, bounds=None, add=False, stream=None):
+    """dLogits of dLoss[0] loss[0] + dLoss[1] loss[1], dLoss [2] float32 on the
+    GPU, for the counts and tokens that ``balance`` gave; add: on top of what
+    dLogits holds (what ``route_bwd`` wrote)."""
+    here = _enter()
+    Nt, Ng, Kt, Ns = _balance_check(Logits, choice, counts, tokens, bounds, dLoss=dLoss)
+    if not (dLogits.get_device() == here and dLogits.is_contiguous() and dLogits.shape == Logits.shape):
+        _refuse(dLogits=dLogits)
+        _shape("dLogits", dLogits, Nt, Ng)
+    dt = _dtype(dLogits, Logits)
+    st = (cnn._lib or cnn.lib()).cnn_balance_bwd(
+        Logits.data_ptr(), choice.data_ptr(), 0 if bounds is None else bounds.data_ptr(),
+        counts.data_ptr(), tokens.data_ptr(), dLoss.data_ptr(), dLogits.data_ptr(), Nt, Ng, Kt, Ns,
+        dt, int(bool(add)), _raw(stream))
+    if st:
+        _check(st)
+    return dLogits
+
+
+def blocks4(Nc: int) -> int:
+    """Blocks of a row of Nc values in 4 bits: 16 bytes of codes and one of scale each."""
+    return (Nc + 31) // 32
+
+
+def _four(name, codes, scales, *lead_and_blocks):
+    """Whether codes and scales are a tensor in 4 bits of this shape on this GPU;
+    if not, what is wrong."""
+    here, *lead, Nb = _here(), *lead_and_blocks
+    if not (codes.get_device() == here == scales.get_device() and codes.is_contiguous()
+            and scales.is_contiguous() and codes.dtype is _u8 is scales.dtype
+            and codes.shape == (*lead, 16 * Nb) and scales.shape == (*lead, Nb)):
+        _refuse(**{name: codes, name + "Scales": scales})
+        _of(_u8, **{name: codes, name + "Scales": scales})
+        _shape(name, codes, *lead, 16 * Nb)
+        _shape(name + "Scales", scales, *lead, Nb)
+
+
+def _logical(t):
+    """Rows (all leading sizes) and columns of a tensor of values."""
+    if t.dim() < 1:
+        raise ValueError("a row of values is at least 1-d")
+    rows = 1
+    for n in t.shape[:-1]:
+        rows *= n
+    return rows, t.shape[-1]
+
+
+def quantize4(In, Codes, Scales, rule: str = "floor", stream=None):
+    """In [.., Nc] (float32 or bfloat16) in 4 bits: Codes [.., 16 blocks4(Nc)] and
+    Scales [.., blocks4(Nc)] uint8.  rule: a block's scale is a power of two,
+    "floor" of a quarter of its largest magnitude (up to a fourth of it is cut
+    off) or "up", so that nothing is.  A block with an infinity or NaN becomes
+    NaN.  Returns Codes and Scales."""
+    here = _enter()
+    Nt, Nc = _logical(In)
+    if not (In.get_device() == here and In.is_contiguous() and rule in RULES):
+        _refuse(In=In)
+        raise ValueError(f"rule must be one of {sorted(RULES)}")
+    _four("Codes", Codes, Scales, *In.shape[:-1], blocks4(Nc))
+    dt = _types.get((In.dtype, In.dtype))
+    if dt is None:
+        raise ValueError("In must be float32 or bfloat16")
+    st = (cnn._lib or cnn.lib()).cnn_quantize4(In.data_ptr(), Codes.data_ptr(), Scales.data_ptr(), Nt,
+                                               Nc, dt, RULES[rule], _raw(stream))
+    if st:
+        _check(st)
+    return Codes, Scales
+
+
+def dequantize4(Codes, Scales, Out, stream=None):
+    """The values of a tensor in 4 bits, Out [.., Nc] float32 or bfloat16
+    (exact in both; from 2^128 on infinite)."""
+    here = _enter()
+    Nt, Nc = _logical(Out)
+    if not (Out.get_device() == here and Out.is_contiguous()):
+        _refuse(Out=Out)
+    _four("Codes", Codes, Scales, *Out.shape[:-1], blocks4(Nc))
+    dt = _types.get((Out.dtype, Out.dtype))
+    if dt is None:
+        raise ValueError("Out must be float32 or bfloat16")
+    st = (cnn._lib or cnn.lib()).cnn_dequantize4(Codes.data_ptr(), Scales.data_ptr(), Out.data_ptr(),
+                                                 Nt, Nc, dt, _raw(stream))
+    if st:
+        _check(st)
+    return Out
+
+
+def _result4(name, t):
+    if t.dtype is _torch.bfloat16:
+        return CNN_BF16_OBF16
+    if t.dtype is _f32:
+        return CNN_BF16
+    raise ValueError(f"{name} must be float32 or bfloat16")
+
+
+def group_fwd4(In, Ker, KerScales, Out, offsets, rows=None, InScales=None, stream=None):
+    """``group_fwd`` with Ker in 4 bits: Ker [Ng, Nk, 16 Nb], KerScales [Ng, Nk, Nb]
+    as ``quantize4`` makes them of [Ng, Nk, Nc].  In [Nt, Nc] bfloat16, or in 4
+    bits itself: In [Nt, 16 Nb] with InScales [Nt, Nb].  Out float32 or bfloat16."""
+    here = _enter()
+    Ng, Nk, _ = _dims("Ker", Ker, 3)
+    Np, K = _dims("Out", Out, 2)
+    Nt, Nc = _dims("In", In, 2)
+    if InScales is not None:
+        Nc = 32 * _dims("InScales", InScales, 2)[1]
+        _four("In", In, InScales, Nt, Nc // 32)
+    elif In.dtype is not _torch.bfloat16:
+        raise ValueError("In must be bfloat16, or uint8 with InScales")
+    _four("Ker", Ker, KerScales, Ng, Nk, blocks4(Nc))
+    if not (In.get_device() == here == Out.get_device() == offsets.get_device()
+            and In.is_contiguous() and Out.is_contiguous() and offsets.is_contiguous() and K == Nk
+            and offsets.shape == (Ng + 1,) and offsets.dtype is _i32
+            and (Np == Nt if rows is None else
+                 rows.get_device() == here and rows.is_contiguous() and rows.dtype is _i32
+                 and rows.shape == (Np,))):
+        _refuse(In=In, Out=Out, offsets=offsets, rows=rows)
+        _shape("Out", Out, Nt if rows is None else Np, Nk)
+        _order(offsets, rows, Np, Ng)
+    st = (cnn._lib or cnn.lib()).cnn_group_fwd4(
+        In.data_ptr(), 0 if InScales is None else InScales.data_ptr(), Ker.data_ptr(),
+        KerScales.data_ptr(), Out.data_ptr(), offsets.data_ptr(), 0 if rows is None else rows.data_ptr(),
+        Nt, Np, Ng, Nc, Nk, _result4("Out", Out), _raw(stream))
+    if st:
+        _check(st)
+    return Out
+
+
+def group_bwd_in4(dOut, Ker, KerScales, dIn, offsets, stream=None):
+    """``group_bwd_in`` with Ker in 4 bits (along c, as ``group_fwd4`` takes it):
+    dOut [Np, Nk] bfloat16, dIn [Np, Nc] float32 or bfloat16."""
+    here = _enter()
+    Np, Nk = _dims("dOut", dOut, 2)
+    Ng, _, _ = _dims("Ker", Ker, 3)
+    Nc = _dims("dIn", dIn, 2)[1]
+    _four("Ker", Ker, KerScales, Ng, Nk, blocks4(Nc))
+    if not (dOut.get_device() == here == dIn.get_device() == offsets.get_device()
+            and dOut.is_contiguous() and dIn.is_contiguous() and offsets.is_contiguous()
+            and dIn.shape == (Np, Nc) and offsets.shape == (Ng + 1,) and offsets.dtype is _i32):
+        _refuse(dOut=dOut, dIn=dIn, offsets=offsets)
+        _shape("dIn", dIn, Np, Nc)
+        _order(offsets, None, Np, Ng)
+    if dOut.dtype is not _torch.bfloat16:
+        raise ValueError("dOut must be bfloat16")
+    st = (cnn._lib or cnn.lib()).cnn_group_bwd_in4(
+        dOut.data_ptr(), Ker.data_ptr(), KerScales.data_ptr(), dIn.data_ptr(), offsets.data_ptr(), Np,
+        Ng, Nc, Nk, _result4("dIn", dIn), _raw(stream))
+    if st:
+        _check(st)
+    return dIn
