@@ -393,7 +393,7 @@ int cnn_quantize4(const void* In, uint8_t* Codes, uint8_t* Scales, int64_t Nt, i
     if ((st = check_sizes(s)) || (st = check_type(dtype))) return st;
     if (rule != CNN_SCALE_FLOOR && rule != CNN_SCALE_UP) return fail(CNN_E_UNSUPPORTED, "unknown rule %d", rule);
     const Buf in[] = {{"In", In, Nt * Nc, in_bytes(dtype)}};
-    const Buf out[] = {{"Codes", Codes, Nt * blocks4(Nc), 16}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
+    const Buf out[] = {{"Codes", Codes, Nt * blocks4(Nc) * 16, 1}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
     if ((st = check_codes("Codes", Codes)) || (st = check_bufs(in, out))) return st;
     if (!Nt) return (int)CNN_OK;
     return launched(launch_quantize4(In, Codes, Scales, Nt, Nc, dtype != CNN_F32, rule == CNN_SCALE_UP,
@@ -407,7 +407,7 @@ int cnn_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void* Out, int6
     const Size s[] = {{"Nt", Nt, 0, kRows}, {"Nc", Nc, 1, kFeatures}};
     int st;
     if ((st = check_sizes(s)) || (st = check_type(dtype))) return st;
-    const Buf in[] = {{"Codes", Codes, Nt * blocks4(Nc), 16}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
+    const Buf in[] = {{"Codes", Codes, Nt * blocks4(Nc) * 16, 1}, {"Scales", Scales, Nt * blocks4(Nc), 1}};
     const Buf out[] = {{"Out", Out, Nt * Nc, in_bytes(dtype)}};
     if ((st = check_codes("Codes", Codes)) || (st = check_bufs(in, out))) return st;
     if (!Nt) return (int)CNN_OK;
@@ -424,9 +424,9 @@ int cnn_group_fwd4(const void* In, const uint8_t* InScales, const uint8_t* Ker, 
         (st = check_tiles(Np, Ng, Nk)))
       return st;
     const int64_t Nb = blocks4(Nc);
-    const Buf in[] = {{"In", In, InScales ? Nt * Nb : Nt * Nc, InScales ? 16 : 2},
+    const Buf in[] = {{"In", In, InScales ? Nt * Nb * 16 : Nt * Nc, InScales ? 1 : 2},
                       {"InScales", InScales, InScales ? Nt * Nb : 0, 1},
-                      {"Ker", Ker, product(Ng, Nk, Nb), 16}, {"KerScales", KerScales, product(Ng, Nk, Nb), 1},
+                      {"Ker", Ker, product(Ng, Nk, 16 * Nb), 1}, {"KerScales", KerScales, product(Ng, Nk, Nb), 1},
                       {"Offsets", Offsets, Ng + 1, 4}, {"Rows", Rows, Rows ? Np : 0, 4}};
     const Buf out[] = {{"Out", Out, Np * Nk, out_bytes(dtype)}};
     if ((st = check_codes("Ker", Ker)) || (InScales && (st = check_codes("In", In))) ||
@@ -454,7 +454,7 @@ int cnn_group_bwd_in4(const void* dOut, const uint8_t* Ker, const uint8_t* KerSc
         (st = check_tiles(Np, Ng, Nc)))
       return st;
     const int64_t Nb = blocks4(Nc);
-    const Buf in[] = {{"dOut", dOut, Np * Nk, 2}, {"Ker", Ker, product(Ng, Nk, Nb), 16},
+    const Buf in[] = {{"dOut", dOut, Np * Nk, 2}, {"Ker", Ker, product(Ng, Nk, 16 * Nb), 1},
                       {"KerScales", KerScales, product(Ng, Nk, Nb), 1}, {"Offsets", Offsets, Ng + 1, 4}};
     const Buf out[] = {{"dIn", dIn, Np * Nc, out_bytes(dtype)}};
     if ((st = check_codes("Ker", Ker)) || (st = check_bufs(in, out))) return st;
