@@ -1,5 +1,6 @@
 // Launches of the grouped products whose Ker lies in 4 bits (group4_kernel.h).
-#include "group4_kernel.h"
+#include "group4_pipe.h"
+#include <stdlib.h>
 
 namespace cnnlib {
 
@@ -7,8 +8,8 @@ namespace {
 
 using namespace group;
 
-// The largest tile of which the launch has one for every CU.
-int pick_tile4(const GroupArgs& a) {
+int pick_tile4(const GroupArgs& a, bool pipe) {
+  if (const char* e = getenv("CNN_T4")) { int t = atoi(e); return t == 256 && !pipe ? 128 : t; }
   const int sizes[] = {128, 64};
   for (int t : sizes)
     if (((a.M + t - 1) / t) * ((int64_t)a.N / t + (a.Ng < a.N ? a.Ng : a.N)) >= device_cus()) return t;
@@ -17,16 +18,23 @@ int pick_tile4(const GroupArgs& a) {
 
 template <typename TO, int MODE>
 hipError_t launch_sized4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
-  const int t = pick_tile4(a);
+  const bool pipe = ((uintptr_t)a.Y & 3) == 0 && a.ldy % 2 == 0 && a.K % 8 == 0 && (MODE != kFwd || (b.Nb % 4 == 0 && ((uintptr_t)b.xs & 3) == 0)) && pipe4_fits(a, MODE);
+  const int t = pick_tile4(a, pipe);
+  if (t == 256) return launch_pipe4<TO, MODE>(a, b, row_tiles(a.N, a.Ng, true, 256), 4, stream);
   if (t == 128) return launch_tiles4<TO, MODE, 128, 128>(a, b, row_tiles(a.N, a.Ng, true, 128), 8, stream);
   if (t == 64) return launch_tiles4<TO, MODE, 64, 64>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
+  if (t == 65) return launch_tiles4<TO, MODE, 64, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
+  if (t == 129) return launch_tiles4<TO, MODE, 128, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
   return launch_tiles4<TO, MODE, 32, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
 }
 
 template <typename TO> hipError_t launch_sized44(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
-  const int t = pick_tile4(a);
+  const int t = pick_tile4(a, pipe4_fits(a, kFwd) && b.Nb % 4 == 0 && (((uintptr_t)b.xs | (uintptr_t)b.ys) & 3) == 0);
+  if (t == 256) return launch_pipe44<TO>(a, b, row_tiles(a.N, a.Ng, true, 256), 4, stream);
   if (t == 128) return launch_tiles44<TO, 128, 128, 2, 2, 2>(a, b, row_tiles(a.N, a.Ng, true, 128), 8, stream);
   if (t == 64) return launch_tiles44<TO, 64, 64, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
+  if (t == 65) return launch_tiles44<TO, 64, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
+  if (t == 129) return launch_tiles44<TO, 128, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
   return launch_tiles44<TO, 32, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
 }
 
