@@ -25,7 +25,7 @@ SOURCES = ["cnn_api.cpp", "cnn_select.cpp", "k_direct.hip", "k_igemm.hip", "k_ig
            "k_srows.hip", "k_cslice.hip", "k_small.hip", "k_tile.hip", "k_tile_f32.hip",
            "k_tile_3x3_bf16.hip", "k_tile_3x3_obf16.hip", "k_tile_any_bf16.hip",
            "k_tile_any_obf16.hip", "cnn_static.hip", "routed_api.cpp", "k_route.hip",
-           "k_combine.hip", "k_group.hip", "k_few.hip", "k_balance.hip", "k_block4.hip", "k_group4.hip"]
+           "k_combine.hip", "k_group.hip", "k_few.hip", "k_balance.hip", "k_block4.hip", "k_group4.hip", "k_few4.hip"]
 
 ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

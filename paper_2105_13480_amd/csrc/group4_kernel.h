@@ -32,6 +32,21 @@ __device__ __forceinline__ u32x4_t bf16_of4(uint32_t code, float scale) {
 #endif
 }
 
+// Bytes [0, n) from p on, both on 4-byte boundaries (rsrc_words: at any).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t n) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)n, 0x00020000);
+}
+__device__ __forceinline__ void buffer_lds(__amdgpu_buffer_rsrc_t r, u32x4_t* lds, uint32_t voff, uint32_t soff) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDS_AS(void, lds), 16, (int)voff, (int)soff, 0, 0);
+#else
+  (void)r;
+  (void)lds;
+  (void)voff;
+  (void)soff;
+#endif
+}
+
 // Stages R rows of features by 64 of k (KC) or 64 rows of k by R of c of a Ker in
 // 4 bits as bf16: a thread takes half blocks (8 bytes, 16 values).
 template <bool KC, int R, int NT> struct Stager4 {
@@ -194,22 +209,30 @@ hipError_t launch_tiles4(const GroupArgs& a, const Group4Args& b, int64_t row_ti
 // values a block are, straight to LDS, and a stage of 128 bytes holds 256 values.
 // Lane l takes blocks 2 (l / 16) and the next, whose two scales it loads at once;
 // the other operand's lane takes the same.
-template <int NB> struct Scales4 {
-  const uint8_t* p[NB];  // this lane's rows
+template <int NB, bool BUF> struct Scales4 {
+  const uint8_t* p[BUF ? 1 : NB];  // this lane's rows
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t off[BUF ? NB : 1];
 
-  // Scales of blocks `at` and the next of rows of Nb; past their end 2^-127 (the
-  // codes there are zeros).
+  // Scales of blocks `at` and the next of rows of Nb (2 at least with BUF, whose loads
+  // know no branch), as load() found them; cut() clears what lies past the rows' end
+  // (2^-127: the codes there are zeros).
   __device__ __forceinline__ void load(int at, int Nb, uint32_t (&s)[NB]) const {
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      if (at + 1 < Nb) {
-        uint16_t v;
-        __builtin_memcpy(&v, p[i] + at, 2);
-        s[i] = v;
+      if constexpr (BUF) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        s[i] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, (int)(off[i] + min(at, Nb - 2)), 0, 0);
+#endif
       } else {
-        s[i] = at < Nb ? p[i][at] : 0u;
+        s[i] = at + 1 < Nb ? (uint32_t)p[i][at] | (uint32_t)p[i][at + 1] << 8 : at < Nb ? p[i][at] : 0u;
       }
     }
+  }
+  __device__ __forceinline__ void cut(int at, int Nb, uint32_t (&s)[NB]) const {
+    if constexpr (BUF)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) s[i] = at + 2 <= Nb ? s[i] : at < Nb ? s[i] >> 8 : 0u;
   }
 };
 
@@ -229,12 +252,17 @@ __device__ __forceinline__ f32x4_t mma4(u32x4_t x, u32x4_t y, f32x4_t acc, uint3
 #endif
 }
 
-template <typename TO, int TM, int TN, int WM, int WN, int DEPTH>
+// BUF: operands by buffer instructions (at most 2^31 bytes of each, two blocks a row at
+// least); copies with addresses of their own beside loads make the compiler wait for
+// all of both where it needs one.
+template <typename TO, int TM, int TN, int WM, int WN, int DEPTH, bool BUF>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Group4Args b, int band) {
   typedef bf16_t T;
   constexpr int NT = 64 * WM * WN, TK = 64;  // of 16-bit words: 256 values
   constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
   constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
+  constexpr int NX = XU / NT, NY = 8 * TN / NT;  // units a thread copies
+  static_assert(XU % NT == 0 && 8 * TN % NT == 0, "whole rounds");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   u32x4_t* const ring = reinterpret_cast<u32x4_t*>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -246,10 +274,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
   Tile<T, TO> w;
   if (!setup_tile<T, TO, kFwd, TM, TN>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
-  Stager<T, true, TM, NT, false> sx;
-  Stager<T, true, TN, NT, true> sy;
-  Scales4<NI> px;
-  Scales4<NJ> py;
 
   f32x4_t acc[NI][NJ];
 #pragma unroll
@@ -258,27 +282,64 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   if (w.K > 0) {
-    sx.init(tid, w.X, a.ldx, w.m0, w.m_valid, nullptr, 0);
-    sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, w.rows, a.Nsrc);
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-      px.p[i] = b.xs + (g * a.M + w.m0 + min(xrow(i) + l16, w.m_valid - 1)) * b.Nb;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      int64_t r = w.n0 + min(yrow(j) + l16, w.n_valid - 1);
+    const int Nb = b.Nb;
+    const int64_t x0 = g * a.M + w.m0;
+    // the row of Y of a row of the tile
+    auto source = [&](int n) __attribute__((always_inline)) -> int64_t {
+      int64_t r = w.n0 + min(n, w.n_valid - 1);
       if (w.rows) {
         r = w.rows[r];
         if (r < 0 || r >= a.Nsrc) r = 0;
       }
-      py.p[j] = b.ys + r * b.Nb;
+      return r;
+    };
+    // this thread's unit column, and its rows NT / 8 by NT / 8
+    const int r0 = tid >> 3, c8 = 8 * ((tid & 7) ^ ((r0 >> 1) & 7));
+    static_assert((NT / 8) % 16 == 0, "one unit column in all rows");
+    const T* const X = reinterpret_cast<const T*>(a.X) + x0 * a.ldx + c8;
+    const T* const Y = reinterpret_cast<const T*>(a.Y) + c8;
+    __amdgpu_buffer_rsrc_t xr, yr;
+    int64_t yat[NY];
+    uint32_t xoff = 0;
+#pragma unroll
+    for (int j = 0; j < NY; ++j) yat[j] = source(r0 + j * (NT / 8)) * a.ldy;
+    Scales4<NI, BUF> px;
+    Scales4<NJ, BUF> py;
+    if constexpr (BUF) {
+      xr = rsrc_of(reinterpret_cast<const T*>(a.X) + x0 * a.ldx, (int64_t)w.m_valid * a.ldx * 2);
+      yr = rsrc_of(a.Y, (int64_t)a.Nsrc * a.ldy * 2);
+      px.rsrc = rsrc_words(b.xs + x0 * Nb, (int64_t)w.m_valid * Nb);
+      py.rsrc = rsrc_words(b.ys, (int64_t)a.Nsrc * Nb);
+      xoff = (uint32_t)((r0 * a.ldx + c8) * 2);
     }
-    constexpr int COPIES = sx.NU + sy.NU;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int m = min(xrow(i) + l16, w.m_valid - 1);
+      if constexpr (BUF) px.off[i] = (uint32_t)(m * Nb);
+      else px.p[i] = b.xs + (x0 + m) * Nb;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t r = source(yrow(j) + l16);
+      if constexpr (BUF) py.off[j] = (uint32_t)(r * Nb);
+      else py.p[j] = b.ys + r * Nb;
+    }
     const int n_st = (w.K + TK - 1) / TK;
+    // past K zeros, so that every wait counts the same
     auto copy = [&](int s) __attribute__((always_inline)) {
-      u32x4_t* const dst = ring + (s % DEPTH) * STAGE;
-      const int K = s < n_st ? w.K : 0;
-      sx.copy(tid, dst, s * TK, a.ldx, K, nullptr, 0);
-      sy.copy(tid, dst + XU, s * TK, a.ldy, K, nullptr, 0);
+      u32x4_t* const dst = ring + (s % DEPTH) * STAGE + 64 * wave;
+      const bool ok = s * TK + c8 < w.K;
+#pragma unroll
+      for (int j = 0; j < NX; ++j) {
+        const int row = j * (NT / 8);
+        if constexpr (BUF) buffer_lds(xr, dst + j * NT, ok ? xoff : ~0u, (uint32_t)((row * a.ldx + s * TK) * 2));
+        else copy16_lds(ok ? (const void*)(X + (int64_t)min(row + r0, w.m_valid - 1) * a.ldx + s * TK) : (const void*)zero_unit, dst + j * NT);
+      }
+#pragma unroll
+      for (int j = 0; j < NY; ++j) {
+        if constexpr (BUF) buffer_lds(yr, dst + XU + j * NT, ok ? (uint32_t)((yat[j] + c8) * 2) : ~0u, (uint32_t)(2 * s * TK));
+        else copy16_lds(ok ? (const void*)(Y + yat[j] + s * TK) : (const void*)zero_unit, dst + XU + j * NT);
+      }
     };
     uint32_t at[2][2];  // LDS bytes of this lane's units, by sub-step
 #pragma unroll
@@ -286,15 +347,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
       at[0][ks] = 16 * unit_at<T, true, TM>(xrow(0) + l16, 2 * G + ks);
       at[1][ks] = 16 * unit_at<T, true, TN>(yrow(0) + l16, 2 * G + ks);
     }
+    uint32_t fx[2][NI], fy[2][NJ];  // scales of this stage and the next
+    px.load(2 * G, Nb, fx[0]);
+    py.load(2 * G, Nb, fy[0]);
 #pragma unroll
     for (int s = 0; s < DEPTH - 1; ++s) copy(s);
-    for (int s = 0; s < n_st; ++s) {
-      uint32_t fx[NI], fy[NJ];
-      px.load(8 * s + 2 * G, b.Nb, fx);
-      py.load(8 * s + 2 * G, b.Nb, fy);
-      // stage s has landed (the later ones' copies and the scales may be in flight);
-      // every wave is done with stage s - 1
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COPIES * (DEPTH - 2)) : "memory");
+    auto step = [&](auto set, auto first, int s) __attribute__((always_inline)) {
+      constexpr int S = set.value;
+      // stage s has landed (the later ones' copies, and the scales that were asked for
+      // with them but for the first, may be in flight); every wave is done with stage s - 1
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((DEPTH - 2) * (NX + NY + (BUF && !first.value ? NI + NJ : 0))) : "memory");
+      px.load(8 * s + 8 + 2 * G, Nb, fx[1 - S]);
+      py.load(8 * s + 8 + 2 * G, Nb, fy[1 - S]);
       copy(s + DEPTH - 1);
       const char* const buf = reinterpret_cast<const char*>(ring + (s % DEPTH) * STAGE);
       u32x4_t xf[NI][2], yf[NJ][2];
@@ -305,22 +369,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
 #pragma unroll
         for (int j = 0; j < NJ; ++j) yf[j][ks] = *reinterpret_cast<const u32x4_t*>(buf + 16 * XU + at[1][ks] + 2048 * j);
       }
+      px.cut(8 * s + 2 * G, Nb, fx[S]);
+      py.cut(8 * s + 2 * G, Nb, fy[S]);
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          acc[i][j] = mma4<0>(xf[i][0], yf[j][0], acc[i][j], fx[i], fy[j]);
-          acc[i][j] = mma4<1>(xf[i][1], yf[j][1], acc[i][j], fx[i], fy[j]);
+          acc[i][j] = mma4<0>(xf[i][0], yf[j][0], acc[i][j], fx[S][i], fy[S][j]);
+          acc[i][j] = mma4<1>(xf[i][1], yf[j][1], acc[i][j], fx[S][i], fy[S][j]);
         }
+    };
+    static_assert(DEPTH <= 4, "two first stages");
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    constexpr std::integral_constant<bool, true> first;
+    constexpr std::integral_constant<bool, false> later;
+    step(even, first, 0);
+    if (n_st > 1) step(odd, first, 1);
+    int s = 2;
+    for (; s + 2 <= n_st; s += 2) {
+      step(even, later, s);
+      step(odd, later, s + 1);
     }
+    if (s < n_st) step(even, later, s);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the trailing (empty) copies
   }
   store_tile<T, TO, kFwd, true>(a, w, lane, acc, xrow, yrow);
 }
 
-template <typename TO, int TM, int TN, int WM, int WN, int DEPTH>
+template <typename TO, int TM, int TN, int WM, int WN, int DEPTH, bool BUF = true>
 hipError_t launch_tiles44(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
-  auto* const k = group44_tiles<TO, TM, TN, WM, WN, DEPTH>;
+  auto* const k = group44_tiles<TO, TM, TN, WM, WN, DEPTH, BUF>;
   const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
   const hipError_t fit = grid_fits(grid, 64 * WM * WN);
   if (fit != hipSuccess) return fit;

@@ -12,20 +12,6 @@
 namespace cnnlib {
 namespace group {
 
-// Bytes [0, n) from p on, p on a 4-byte boundary where it is copied to LDS.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t n) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)n, 0x00020000);
-}
-__device__ __forceinline__ void buffer_lds(__amdgpu_buffer_rsrc_t r, u32x4_t* lds, uint32_t voff, uint32_t soff) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDS_AS(void, lds), 16, (int)voff, (int)soff, 0, 0);
-#else
-  (void)r;
-  (void)lds;
-  (void)voff;
-  (void)soff;
-#endif
-}
 __device__ __forceinline__ void write_lds(uint32_t at, u32x4_t v) {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");
@@ -116,7 +102,7 @@ struct PipeKer4 {
     const int k = tid >> 3, g = (k & 3) | ((k >> 1) & 4);
     Nb = Nb_;
     codes = rsrc_of(c4 + m0 / 2, (int64_t)K * 16 * Nb - m0 / 2);
-    scales = rsrc_of(s4 + m0 / 32, (int64_t)K * Nb - m0 / 32);
+    scales = rsrc_words(s4 + m0 / 32, (int64_t)K * Nb - m0 / 32);
     dst = (uint32_t)(16 * (k * 16 + ((2 * (tid & 7)) ^ (g << 1))));
   }
   // Asks for half h of the stage at k0; past K zeros.
@@ -216,7 +202,7 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
     // this thread's part of X: 16 bytes of row tid / 2; and a row's four scales
     const int64_t x0 = g * a.M + w.m0;
     const __amdgpu_buffer_rsrc_t xr = rsrc_of(reinterpret_cast<const uint8_t*>(a.X) + x0 * 16 * b.Nb, (int64_t)w.m_valid * 16 * b.Nb);
-    const __amdgpu_buffer_rsrc_t sr = rsrc_of(b.xs + x0 * b.Nb, (int64_t)w.m_valid * b.Nb);
+    const __amdgpu_buffer_rsrc_t sr = rsrc_words(b.xs + x0 * b.Nb, (int64_t)w.m_valid * b.Nb);
     const uint32_t xoff = (uint32_t)((tid >> 1) * 16 * b.Nb + 16 * (tid & 1));
     // X of stage s, past the row's end zeros
     auto copy_x = [&](auto check, int s) __attribute__((always_inline)) {
@@ -477,14 +463,14 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
     __amdgpu_buffer_rsrc_t srsrc;
     uint32_t soff = (uint32_t)((tid & 255) * b.Nb);
     if (wave < 4) {
-      srsrc = rsrc_of(b.xs + (g * a.M + w.m0) * b.Nb, (int64_t)w.m_valid * b.Nb);
+      srsrc = rsrc_words(b.xs + (g * a.M + w.m0) * b.Nb, (int64_t)w.m_valid * b.Nb);
     } else if (w.rows) {
       int r = w.rows[w.n0 + min(tid & 255, w.n_valid - 1)];
       if (r < 0 || r >= a.Nsrc) r = 0;
       soff = (uint32_t)(r * b.Nb);
-      srsrc = rsrc_of(b.ys, (int64_t)a.Nsrc * b.Nb);
+      srsrc = rsrc_words(b.ys, (int64_t)a.Nsrc * b.Nb);
     } else {
-      srsrc = rsrc_of(b.ys + (int64_t)w.n0 * b.Nb, (int64_t)w.n_valid * b.Nb);
+      srsrc = rsrc_words(b.ys + (int64_t)w.n0 * b.Nb, (int64_t)w.n_valid * b.Nb);
     }
     auto copy_scales = [&](int pair) __attribute__((always_inline)) {  // of stages 2 pair, 2 pair + 1
       buffer_lds(srsrc, lds + kPipeLds / 16 + (pair & 1) * 512 + 64 * wave, soff, (uint32_t)(16 * pair));

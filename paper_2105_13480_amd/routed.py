@@ -402,30 +402,30 @@ def balance_workspace(Nt: int, Ng: int, Ns: int = 1, device=None):
     return _torch.empty(n.value, dtype=_u8, device=device) if n.value else None
 
 
-def _balance_check(Logits, choice, counts, tokens, bounds, **more):
-    """Of balance and balance_bwd: Nt, Ng, Kt, Ns."""
-    here = _here()
-    Nt, Ng = _dims("Logits", Logits, 2)
-    _, Kt = _dims("choice", choice, 2)
-    Ns, _ = _dims("counts", counts, 2)
-    if not (Logits.get_device() == here == choice.get_device() == counts.get_device() == tokens.get_device()
+def _balance_check(here, Logits, choice, counts, tokens, bounds, name, pair):
+    """Of balance and balance_bwd (pair: the two losses or their gradients): Nt, Ng,
+    Kt, Ns."""
+    shape, pairs, table = Logits.shape, choice.shape, counts.shape
+    if (Logits.get_device() == here == choice.get_device() == counts.get_device() == tokens.get_device() ==
+            pair.get_device() and len(shape) == 2 == len(pairs) and len(table) == 2 and pairs[0] == shape[0]
+            and table[1] == shape[1] and tokens.shape == (table[0],) and pair.shape == (2,)
+            and choice.dtype is _i32 is counts.dtype and tokens.dtype is _i32 and pair.dtype is _f32
             and Logits.is_contiguous() and choice.is_contiguous() and counts.is_contiguous()
-            and tokens.is_contiguous() and choice.shape == (Nt, Kt) and counts.shape == (Ns, Ng)
-            and tokens.shape == (Ns,) and choice.dtype is _i32 is counts.dtype and tokens.dtype is _i32
+            and tokens.is_contiguous() and pair.is_contiguous()
             and (bounds is None or (bounds.get_device() == here and bounds.is_contiguous()
-                                    and bounds.shape == (Ns + 1,) and bounds.dtype is _i32))):
-        _refuse(Logits=Logits, choice=choice, counts=counts, tokens=tokens, bounds=bounds)
-        _shape("choice", choice, Nt, Kt)
-        _shape("counts", counts, Ns, Ng)
-        _shape("tokens", tokens, Ns)
-        _of(_i32, choice=choice, counts=counts, tokens=tokens, bounds=bounds)
-        _shape("bounds", bounds, Ns + 1)
-    for name, t in more.items():
-        if not (t.get_device() == here and t.is_contiguous() and t.shape == (2,) and t.dtype is _f32):
-            _refuse(**{name: t})
-            _shape(name, t, 2)
-            _of(_f32, **{name: t})
-    return Nt, Ng, Kt, Ns
+                                    and bounds.shape == (table[0] + 1,) and bounds.dtype is _i32))):
+        return shape[0], shape[1], pairs[1], table[0]
+    Nt, Ng = _dims("Logits", Logits, 2)
+    Kt = _dims("choice", choice, 2)[1]
+    Ns = _dims("counts", counts, 2)[0]
+    _refuse(Logits=Logits, choice=choice, counts=counts, tokens=tokens, bounds=bounds, **{name: pair})
+    _shape("choice", choice, Nt, Kt)
+    _shape("counts", counts, Ns, Ng)
+    _shape("tokens", tokens, Ns)
+    _shape(name, pair, 2)
+    _of(_i32, choice=choice, counts=counts, tokens=tokens, bounds=bounds)
+    _of(_f32, **{name: pair})
+    _shape("bounds", bounds, Ns + 1)
 
 
 def balance(Logits, choice, counts, tokens, loss, bounds=None, ws=None, stream=None):
@@ -437,7 +437,7 @@ def balance(Logits, choice, counts, tokens, loss, bounds=None, ws=None, stream=N
     of the rows' log-sum-exp.  ws: the tensor that ``balance_workspace`` gives,
     kept by the caller (None: one of its own for this call, if it needs any)."""
     here = _enter()
-    Nt, Ng, Kt, Ns = _balance_check(Logits, choice, counts, tokens, bounds, loss=loss)
+    Nt, Ng, Kt, Ns = _balance_check(here, Logits, choice, counts, tokens, bounds, "loss", loss)
     dt = _types.get((Logits.dtype, Logits.dtype))
     if dt is None:
         raise ValueError("Logits must be float32 or bfloat16")
@@ -460,7 +460,7 @@ def balance_bwd(Logits, choice, counts, tokens, dLoss, dLogits, bounds=None, add
     GPU, for the counts and tokens that ``balance`` gave; add: on top of what
     dLogits holds (what ``route_bwd`` wrote)."""
     here = _enter()
-    Nt, Ng, Kt, Ns = _balance_check(Logits, choice, counts, tokens, bounds, dLoss=dLoss)
+    Nt, Ng, Kt, Ns = _balance_check(here, Logits, choice, counts, tokens, bounds, "dLoss", dLoss)
     if not (dLogits.get_device() == here and dLogits.is_contiguous() and dLogits.shape == Logits.shape):
         _refuse(dLogits=dLogits)
         _shape("dLogits", dLogits, Nt, Ng)
@@ -479,27 +479,28 @@ def blocks4(Nc: int) -> int:
     return (Nc + 31) // 32
 
 
-def _four(name, codes, scales, *lead_and_blocks):
-    """Whether codes and scales are a tensor in 4 bits of this shape on this GPU;
-    if not, what is wrong."""
-    here, *lead, Nb = _here(), *lead_and_blocks
-    if not (codes.get_device() == here == scales.get_device() and codes.is_contiguous()
-            and scales.is_contiguous() and codes.dtype is _u8 is scales.dtype
-            and codes.shape == (*lead, 16 * Nb) and scales.shape == (*lead, Nb)):
+def _four(here, name, codes, scales, lead, Nb):
+    """Refuses what is no tensor in 4 bits of sizes `lead` and Nb blocks on this GPU."""
+    if not (codes.get_device() == here == scales.get_device() and codes.dtype is _u8 is scales.dtype
+            and codes.shape == (*lead, 16 * Nb) and scales.shape == (*lead, Nb)
+            and codes.is_contiguous() and scales.is_contiguous()):
         _refuse(**{name: codes, name + "Scales": scales})
         _of(_u8, **{name: codes, name + "Scales": scales})
         _shape(name, codes, *lead, 16 * Nb)
         _shape(name + "Scales", scales, *lead, Nb)
 
 
-def _logical(t):
-    """Rows (all leading sizes) and columns of a tensor of values."""
-    if t.dim() < 1:
-        raise ValueError("a row of values is at least 1-d")
-    rows = 1
-    for n in t.shape[:-1]:
+def _rows_of(name, t):
+    """Leading sizes, their product and columns of a tensor of values."""
+    shape = t.shape
+    if not shape:
+        raise ValueError(f"{name} must be at least 1-d")
+    if len(shape) == 2:
+        return shape[:1], shape[0], shape[1]
+    lead, rows = shape[:-1], 1
+    for n in lead:
         rows *= n
-    return rows, t.shape[-1]
+    return lead, rows, shape[-1]
 
 
 def quantize4(In, Codes, Scales, rule: str = "floor", stream=None):
@@ -509,11 +510,11 @@ def quantize4(In, Codes, Scales, rule: str = "floor", stream=None):
     off) or "up", so that nothing is.  A block with an infinity or NaN becomes
     NaN.  Returns Codes and Scales."""
     here = _enter()
-    Nt, Nc = _logical(In)
+    lead, Nt, Nc = _rows_of("In", In)
     if not (In.get_device() == here and In.is_contiguous() and rule in RULES):
         _refuse(In=In)
         raise ValueError(f"rule must be one of {sorted(RULES)}")
-    _four("Codes", Codes, Scales, *In.shape[:-1], blocks4(Nc))
+    _four(here, "Codes", Codes, Scales, lead, (Nc + 31) // 32)
     dt = _types.get((In.dtype, In.dtype))
     if dt is None:
         raise ValueError("In must be float32 or bfloat16")
@@ -528,10 +529,10 @@ def dequantize4(Codes, Scales, Out, stream=None):
     """The values of a tensor in 4 bits, Out [.., Nc] float32 or bfloat16
     (exact in both; from 2^128 on infinite)."""
     here = _enter()
-    Nt, Nc = _logical(Out)
+    lead, Nt, Nc = _rows_of("Out", Out)
     if not (Out.get_device() == here and Out.is_contiguous()):
         _refuse(Out=Out)
-    _four("Codes", Codes, Scales, *Out.shape[:-1], blocks4(Nc))
+    _four(here, "Codes", Codes, Scales, lead, (Nc + 31) // 32)
     dt = _types.get((Out.dtype, Out.dtype))
     if dt is None:
         raise ValueError("Out must be float32 or bfloat16")
@@ -560,10 +561,10 @@ def group_fwd4(In, Ker, KerScales, Out, offsets, rows=None, InScales=None, strea
     Nt, Nc = _dims("In", In, 2)
     if InScales is not None:
         Nc = 32 * _dims("InScales", InScales, 2)[1]
-        _four("In", In, InScales, Nt, Nc // 32)
+        _four(here, "In", In, InScales, (Nt,), Nc // 32)
     elif In.dtype is not _torch.bfloat16:
         raise ValueError("In must be bfloat16, or uint8 with InScales")
-    _four("Ker", Ker, KerScales, Ng, Nk, blocks4(Nc))
+    _four(here, "Ker", Ker, KerScales, (Ng, Nk), (Nc + 31) // 32)
     if not (In.get_device() == here == Out.get_device() == offsets.get_device()
             and In.is_contiguous() and Out.is_contiguous() and offsets.is_contiguous() and K == Nk
             and offsets.shape == (Ng + 1,) and offsets.dtype is _i32
@@ -589,7 +590,7 @@ def group_bwd_in4(dOut, Ker, KerScales, dIn, offsets, stream=None):
     Np, Nk = _dims("dOut", dOut, 2)
     Ng, _, _ = _dims("Ker", Ker, 3)
     Nc = _dims("dIn", dIn, 2)[1]
-    _four("Ker", Ker, KerScales, Ng, Nk, blocks4(Nc))
+    _four(here, "Ker", Ker, KerScales, (Ng, Nk), (Nc + 31) // 32)
     if not (dOut.get_device() == here == dIn.get_device() == offsets.get_device()
             and dOut.is_contiguous() and dIn.is_contiguous() and offsets.is_contiguous()
             and dIn.shape == (Np, Nc) and offsets.shape == (Ng + 1,) and offsets.dtype is _i32):
