@@ -32,6 +32,10 @@ __device__ __forceinline__ u32x4_t bf16_of4(uint32_t code, float scale) {
 #endif
 }
 
+// An offset past the end of any buffer here (2^31 bytes at most), also with a scalar
+// offset on top: it reads zeros.
+constexpr uint32_t kNowhere = 0x80000000u;
+
 // Bytes [0, n) from p on, both on 4-byte boundaries (rsrc_words: at any).
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t n) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)n, 0x00020000);
@@ -332,12 +336,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
 #pragma unroll
       for (int j = 0; j < NX; ++j) {
         const int row = j * (NT / 8);
-        if constexpr (BUF) buffer_lds(xr, dst + j * NT, ok ? xoff : ~0u, (uint32_t)((row * a.ldx + s * TK) * 2));
+        if constexpr (BUF) buffer_lds(xr, dst + j * NT, ok ? xoff : kNowhere, (uint32_t)((row * a.ldx + s * TK) * 2));
         else copy16_lds(ok ? (const void*)(X + (int64_t)min(row + r0, w.m_valid - 1) * a.ldx + s * TK) : (const void*)zero_unit, dst + j * NT);
       }
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
-        if constexpr (BUF) buffer_lds(yr, dst + XU + j * NT, ok ? (uint32_t)((yat[j] + c8) * 2) : ~0u, (uint32_t)(2 * s * TK));
+        if constexpr (BUF) buffer_lds(yr, dst + XU + j * NT, ok ? (uint32_t)((yat[j] + c8) * 2) : kNowhere, (uint32_t)(2 * s * TK));
         else copy16_lds(ok ? (const void*)(Y + yat[j] + s * TK) : (const void*)zero_unit, dst + XU + j * NT);
       }
     };

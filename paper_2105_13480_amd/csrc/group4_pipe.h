@@ -81,7 +81,7 @@ template <bool GATHER> struct PipeRows {
     const bool ok = !CHECK || k0 + c8 < K;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      buffer_lds(rsrc, dst + 512 * j, ok ? off[GATHER ? 2 * h + j : 0] : ~0u,
+      buffer_lds(rsrc, dst + 512 * j, ok ? off[GATHER ? 2 * h + j : 0] : kNowhere,
                  (uint32_t)(2 * k0) + (GATHER ? 0u : (2 * h + j) * step));
   }
 };
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
     // X of stage s, past the row's end zeros
     auto copy_x = [&](auto check, int s) __attribute__((always_inline)) {
       const bool ok = !check.value || 64 * s + 32 * (tid & 1) < Kx;
-      buffer_lds(xr, lds + (kPipe4Codes + (s & 3) * 8192) / 16 + 64 * wave, ok ? xoff : ~0u, 32u * s);
+      buffer_lds(xr, lds + (kPipe4Codes + (s & 3) * 8192) / 16 + 64 * wave, ok ? xoff : kNowhere, 32u * s);
     };
     // the scales of stages 2 pair and the next, whole where some of it is the row's
     auto copy_scales = [&](int pair) __attribute__((always_inline)) {
@@ -576,10 +576,10 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
 
 // Whether the byte offsets of a tile's rows, of any row that may be gathered and (the
 // gradient's) of a group's Ker fit a buffer of 2^31.
+constexpr int64_t kMostBytes = (1LL << 31) - 65536;
 inline bool pipe4_fits(const GroupArgs& a, int mode) {
-  constexpr int64_t most = (1LL << 31) - 65536;
-  return a.ldx < (1 << 22) && a.ldy < (1 << 22) && (!a.rows || a.Nsrc * a.ldy * 2 < most) &&
-         (mode == kFwd || a.K * a.ldx * 2 < most);
+  return a.ldx < (1 << 22) && a.ldy < (1 << 22) && (!a.rows || a.Nsrc * a.ldy * 2 < kMostBytes) &&
+         (mode == kFwd || a.K * a.ldx * 2 < kMostBytes);
 }
 
 template <typename TO, int MODE>

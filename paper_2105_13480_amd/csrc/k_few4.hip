@@ -1,13 +1,13 @@
-// Grouped products of few rows a group with Ker in 4 bits, where Ker's bytes are the
-// bound: its codes go straight from memory to the matrix registers, since the 16 bytes
-// of a block are what one lane gives (lane l: feature l % 16, block l / 16 of 128 of k),
-// and bf16 rows are read so that each lane has the same 32 values.
+// Grouped products of bf16 rows, few a group, with Ker in 4 bits, where Ker's bytes are
+// the bound: its codes go straight from memory to the matrix registers, since the 16
+// bytes of a block are what one lane gives (lane l: feature l % 16, block l / 16 of 128
+// of k), and the rows are read so that each lane has the same 32 values.
 //
 // group4_few: 16 features by 16 rows a workgroup, whose four waves share k and add up
-// in LDS: decoding steps, where no CU has enough workgroups otherwise.
-// group4_rows: 64 or 128 features by 16 to 64 rows; each wave has its own features over
-// all of k, asked for several stages ahead, and (bf16 rows) the rows come through a ring
-// in LDS that the waves share.
+// in LDS: a few rows of long contractions (one group of 4096 x 4096, three rows: 8.0 us,
+// by group4_rows 11.8), where no CU has enough workgroups otherwise.
+// group4_rows: 64 features by 16 or 32 rows, or 128 by 64; each wave has its own features
+// over all of k, and the rows come through a ring in LDS that the waves share.
 #include "group4_kernel.h"
 
 namespace cnnlib {
@@ -34,7 +34,7 @@ template <int SB> struct Blocks4 {
 #pragma unroll
     for (int i = 0; i < SB; ++i) {
       const bool in = first + 4 * i + G < Nb;
-      code[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(in ? at + 16 * G : ~0u), 16 * first + 64 * i, 0));
+      code[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(in ? at + 16 * G : kNowhere), 16 * first + 64 * i, 0));
     }
     __builtin_memcpy(scale, scales + min(first, Nb - 4 * SB), 4 * SB);
 #endif
@@ -51,8 +51,8 @@ template <int SB> struct Blocks4 {
   }
 };
 
-// Each wave takes every fourth SB runs of k.
-template <typename TO, bool Y4, int SB>
+// Each wave takes every fourth SB runs of k; rows at any alignment.
+template <typename TO, int SB>
 __global__ __launch_bounds__(64 * kFewWaves) void group4_few(GroupArgs a, Group4Args b) {
   constexpr int NW = kFewWaves;
   __shared__ f32x4_t red[NW * 64];
@@ -73,36 +73,28 @@ __global__ __launch_bounds__(64 * kFewWaves) void group4_few(GroupArgs a, Group4
     const int m_valid = min(a.M - m0, 16), m = min(l16, m_valid - 1);
     const __amdgpu_buffer_rsrc_t xr = rsrc_of(reinterpret_cast<const uint8_t*>(a.X) + x0 * 16 * Nb, (int64_t)m_valid * 16 * Nb);
     const uint8_t* const xs = b.xs + (x0 + m) * Nb;
-    const __amdgpu_buffer_rsrc_t yr = rsrc_of(a.Y, Y4 ? (int64_t)a.Nsrc * 16 * Nb : 0);
-    const uint8_t* const ys = Y4 ? b.ys + r * Nb : nullptr;
-    const bf16_t* const y16 = Y4 ? nullptr : reinterpret_cast<const bf16_t*>(a.Y) + r * a.ldy;
+    const bf16_t* const y = reinterpret_cast<const bf16_t*>(a.Y) + r * a.ldy;
     for (int first = 4 * SB * wave; first < Nb; first += 4 * SB * NW) {
-      Blocks4<SB> x, y;
-      u32x4_t v[Y4 ? 1 : SB][4];
+      Blocks4<SB> x;
+      u32x4_t v[SB][4];
       x.load(xr, (uint32_t)(m * 16 * Nb), xs, first, G, Nb);
-      if constexpr (Y4) {
-        y.load(yr, (uint32_t)(r * 16 * Nb), ys, first, G, Nb);
-      } else if (32 * (first + 4 * SB) <= a.K) {
+      if (32 * (first + 4 * SB) <= a.K) {
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) __builtin_memcpy(&v[i][j], y16 + 32 * (first + 4 * i + G) + 8 * j, 16);
+          for (int j = 0; j < 4; ++j) __builtin_memcpy(&v[i][j], y + 32 * (first + 4 * i + G) + 8 * j, 16);
       } else {
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[i][j] = load_end(y16, 32 * (first + 4 * i + G) + 8 * j, a.K);
+          for (int j = 0; j < 4; ++j) v[i][j] = load_end(y, 32 * (first + 4 * i + G) + 8 * j, a.K);
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < SB; ++i) {
-        const uint32_t s = x.scale_of(i, first, G, Nb);
-        if constexpr (Y4) {
-          acc = mma4<0>(x.code[i], y.code[i], acc, s, y.scale_of(i, first, G, Nb));
-        } else {
+        const float s = scale4(x.scale_of(i, first, G, Nb) & 255u);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc = mma<bf16_t>(bf16_of4(x.code[i][j], scale4(s & 255u)), v[i][j], acc);
-        }
+        for (int j = 0; j < 4; ++j) acc = mma<bf16_t>(bf16_of4(x.code[i][j], s), v[i][j], acc);
       }
     }
   }
@@ -117,13 +109,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void group4_few(GroupArgs a, Group4
 }
 
 // FB blocks of 16 features a wave, RB blocks of 16 rows.  A wave asks for SB runs of k of
-// its features at a time, 64 SB bytes of each row in loads that follow one another (a run
-// at a time, 64 bytes of a row, half a line: 2.4 TB/s where this has @), and for the next
-// ones while it multiplies.  bf16 rows: a ring of four stages of 128 of k.
-template <typename TO, bool Y4, int FB, int RB, int SB>
+// its features at a time, 64 SB bytes of each row in loads that follow one another, and
+// for the next ones while it multiplies (a run at a time, 64 bytes of a row, half a
+// line: 256 rows of two of 28 groups of 4096 x 1024 27.5 us in 64 x 32 tiles, this way
+// 20.9, 3.2 TB/s; 8 rows of four of 20 of 1024 x 2048 in 64 x 16 13.1 and 9.0).  The
+// rows come through a ring of four runs.
+template <typename TO, int FB, int RB, int SB>
 __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
   constexpr int TM = 64 * FB, TN = 16 * RB, D = 4;
-  __shared__ u32x4_t ring[Y4 ? 1 : D * TN * 16];
+  __shared__ u32x4_t ring[D * TN * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   RowTile t;
   if (!find_tile<TN>(a.off, a.Ng, a.N, (a.M + TM - 1) / TM, blockIdx.x, 1, &t)) return;
@@ -150,87 +144,60 @@ __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
       xoff[f] = (uint32_t)(m * 16 * Nb);
       xs[f] = b.xs + (x0 + m) * Nb;
     }
-    // its rows in 4 bits, or this thread's units of a stage of bf16 rows
-    __amdgpu_buffer_rsrc_t yr = xr;
-    uint32_t yoff[Y4 ? RB : 1];
-    const uint8_t* ys[Y4 ? RB : 1];
-    uint32_t src[Y4 ? 1 : RB];
+    // this thread's units of a run of rows
     const int c8 = 8 * ((tid & 15) ^ (tid >> 4));
-    yr = rsrc_of(a.Y, (int64_t)a.Nsrc * (Y4 ? 16 * Nb : 2 * a.ldy));
+    const __amdgpu_buffer_rsrc_t yr = rsrc_of(a.Y, (int64_t)a.Nsrc * 2 * a.ldy);
+    uint32_t src[RB];
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
-      int64_t r = t.n0 + min(16 * i + (Y4 ? l16 : tid >> 4), n_valid - 1);
+      int64_t r = t.n0 + min(16 * i + (tid >> 4), n_valid - 1);
       if (a.rows) {
         r = a.rows[r];
         if (r < 0 || r >= a.Nsrc) r = 0;
       }
-      if constexpr (Y4) {
-        yoff[i] = (uint32_t)(r * 16 * Nb);
-        ys[i] = b.ys + r * Nb;
-      } else {
-        src[i] = (uint32_t)((r * a.ldy + c8) * 2);
-      }
+      src[i] = (uint32_t)((r * a.ldy + c8) * 2);
     }
     const int n_run = (Nb + 3) / 4;
-    Blocks4<SB> x[2][FB], y[2][Y4 ? RB : 1];
-    // the runs from `run` on
-    auto load = [&](auto set, int run) __attribute__((always_inline)) {
+    Blocks4<SB> x[2][FB];
+    auto load = [&](auto set, int run) __attribute__((always_inline)) {  // the runs from `run` on
 #pragma unroll
       for (int f = 0; f < FB; ++f) x[set.value][f].load(xr, xoff[f], xs[f], 4 * run, G, Nb);
-      if constexpr (Y4)
-#pragma unroll
-        for (int i = 0; i < RB; ++i) y[set.value][i].load(yr, yoff[i], ys[i], 4 * run, G, Nb);
     };
+    // (copies with addresses of their own, beside loads, make the compiler wait for all
+    // of both)
     auto copy_y = [&](int run) __attribute__((always_inline)) {
-      if constexpr (!Y4)
 #pragma unroll
-        for (int i = 0; i < RB; ++i)
-          // (global copies to LDS beside loads make the compiler wait for all of both)
-          buffer_lds(yr, ring + ((run & 3) * RB + i) * 256 + 64 * wave, 128 * run + c8 < a.K ? src[i] : ~0u, 256u * run);
+      for (int i = 0; i < RB; ++i)
+        buffer_lds(yr, ring + ((run & 3) * RB + i) * 256 + 64 * wave, 128 * run + c8 < a.K ? src[i] : kNowhere, 256u * run);
     };
     auto multiply = [&](auto set, auto at, int run0) __attribute__((always_inline)) {
       constexpr int I = at.value;
       const int run = run0 + I;
-      if constexpr (Y4) {
-        if (run >= n_run) return;
-        uint32_t sy[RB];
+      // the two runs before this one asked for as many copies and loads after those of
+      // this run (of the first of SB, whose codes are needed now too, the copies): it has
+      // landed, then every wave's; every wave is done with the last run
+      constexpr int X = I == 1 || I == 2 ? 1 : 0;
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * RB + X * FB * (SB + 1)) : "memory");
+      if constexpr (I == 0) load(std::integral_constant<int, 1 - set.value>{}, run0 + SB);
+      copy_y(run + 3);
+      if (run >= n_run) return;
+      u32x4_t v[RB][4];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) sy[i] = y[set.value][i].scale_of(I, 4 * run0, G, Nb);
+      for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int f = 0; f < FB; ++f) {
-          const uint32_t s = x[set.value][f].scale_of(I, 4 * run0, G, Nb);
+        for (int j = 0; j < 4; ++j) v[i][j] = ring[((run & 3) * RB + i) * 256 + 16 * l16 + ((4 * G + j) ^ l16)];
 #pragma unroll
-          for (int i = 0; i < RB; ++i)
-            acc[f][i] = mma4<0>(x[set.value][f].code[I], y[set.value][i].code[I], acc[f][i], s, sy[i]);
-        }
-      } else {
-        // the two runs before this one asked for as many copies and loads after those of
-        // this run (of the first of SB, whose codes are needed now too, the copies): it has
-        // landed, then every wave's; every wave is done with the last run
-        constexpr int X = I == 1 || I == 2 ? 1 : 0;
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * RB + X * FB * (SB + 1)) : "memory");
-        if constexpr (I == 0) load(std::integral_constant<int, 1 - set.value>{}, run0 + SB);
-        copy_y(run + 3);
-        if (run >= n_run) return;
-        u32x4_t v[RB][4];
+      for (int f = 0; f < FB; ++f) {
+        const float s = scale4(x[set.value][f].scale_of(I, 4 * run0, G, Nb) & 255u);
 #pragma unroll
-        for (int i = 0; i < RB; ++i)
+        for (int j = 0; j < 4; ++j) {
+          const u32x4_t w = bf16_of4(x[set.value][f].code[I][j], s);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[i][j] = ring[((run & 3) * RB + i) * 256 + 16 * l16 + ((4 * G + j) ^ l16)];
-#pragma unroll
-        for (int f = 0; f < FB; ++f) {
-          const float s = scale4(x[set.value][f].scale_of(I, 4 * run0, G, Nb) & 255u);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const u32x4_t w = bf16_of4(x[set.value][f].code[I][j], s);
-#pragma unroll
-            for (int i = 0; i < RB; ++i) acc[f][i] = mma<bf16_t>(w, v[i][j], acc[f][i]);
-          }
+          for (int i = 0; i < RB; ++i) acc[f][i] = mma<bf16_t>(w, v[i][j], acc[f][i]);
         }
       }
     };
     auto runs = [&](auto set, int run) __attribute__((always_inline)) {
-      if constexpr (Y4) load(std::integral_constant<int, 1 - set.value>{}, run + SB);
       multiply(set, std::integral_constant<int, 0>{}, run);
       multiply(set, std::integral_constant<int, 1>{}, run);
       if constexpr (SB == 4) {
@@ -266,56 +233,42 @@ __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
   }
 }
 
-template <typename TO, bool Y4>
-hipError_t launch_few(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
+template <typename TO> hipError_t launch_few(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
   const int64_t blocks = row_tiles(a.N, a.Ng, true, 16) * ((a.M + 15) / 16);
   const hipError_t e = grid_fits(blocks, 64 * kFewWaves);
   if (e != hipSuccess) return e;
   // some runs for each wave
-  auto* const k = b.Nb >= 64 ? group4_few<TO, Y4, 4> : group4_few<TO, Y4, 2>;
+  auto* const k = b.Nb >= 64 ? group4_few<TO, 4> : group4_few<TO, 2>;
   k<<<dim3((uint32_t)blocks), dim3(64 * kFewWaves), 0, stream>>>(a, b);
   return hipGetLastError();
 }
 
-template <typename TO, bool Y4, int FB, int RB, int SB>
+template <typename TO, int FB, int RB, int SB>
 hipError_t launch_rows(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
   const int64_t blocks = row_tiles(a.N, a.Ng, true, 16 * RB) * ((a.M + 64 * FB - 1) / (64 * FB));
   const hipError_t e = grid_fits(blocks, 256);
   if (e != hipSuccess) return e;
-  group4_rows<TO, Y4, FB, RB, SB><<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>(a, b);
+  group4_rows<TO, FB, RB, SB><<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>(a, b);
   return hipGetLastError();
 }
 
-template <typename TO, bool Y4>
-hipError_t launch_rows_sized(const GroupArgs& a, const Group4Args& b, int features, int rows, hipStream_t stream) {
-  if (features == 64) {
-    switch (rows) {
-      case 16: return launch_rows<TO, Y4, 1, 1, 4>(a, b, stream);
-      case 32: return launch_rows<TO, Y4, 1, 2, 4>(a, b, stream);
-      default: return launch_rows<TO, Y4, 1, 4, Y4 ? 2 : 4>(a, b, stream);
-    }
-  }
+template <typename TO>
+hipError_t launch_rows_sized(const GroupArgs& a, const Group4Args& b, int rows, hipStream_t stream) {
   switch (rows) {
-    case 16: return launch_rows<TO, Y4, 2, 1, 4>(a, b, stream);
-    case 32: return launch_rows<TO, Y4, 2, 2, Y4 ? 2 : 4>(a, b, stream);
-    default: return launch_rows<TO, Y4, 2, 4, 2>(a, b, stream);
+    case 16: return launch_rows<TO, 1, 1, 4>(a, b, stream);
+    case 32: return launch_rows<TO, 1, 2, 4>(a, b, stream);
+    default: return launch_rows<TO, 2, 4, 2>(a, b, stream);
   }
 }
 
 }  // namespace
 
 hipError_t launch_group4_few(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream) {
-  if (b.ys) return bf16_out ? launch_few<bf16_t, true>(a, b, stream) : launch_few<float, true>(a, b, stream);
-  return bf16_out ? launch_few<bf16_t, false>(a, b, stream) : launch_few<float, false>(a, b, stream);
+  return bf16_out ? launch_few<bf16_t>(a, b, stream) : launch_few<float>(a, b, stream);
 }
 
-hipError_t launch_group4_rows(const GroupArgs& a, const Group4Args& b, bool bf16_out, int features, int rows,
-                              hipStream_t stream) {
-  if (b.ys)
-    return bf16_out ? launch_rows_sized<bf16_t, true>(a, b, features, rows, stream)
-                    : launch_rows_sized<float, true>(a, b, features, rows, stream);
-  return bf16_out ? launch_rows_sized<bf16_t, false>(a, b, features, rows, stream)
-                  : launch_rows_sized<float, false>(a, b, features, rows, stream);
+hipError_t launch_group4_rows(const GroupArgs& a, const Group4Args& b, bool bf16_out, int rows, hipStream_t stream) {
+  return bf16_out ? launch_rows_sized<bf16_t>(a, b, rows, stream) : launch_rows_sized<float>(a, b, rows, stream);
 }
 
 }  // namespace cnnlib

@@ -1,6 +1,7 @@
-// Launches of the grouped products whose Ker lies in 4 bits (group4_kernel.h).
+// Launches of the grouped products whose Ker lies in 4 bits: which kernel and tile.
+#include <algorithm>
+
 #include "group4_pipe.h"
-#include <stdlib.h>
 
 namespace cnnlib {
 
@@ -8,62 +9,121 @@ namespace {
 
 using namespace group;
 
-int pick_tile4(const GroupArgs& a, bool pipe) {
-  if (const char* e = getenv("CNN_T4")) { int t = atoi(e); return t == 256 && !pipe ? 128 : t; }
-  const int sizes[] = {128, 64};
-  for (int t : sizes)
-    if (((a.M + t - 1) / t) * ((int64_t)a.N / t + (a.Ng < a.N ? a.Ng : a.N)) >= device_cus()) return t;
-  return 32;
+// What a kernel's tile of tm features by tn rows costs (microseconds, fitted to 155
+// products on MI355X: 1 to 32 groups of 1 to 3000 rows, 512 to 4096 features each way,
+// Ker cold): of s stages and n tiles a CU, once + max(s max(alone, n share), Ker's bytes
+// at bw TB/s) + n ends.  The least is within 1 to 4 % of the best kernel's time on
+// average, 1.4 times it at worst.
+struct Cost4 {
+  int tm, tn;
+  double alone, share, ends, once, bw;
+};
+
+// Group sizes are not known here: of several groups, half a tile each is taken to be
+// empty, and each to have one.
+double cost_of(const Cost4& c, const GroupArgs& a, double stages, double ker_bytes) {
+  const double groups = a.Ng < a.N ? a.Ng : a.N;
+  double nt = (a.N + c.tn - 1) / c.tn;
+  if (a.Ng > 1) nt = std::max(groups, (double)a.N / c.tn + 0.5 * groups);
+  const double tiles = nt * ((a.M + c.tm - 1) / c.tm);
+  const double n = 1 + (double)(int64_t)(tiles / device_cus() - 1e-3);  // of the CU with most
+  return c.once + std::max(stages * std::max(c.alone, n * c.share), ker_bytes / (c.bw * 1e6)) + n * c.ends;
 }
 
-template <typename TO, int MODE>
-hipError_t launch_sized4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
-  const bool pipe = ((uintptr_t)a.Y & 3) == 0 && a.ldy % 2 == 0 && a.K % 8 == 0 && (MODE != kFwd || (b.Nb % 4 == 0 && ((uintptr_t)b.xs & 3) == 0)) && pipe4_fits(a, MODE);
-  const int t = pick_tile4(a, pipe);
-  if (t == 256) return launch_pipe4<TO, MODE>(a, b, row_tiles(a.N, a.Ng, true, 256), 4, stream);
-  if (t == 128) return launch_tiles4<TO, MODE, 128, 128>(a, b, row_tiles(a.N, a.Ng, true, 128), 8, stream);
-  if (t == 64) return launch_tiles4<TO, MODE, 64, 64>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 65) return launch_tiles4<TO, MODE, 64, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 129) return launch_tiles4<TO, MODE, 128, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  return launch_tiles4<TO, MODE, 32, 32>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
+// The cheapest of c[first ..]; `last`: one past those that may run.
+template <int N> int cheapest(const Cost4 (&c)[N], int first, int last, const GroupArgs& a, double stages) {
+  const double ker = (a.Ng < a.N ? a.Ng : a.N) * 0.53125 * a.M * a.K;
+  int best = first;
+  double least = 1e30;
+  for (int i = first; i < last; ++i) {
+    const double t = cost_of(c[i], a, stages, ker);
+    if (t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
 }
 
-template <typename TO> hipError_t launch_sized44(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
-  const bool buf = pipe4_fits(a, kFwd) && b.Nb >= 2 && (int64_t)a.Nsrc * a.ldy * 2 < (1LL << 31) - 65536;
-  if (!buf) return launch_tiles44<TO, 64, 32, 2, 2, 4, false>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  const int t = pick_tile4(a, buf && b.Nb % 4 == 0 && (((uintptr_t)b.xs | (uintptr_t)b.ys) & 3) == 0);
-  if (t == 256) return launch_pipe44<TO>(a, b, row_tiles(a.N, a.Ng, true, 256), 4, stream);
-  if (t == 128) return launch_tiles44<TO, 128, 128, 2, 2, 2>(a, b, row_tiles(a.N, a.Ng, true, 128), 8, stream);
-  if (t == 64) return launch_tiles44<TO, 64, 64, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 65) return launch_tiles44<TO, 64, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 129) return launch_tiles44<TO, 128, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 130) return launch_tiles44<TO, 128, 64, 2, 2, 3>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 131) return launch_tiles44<TO, 128, 32, 4, 1, 3>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 132) return launch_tiles44<TO, 128, 128, 2, 2, 3>(a, b, row_tiles(a.N, a.Ng, true, 128), 8, stream);
-  if (t == 140) return launch_tiles44<TO, 128, 64, 4, 1, 3>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 141) return launch_tiles44<TO, 64, 64, 4, 1, 3>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 142) return launch_tiles44<TO, 64, 32, 4, 1, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 143) return launch_tiles44<TO, 64, 64, 4, 1, 4>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  if (t == 144) return launch_tiles44<TO, 128, 32, 4, 1, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 145) return launch_tiles44<TO, 128, 32, 4, 1, 2>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 146) return launch_tiles44<TO, 64, 32, 4, 1, 3>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
-  if (t == 149) return launch_tiles44<TO, 128, 64, 4, 1, 2>(a, b, row_tiles(a.N, a.Ng, true, 64), 16, stream);
-  return launch_tiles44<TO, 32, 32, 2, 2, 4>(a, b, row_tiles(a.N, a.Ng, true, 32), 16, stream);
+int64_t tiles_of(const GroupArgs& a, int tn) { return row_tiles(a.N, a.Ng, true, tn); }
+
+// bf16 rows.  Straight from memory: rows on 4-byte boundaries and of whole units, 16 blocks
+// a row at least; the pipelined kernel besides: scales on 4-byte boundaries.
+constexpr Cost4 kFwd4[] = {{64, 32, 0.630, 0.355, 0.00, 4.3, 2.7},  // through registers
+                           {64, 64, 0.821, 0.506, 0.00, 4.0, 2.2},
+                           {128, 128, 1.648, 1.213, 1.43, 3.0, 2.4},
+                           {16, 16, 0.028, 0.116, 0.15, 5.9, 3.7},  // straight from memory
+                           {64, 16, 0.176, 0.172, 0.16, 5.1, 6.7},
+                           {64, 32, 0.166, 0.217, 0.31, 5.0, 5.8},
+                           {128, 64, 0.683, 0.553, 1.60, 3.0, 6.0},
+                           {256, 256, 0.959, 2.600, 4.09, 3.0, 1.7}};  // pipelined
+
+template <typename TO> hipError_t launch_fwd4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
+  constexpr bool OB = sizeof(TO) == 2;
+  const bool rows = ((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0 && b.Nb >= 16 && pipe4_fits(a, kFwd) &&
+                    a.Nsrc * a.ldy * 2 < kMostBytes;
+  const bool pipe = rows && b.Nb % 4 == 0 && ((uintptr_t)b.xs & 3) == 0;
+  const int first = rows ? 3 : 0, last = pipe ? 8 : rows ? 7 : 3;
+  const int pick = cheapest(kFwd4, first, last, a, (a.K + 127) / 128);
+  switch (pick) {
+    case 0: return launch_tiles4<TO, kFwd, 64, 32>(a, b, tiles_of(a, 32), 16, stream);
+    case 1: return launch_tiles4<TO, kFwd, 64, 64>(a, b, tiles_of(a, 64), 16, stream);
+    case 2: return launch_tiles4<TO, kFwd, 128, 128>(a, b, tiles_of(a, 128), 8, stream);
+    case 3: return launch_group4_few(a, b, OB, stream);
+    case 7: return launch_pipe4<TO, kFwd>(a, b, tiles_of(a, 256), 4, stream);
+    default: return launch_group4_rows(a, b, OB, pick == 4 ? 16 : pick == 5 ? 32 : 64, stream);
+  }
+}
+
+// Both in 4 bits.
+constexpr Cost4 kFwd44[] = {{32, 32, 0.109, 0.229, 0.36, 5.6, 6.7},   {64, 32, 0.217, 0.356, 0.64, 5.1, 6.4},
+                            {128, 32, 0.252, 0.497, 1.37, 4.3, 7.0},  {128, 64, 0.306, 0.681, 1.89, 4.0, 6.8},
+                            {128, 128, 1.188, 1.146, 1.76, 3.7, 5.8}, {256, 256, 0.555, 1.253, 4.79, 3.0, 5.0}};
+
+template <typename TO> hipError_t launch_fwd44(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
+  const bool buf = pipe4_fits(a, kFwd) && b.Nb >= 2 && a.Nsrc * a.ldy * 2 < kMostBytes;
+  if (!buf) return launch_tiles44<TO, 64, 32, 2, 2, 4, false>(a, b, tiles_of(a, 32), 16, stream);
+  const bool pipe = b.Nb % 4 == 0 && (((uintptr_t)b.xs | (uintptr_t)b.ys) & 3) == 0;
+  GroupArgs values = a;
+  values.K = 32 * b.Nb;
+  // rings: more workgroups on a CU do more than more stages of each (1536 rows of 60
+  // groups of 1536 x 2048 in 128 x 32 tiles, four stages, three, two: 36, 34 and 33 us with
+  // the quantisation), but a lone one wants them
+  switch (cheapest(kFwd44, 0, pipe ? 6 : 5, values, (b.Nb + 7) / 8)) {
+    case 0: return launch_tiles44<TO, 32, 32, 2, 2, 4>(a, b, tiles_of(a, 32), 16, stream);
+    case 1: return launch_tiles44<TO, 64, 32, 2, 2, 4>(a, b, tiles_of(a, 32), 16, stream);
+    case 2: return launch_tiles44<TO, 128, 32, 4, 1, 3>(a, b, tiles_of(a, 32), 16, stream);
+    case 3: return launch_tiles44<TO, 128, 64, 4, 1, 3>(a, b, tiles_of(a, 64), 16, stream);
+    case 4: return launch_tiles44<TO, 128, 128, 2, 2, 2>(a, b, tiles_of(a, 128), 8, stream);
+    default: return launch_pipe44<TO>(a, b, tiles_of(a, 256), 4, stream);
+  }
+}
+
+// The gradient of In.  Pipelined: dOut's rows on 4-byte boundaries and of whole units.
+constexpr Cost4 kBwdIn4[] = {{64, 32, 0.470, 0.204, 0.00, 3.0, 2.0},
+                             {64, 64, 0.526, 0.287, 0.00, 3.0, 1.8},
+                             {128, 128, 0.862, 0.641, 0.45, 3.0, 6.9},
+                             {256, 256, 0.361, 1.372, 3.56, 3.0, 1.6}};
+
+template <typename TO> hipError_t launch_bwd_in4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
+  const bool pipe = ((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0 && pipe4_fits(a, kBwdIn);
+  switch (cheapest(kBwdIn4, 0, pipe ? 4 : 3, a, (a.K + 63) / 64)) {
+    case 0: return launch_tiles4<TO, kBwdIn, 64, 32>(a, b, tiles_of(a, 32), 16, stream);
+    case 1: return launch_tiles4<TO, kBwdIn, 64, 64>(a, b, tiles_of(a, 64), 16, stream);
+    case 2: return launch_tiles4<TO, kBwdIn, 128, 128>(a, b, tiles_of(a, 128), 8, stream);
+    default: return launch_pipe4<TO, kBwdIn>(a, b, tiles_of(a, 256), 4, stream);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_group_fwd4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream) {
-  const int t = pick_tile4(a, false);
-  const bool ok = a.Nsrc * (int64_t)a.ldy * 2 < (1LL << 31) && (b.ys || (((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0));
-  if (t == 16 && b.Nb >= 8 && (!b.ys || ok)) return launch_group4_few(a, b, bf16_out, stream);
-  if (t > 1000 && ok && b.Nb >= 16) return launch_group4_rows(a, b, bf16_out, t > 2000 ? 128 : 64, t % 1000, stream);
-  if (b.ys) return bf16_out ? launch_sized44<bf16_t>(a, b, stream) : launch_sized44<float>(a, b, stream);
-  return bf16_out ? launch_sized4<bf16_t, kFwd>(a, b, stream) : launch_sized4<float, kFwd>(a, b, stream);
+  if (b.ys) return bf16_out ? launch_fwd44<bf16_t>(a, b, stream) : launch_fwd44<float>(a, b, stream);
+  return bf16_out ? launch_fwd4<bf16_t>(a, b, stream) : launch_fwd4<float>(a, b, stream);
 }
 
 hipError_t launch_group_bwd_in4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream) {
-  return bf16_out ? launch_sized4<bf16_t, kBwdIn>(a, b, stream) : launch_sized4<float, kBwdIn>(a, b, stream);
+  return bf16_out ? launch_bwd_in4<bf16_t>(a, b, stream) : launch_bwd_in4<float>(a, b, stream);
 }
 
 }  // namespace cnnlib

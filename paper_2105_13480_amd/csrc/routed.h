@@ -148,10 +148,10 @@ hipError_t launch_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void*
 hipError_t launch_group_fwd4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream);
 hipError_t launch_group_bwd_in4(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream);
 
-// Few rows a group, Ker straight from memory: 16 rows and features a workgroup, or 64 or
-// 128 features by 16, 32 or 64 rows (bf16 rows then on 4-byte boundaries, of whole units).
+// bf16 rows, few a group, Ker in 4 bits straight from memory: 16 rows and features a
+// workgroup (8 blocks a row at least), or 64 features by 16 or 32 rows, or 128 by 64
+// (16 blocks; rows on 4-byte boundaries, of whole units, less than 2^31 bytes of them).
 hipError_t launch_group4_few(const GroupArgs& a, const Group4Args& b, bool bf16_out, hipStream_t stream);
-hipError_t launch_group4_rows(const GroupArgs& a, const Group4Args& b, bool bf16_out, int features, int rows,
-                              hipStream_t stream);
+hipError_t launch_group4_rows(const GroupArgs& a, const Group4Args& b, bool bf16_out, int rows, hipStream_t stream);
 
 }  // namespace cnnlib
