@@ -153,22 +153,24 @@ template <typename F> __device__ __forceinline__ void pipe_stages(int K, F stage
   }
 }
 
-// bf16 rows, forward.  Ker stays in 4 bits in LDS, 128 of k at a time, and each wave
-// turns what it reads into bf16 in its registers (32 instructions a half of X, in the
-// slot in which the other waves multiply), so that X takes a quarter of the copies and
-// reads: with bf16 in LDS these and the writes were as long as the products.  A lane
-// takes 16 values that follow one another, half a block; the other operand's lane the
-// same.  Of a pair of stages, 8 phases, the copies are: 0 X of its even stage and the
-// scales (of the next pair), 2 X of its odd stage, 1 3 5 7 Y as in group_pipe; what is
-// asked for in a phase is there in the sixth phase after it, so each wait leaves as many
-// in flight as the five phases up to it have.
-// Y's half 0 is read once for each half of X, not kept: registers are short and reads
-// are not.  So it has a third place in LDS.
-constexpr int kPipe4Y1 = 3 * kHalfBytes;              // [stage % 3] of half 0, [stage % 2] of half 1
-constexpr int kPipe4Codes = kPipe4Y1 + 2 * kHalfBytes;  // [stage % 4][256][32]
+// bf16 rows, forward.  Ker stays in 4 bits in LDS and each wave turns what it reads into
+// bf16 in its registers, in the slot in which the other waves multiply, so that X takes a
+// quarter of the copies and reads: with bf16 in LDS these and the writes were as long as
+// the products.  A wave has 64 (m) by 128 (n) results, so that it turns 64 rows of X, not
+// 128.  A lane takes 16 values that follow one another, half a block; the other operand's
+// lane the same.  A stage:
+//   phase  reads from LDS            copies                          products
+//     0    Y half 0, X1's codes      Y half 1 of s + 1               X0 Y0
+//     1                              (even) X, scales of s + 2       X1 Y0
+//     2    Y half 1                  Y half 0 of s + 2               X1 Y1
+//     3    X0's codes of s + 1       -                               X0 Y1
+// and X of s + 2 in an odd stage's phase 1; X0 and X1 become bf16 in phases 0 and 1, and X0
+// is kept.  What is asked for in a phase is there in the sixth phase after it, so each wait
+// leaves as many in flight as the five phases up to it have, by phases of two stages.
+constexpr int kPipe4Codes = 4 * kHalfBytes;           // after Y: [stage % 4][256][32]
 constexpr int kPipe4Scales = kPipe4Codes + 4 * 8192;  // [pair % 2][512][4], the second 256 not read
 constexpr int kPipe4Lds = kPipe4Scales + 2 * 2048;
-constexpr int kPipe4Waits[8] = {6, 8, 7, 9, 7, 7, 5, 6};
+constexpr int kPipe4Waits[8] = {7, 7, 8, 6, 8, 7, 7, 5};
 
 template <typename TO>
 __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b, int band) {
@@ -178,26 +180,26 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, G = lane >> 4;
   const int late = wave >> 2;  // one slot behind
-  const int wm = wave >> 2, wn = wave & 3;
-  auto xrow = [&](int i) { return (i >> 2) * 128 + wm * 64 + 16 * (i & 3); };
-  auto yrow = [&](int j) { return (j >> 1) * 128 + wn * 32 + 16 * (j & 1); };
+  const int wm = wave & 3, wn = wave >> 2;
+  auto xrow = [&](int i) { return (i >> 1) * 128 + wm * 32 + 16 * (i & 1); };
+  auto yrow = [&](int j) { return (j >> 2) * 128 + wn * 64 + 16 * (j & 3); };
 
   Tile<T, TO> w;
   if (!setup_tile<T, TO, kFwd, 256, 256>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
 
-  f32x4_t acc[8][4];
+  f32x4_t acc[4][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   if (w.K > 0) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
     const int K = w.K, Kx = 32 * b.Nb;
     PipeRows<true> ys;
-    PipeReads<2, true> Y;
-    Y.init(wn * 32, lane, lds0);
+    PipeReads<4, true> Y;
+    Y.init(wn * 64, lane, lds0);
     ys.init(tid, w.Y, w.n0, w.n_valid, a.ldy, w.rows, a.Nsrc);
     // this thread's part of X: 16 bytes of row tid / 2; and a row's four scales
     const int64_t x0 = g * a.M + w.m0;
@@ -217,35 +219,35 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
 #endif
     };
     auto copy_y = [&](auto par, auto check, int s, int h) __attribute__((always_inline)) {
-      ys.template copy<check.value>(h, 64 * s, K, lds + (h ? 3 + par.value : s % 3) * kPipeHalf + 64 * wave);
+      ys.template copy<check.value>(h, 64 * s, K, lds + (par.value * 2 + h) * kPipeHalf + 64 * wave);
     };
-    const char* const xget = smem + kPipe4Codes + 32 * (wm * 64 + l16) + 8 * G;
-    const char* const sget = smem + kPipe4Scales + 4 * (wm * 64 + l16) + (G >> 1);
-    u32x2_t code[4];
-    uint32_t scale[4];
+    const char* const xget = smem + kPipe4Codes + 32 * (wm * 32 + l16) + 8 * G;
+    const char* const sget = smem + kPipe4Scales + 4 * (wm * 32 + l16) + (G >> 1);
+    u32x2_t code[2];
+    uint32_t scale[2];
     auto read_x = [&](int s, int h) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         code[i] = *reinterpret_cast<const u32x2_t*>(xget + (s & 3) * 8192 + 4096 * h + 512 * i);
         scale[i] = *reinterpret_cast<const uint8_t*>(sget + (s & 2) * 1024 + 2 * (s & 1) + 512 * h + 64 * i);
       }
     };
-    u32x4_t xf[4][2], yf[2][2];
-    auto turn_x = [&]() __attribute__((always_inline)) {
+    u32x4_t x[2][2][2], yf[4][2];
+    auto turn_x = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) xf[i][ks] = bf16_of4(code[i][ks], scale4(scale[i]));
+        for (int ks = 0; ks < 2; ++ks) x[h][i][ks] = bf16_of4(code[i][ks], scale4(scale[i]));
     };
     auto products = [&](int hm, int hn) __attribute__((always_inline)) {
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[4 * hm + i][2 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
+          for (int j = 0; j < 4; ++j)
+            acc[2 * hm + i][4 * hn + j] = mma<T>(x[hm][i][ks], yf[j][ks], acc[2 * hm + i][4 * hn + j]);
       __builtin_amdgcn_s_setprio(0);
     };
     constexpr std::integral_constant<int, 0> even;
@@ -253,12 +255,11 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
     constexpr std::integral_constant<bool, true> check;
     copy_x(check, 0);
     copy_scales(0);
+    copy_x(check, 1);
     copy_y(even, check, 0, 0);
     copy_y(even, check, 0, 1);
-    copy_x(check, 1);
     copy_y(odd, check, 1, 0);
-    copy_y(odd, check, 1, 1);
-    pipe_landed<0>();
+    pipe_landed<2>();
     read_x(0, 0);
     pipe_done();
     if (late) pipe_done();
@@ -267,31 +268,28 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
       constexpr bool HALF = half.value;
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
-        Y.read(s % 3 * kHalfBytes, yf);
-        turn_x();
-        if constexpr (P == 0) {
-          copy_x(chk, s + 2);
-          copy_scales((s >> 1) + 1);
-        }
+        std::integral_constant<int, 1 - P> other;
+        Y.read(2 * P * kHalfBytes, yf);
+        turn_x(0);
+        read_x(s, 1);
+        copy_y(other, chk, s + 1, 1);
         pipe_landed<kPipe4Waits[4 * P]>();
         products(0, 0);
         pipe_done();
-        if constexpr (!HALF) Y.read(kPipe4Y1 + P * kHalfBytes, yf);
-        read_x(s, 1);
-        copy_y(par, chk, s + 2, 0);
+        turn_x(1);
+        copy_x(chk, s + 2);
+        if constexpr (P == 0) copy_scales((s >> 1) + 1);
         pipe_landed<kPipe4Waits[4 * P + 1]>();
-        if constexpr (!HALF) products(0, 1);
+        products(1, 0);
         pipe_done();
-        turn_x();
-        if constexpr (P == 0) copy_x(chk, s + 3);
+        if constexpr (!HALF) Y.read((2 * P + 1) * kHalfBytes, yf);
+        copy_y(par, chk, s + 2, 0);
         pipe_landed<kPipe4Waits[4 * P + 2]>();
         if constexpr (!HALF) products(1, 1);
         pipe_done();
-        Y.read(s % 3 * kHalfBytes, yf);
         read_x(s + 1, 0);
-        copy_y(par, chk, s + 2, 1);
         pipe_landed<kPipe4Waits[4 * P + 3]>();
-        products(1, 0);
+        if constexpr (!HALF) products(0, 1);
         pipe_done();
       });
     };
@@ -511,15 +509,16 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
     constexpr std::integral_constant<bool, true> check;
-    copy_scales(0);
-    copy_y(even, check, 0, 0);
+    // X first: Y's copies wait for the rows' numbers
     copy_x(even, check, 0, 0);
-    copy_y(even, check, 0, 1);
     copy_x(even, check, 0, 1);
-    copy_y(odd, check, 1, 0);
+    copy_y(even, check, 0, 0);
+    copy_scales(0);
+    copy_y(even, check, 0, 1);
     copy_x(odd, check, 1, 0);
+    copy_y(odd, check, 1, 0);
     copy_y(odd, check, 1, 1);
-    pipe_landed<10>();
+    pipe_landed<6>();
     Y.read(0, y0);
     pipe_done();
     if (late) pipe_done();
