@@ -302,10 +302,16 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
 }
 
 // The gradient of In.  Ker's part of a stage is 16 values a thread and half: codes and
-// scale are asked for a stage before they become bf16 in LDS, in the phase in which
-// group_pipe asks for the copy; two loads then, as it has two copies, so every wait
-// counts the same.  The conversion is 8 instructions a half and thread, beside the
-// other waves' matrix instructions.
+// scale are asked for a stage before they become bf16 in LDS (8 instructions), beside the
+// other waves' matrix instructions, and are read back transposed.  Waves of 64 (c) by 128
+// results: half as many transposing reads as with 128 by 64.  A stage:
+//   phase  reads from LDS   copies and loads                       products
+//     0    Y half 0, X0     Y half 1 of s + 1                      X0 Y0
+//     1    X1               X1 of s + 1 to LDS, the next asked for X1 Y0
+//     2    Y half 1         Y half 0 of s + 2                      X1 Y1
+//     3    -                X0 of s + 2 to LDS, the next asked for X0 Y1
+// Two copies or loads a phase, and what is asked for there in the sixth phase after it (the
+// loads, which the compiler waits for, in the fourth): a wait leaves ten in flight.
 template <typename TO>
 __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4Args b, int band) {
   typedef bf16_t T;
@@ -313,33 +319,33 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
   u32x4_t* const lds = reinterpret_cast<u32x4_t*>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int late = wave >> 2;  // one slot behind
-  const int wm = wave >> 2, wn = wave & 3;
-  auto xrow = [&](int i) { return (i >> 2) * 128 + wm * 64 + 16 * (i & 3); };
-  auto yrow = [&](int j) { return (j >> 1) * 128 + wn * 32 + 16 * (j & 1); };
+  const int wm = wave & 3, wn = wave >> 2;
+  auto xrow = [&](int i) { return (i >> 1) * 128 + wm * 32 + 16 * (i & 1); };
+  auto yrow = [&](int j) { return (j >> 2) * 128 + wn * 64 + 16 * (j & 3); };
 
   Tile<T, TO> w;
   if (!setup_tile<T, TO, kBwdIn, 256, 256>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
 
-  f32x4_t acc[8][4];
+  f32x4_t acc[4][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   if (w.K > 0) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(char, smem);
     const int K = w.K;
     PipeKer4 ker;
-    PipeOperand<false, false, 4> X;  // its reads
+    PipeOperand<false, false, 2> X;  // its reads
     PipeRows<false> ys;
-    PipeReads<2, false> Y;
+    PipeReads<4, false> Y;
     ker.init(tid, reinterpret_cast<const uint8_t*>(a.X) + g * K * 16 * b.Nb, b.xs + g * K * b.Nb, b.Nb, w.m0, K);
-    X.init(tid, nullptr, 0, 1, 0, nullptr, 0, wm * 64, lane, lds0);
-    Y.init(wn * 32, lane, lds0);
+    X.init(tid, nullptr, 0, 1, 0, nullptr, 0, wm * 32, lane, lds0);
+    Y.init(wn * 64, lane, lds0);
     ys.init(tid, w.Y, w.n0, w.n_valid, a.ldy, nullptr, 0);
 
-    u32x4_t xf[4][2], y0[2][2], y1[2][2];
+    u32x4_t x0[2][2], x1[2][2], yf[4][2];
     auto half_of = [&](int par, int h) { return (uint32_t)(kPipe4X + (par * 2 + h) * kHalfBytes); };
     // half h of X of stage s to LDS, and the next one of it asked for
     auto put_x = [&](auto par, int s, int h) __attribute__((always_inline)) {
@@ -349,15 +355,15 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
     auto copy_y = [&](auto par, auto check, int s, int h) __attribute__((always_inline)) {
       ys.template copy<check.value>(h, 64 * s, K, lds + (par.value * 2 + h) * kPipeHalf + 64 * wave);
     };
-    auto products = [&](int hm, int hn, const u32x4_t(&yf)[2][2]) __attribute__((always_inline)) {
+    auto products = [&](int hm, int hn, const u32x4_t(&xf)[2][2]) __attribute__((always_inline)) {
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[4 * hm + i][2 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[4 * hm + i][2 * hn + j]);
+          for (int j = 0; j < 4; ++j)
+            acc[2 * hm + i][4 * hn + j] = mma<T>(xf[i][ks], yf[j][ks], acc[2 * hm + i][4 * hn + j]);
       __builtin_amdgcn_s_setprio(0);
     };
     constexpr std::integral_constant<int, 0> even;
@@ -370,12 +376,9 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
     put_x(even, 0, 0);
     put_x(even, 0, 1);
     copy_y(odd, check, 1, 0);
-    copy_y(odd, check, 1, 1);
     put_x(odd, 1, 0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    Y.read(0, y0);
-    pipe_done();
     if (late) pipe_done();
     // HALF: no row of Y half 1 is there, its phases only keep the step
     auto run = [&](auto half) __attribute__((always_inline)) {
@@ -383,31 +386,26 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
         std::integral_constant<int, 1 - P> other;
-        X.template read<0>(half_of(P, 0), xf);
+        Y.read(2 * P * kHalfBytes, yf);
+        X.template read<0>(half_of(P, 0), x0);
+        copy_y(other, chk, s + 1, 1);
+        pipe_landed<10>();
+        products(0, 0, x0);
+        pipe_done();
+        X.template read<0>(half_of(P, 1), x1);
         put_x(other, s + 1, 1);
         pipe_landed<10>();
-        products(0, 0, y0);
+        products(1, 0, x1);
         pipe_done();
-        if constexpr (!HALF) Y.read((2 * P + 1) * kHalfBytes, y1);
+        if constexpr (!HALF) Y.read((2 * P + 1) * kHalfBytes, yf);
         copy_y(par, chk, s + 2, 0);
         pipe_landed<10>();
-        if constexpr (!HALF) products(0, 1, y1);
+        if constexpr (!HALF) products(1, 1, x1);
         pipe_done();
-        X.template read<0>(half_of(P, 1), xf);
         put_x(par, s + 2, 0);
         pipe_landed<10>();
-        if constexpr (!HALF) products(1, 1, y1);
+        if constexpr (!HALF) products(0, 1, x0);
         pipe_done();
-        u32x4_t next[2][2];
-        Y.read(2 * (1 - P) * kHalfBytes, next);
-        copy_y(par, chk, s + 2, 1);
-        pipe_landed<10>();
-        products(1, 0, y0);
-        pipe_done();
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int ks = 0; ks < 2; ++ks) y0[j][ks] = next[j][ks];
       });
     };
     if (w.n_valid <= 128) run(std::integral_constant<bool, true>{});
