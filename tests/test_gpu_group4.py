@@ -28,7 +28,9 @@ CASES = [(1, 1, 1, 1, 0.0, 1, 1), (1, 4, 2, 1, 0.0, 64, 32), (2, 3, 3, 2, 0.0, 1
          (257, 1, 1, 1, 0.0, 64, 129), (500, 70, 66, 2, 0.1, 40, 24), (600, 2, 1, 1, 0.5, 200, 640),
          (1100, 2, 2, 1, 0.1, 192, 328), (700, 1, 1, 1, 0.0, 1000, 520), (333, 12, 11, 2, 0.0, 1001, 537),
          (640, 28, 26, 1, 0.0, 1056, 2048), (1300, 3, 3, 2, 0.1, 1152, 2112), (2600, 2, 2, 2, 0.05, 640, 3000),
-         (3000, 1, 1, 1, 0.0, 1280, 2304), (4100, 5, 5, 1, 0.02, 2304, 1290)]
+         (3000, 1, 1, 1, 0.0, 1280, 2304), (4100, 5, 5, 1, 0.02, 2304, 1290), (20, 2, 2, 1, 0.0, 3008, 250),
+         (6001, 1, 1, 1, 0.0, 267, 2071), (4800, 16, 15, 1, 0.1, 1536, 1544), (8000, 5, 5, 1, 0.05, 1000, 2056),
+         (400, 40, 30, 1, 0.0, 2112, 500), (5000, 3, 3, 1, 0.05, 2056, 2056)]
 
 
 def _order(gen, Nt, Ng, active, Kt, drop):
@@ -71,7 +73,8 @@ def _product(x, ker, offsets):
 @pytest.mark.parametrize("case", CASES, ids=str)
 @pytest.mark.parametrize("both", [False, True])
 def test_forward(case, both, out):
-    """Gathered rows and rows in order; bf16 rows at an odd element."""
+    """Gathered rows and rows in order; bf16 rows at an odd element, scales at an odd
+    byte or not."""
     say(f"[fwd4] {case} {both} {out}")
     Nt, Ng, active, Kt, drop, Nc, Nk = case
     gen = torch.Generator().manual_seed(Nt + Nc)
@@ -89,10 +92,10 @@ def test_forward(case, both, out):
         got = _out(Np + 1, Nk, OUT[out])
         at = rows.long().clamp_min(0)
         if both:
-            In, extra = (xc if gathered else xc[at]).cuda(), {"InScales": _at(xs if gathered else xs[at], 1)}
+            In, extra = (xc if gathered else xc[at]).cuda(), {"InScales": _at(xs if gathered else xs[at], int(Nt % 4 > 0))}
         else:
             In, extra = _at((x if gathered else p).bfloat16(), Nt % 2), {}
-        routed.group_fwd4(In, codes.cuda(), _at(scales, 1), got[:Np], offsets.cuda(),
+        routed.group_fwd4(In, codes.cuda(), _at(scales, int(Nt % 4 > 0)), got[:Np], offsets.cuda(),
                           rows.cuda() if gathered else None, **extra)
         assert torch.equal(got[:Np].cpu(), want.to(OUT[out]))
         assert torch.isnan(got[Np]).all()
