@@ -56,7 +56,7 @@ constexpr Cost4 kFwd4[] = {{64, 32, 0.630, 0.355, 0.00, 4.3, 2.7},  // through r
                            {64, 16, 0.176, 0.172, 0.16, 5.1, 6.7},
                            {64, 32, 0.166, 0.217, 0.31, 5.0, 5.8},
                            {128, 64, 0.683, 0.553, 1.60, 3.0, 6.0},
-                           {256, 256, 0.959, 2.600, 4.09, 3.0, 1.7}};  // pipelined
+                           {256, 256, 1.592, 2.200, 4.17, 3.0, 2.0}};  // pipelined
 
 template <typename TO> hipError_t launch_fwd4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
   constexpr bool OB = sizeof(TO) == 2;
@@ -103,7 +103,7 @@ template <typename TO> hipError_t launch_fwd44(const GroupArgs& a, const Group4A
 constexpr Cost4 kBwdIn4[] = {{64, 32, 0.470, 0.204, 0.00, 3.0, 2.0},
                              {64, 64, 0.526, 0.287, 0.00, 3.0, 1.8},
                              {128, 128, 0.862, 0.641, 0.45, 3.0, 6.9},
-                             {256, 256, 0.361, 1.372, 3.56, 3.0, 1.6}};
+                             {256, 256, 0.728, 1.238, 3.70, 3.0, 1.8}};
 
 template <typename TO> hipError_t launch_bwd_in4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
   const bool pipe = ((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0 && pipe4_fits(a, kBwdIn);
