@@ -53,16 +53,16 @@ __device__ __forceinline__ void buffer_lds(__amdgpu_buffer_rsrc_t r, u32x4_t* ld
 
 // Stages R rows of features by 64 of k (KC) or 64 rows of k by R of c of a Ker in
 // 4 bits as bf16: a thread takes half blocks (8 bytes, 16 values).
-template <bool KC, int R, int NT> struct Stager4 {
+template <bool KC, int R, int NT, int SETS> struct Stager4 {
   static constexpr int ALL = 4 * R, NU = (ALL + NT - 1) / NT;
   static constexpr int U = KC ? 4 : R / 16;  // half blocks of a row of the stage
   const uint8_t* codes[NU];
   const uint8_t* scales[NU];
   int at[NU];        // KC: the half block's first k within a stage; else its row of k
   bool there[NU];    // !KC: the half block is one of the row's
-  u32x2_t code[2][NU];
-  uint32_t scale[2][NU];
-  uint32_t gone[2];  // bit j: half block j of the set is not there
+  u32x2_t code[SETS][NU];
+  uint32_t scale[SETS][NU];
+  uint32_t gone[SETS];  // bit j: half block j of the set is not there
 
   // codes, scales: the group's; rows of Nb blocks; rows (KC) or c (else) [i0, i0 + n) are there.
   __device__ __forceinline__ void init(int tid, const uint8_t* c4, const uint8_t* s4, int Nb, int i0, int n) {
@@ -116,12 +116,13 @@ template <bool KC, int R, int NT> struct Stager4 {
 };
 
 // TM x TN results by 2 x 2 waves, both operands through registers at any
-// alignment of the rows, two stages in LDS and two in flight.
-template <typename TO, int MODE, int TM, int TN>
+// alignment of the rows, two stages in LDS and SETS in flight.  LONG: K is 8 at least.
+template <typename TO, int MODE, int TM, int TN, int SETS, bool LONG>
 __global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b, int band) {
   typedef bf16_t T;
   constexpr int NT = 256, WM = 2, WN = 2, TK = 64;
   constexpr bool XKC = MODE == kFwd, YG = MODE == kFwd;
+  constexpr bool LATE = MODE == kBwdIn && SETS == 2;  // no registers for loads beside the products
   constexpr int NI = TM / WM / 16, NJ = TN / WN / 16;
   constexpr int XU = 8 * TM, STAGE = XU + 8 * TN;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -136,8 +137,8 @@ __global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b
   if (!setup_tile<T, TO, MODE, TM, TN>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
   const int rows_x = XKC ? a.M : a.K;  // rows of one group's Ker
-  Stager4<XKC, TM, NT> sx;
-  Stager<T, true, TN, NT, YG> sy;
+  Stager4<XKC, TM, NT, SETS> sx;
+  Stager<T, true, TN, NT, YG, SETS> sy;
   Reader<T, XKC, TM, NI> rx;
   Reader<T, true, TN, NJ> ry;
   rx.init(xrow(0), lane);
@@ -155,15 +156,6 @@ __global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b
     sy.init(tid, w.Y, a.ldy, w.n0, w.n_valid, YG ? w.rows : nullptr, a.Nsrc);
     const int xk = XKC ? 32 * b.Nb : w.K;
     const int n_st = (w.K + TK - 1) / TK;
-    auto load = [&](auto set, int s) __attribute__((always_inline)) {
-      sx.template load<set.value>(s * TK, b.Nb, xk);
-      sy.template load<set.value>(s * TK, a.ldy, w.K, nullptr, 0);
-    };
-    auto commit = [&](auto set, int s) __attribute__((always_inline)) {
-      u32x4_t* const dst = ring + (s & 1) * STAGE;
-      sx.template commit<set.value>(tid, dst);
-      sy.template commit<set.value>(tid, dst + XU, s * TK, a.ldy, w.K, nullptr, 0);
-    };
     auto compute = [&](const u32x4_t* buf) __attribute__((always_inline)) {
       u32x4_t xf[NI][2], yf[NJ][2];
       rx.read(buf, xf);
@@ -175,30 +167,58 @@ __global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b
 #pragma unroll
           for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(xf[i][ks], yf[j][ks], acc[i][j]);
     };
-    constexpr std::integral_constant<int, 0> even;
-    constexpr std::integral_constant<int, 1> odd;
-    load(even, 0);
-    if (n_st > 1) load(odd, 1);
-    commit(even, 0);
-    auto step = [&](auto set, auto other, int s) __attribute__((always_inline)) {
-      __syncthreads();  // stage s is there; every wave is done with stage s - 1
-      if (s + 2 < n_st) load(set, s + 2);
-      compute(ring + (s & 1) * STAGE);
-      if (s + 1 < n_st) commit(other, s + 1);
+    // stages past the last are loaded too, from where there is something, and never used: a
+    // branch around loads would have the compiler wait for all that are in flight
+    auto load = [&](auto set, int s) __attribute__((always_inline)) {
+      sx.template load<set.value>(s * TK, b.Nb, xk);
+      sy.template load<set.value, LONG>(s * TK, a.ldy, w.K, nullptr, 0);
     };
-    int s = 0;
-    for (; s + 2 <= n_st; s += 2) {
-      step(even, odd, s);
-      step(odd, even, s + 1);
+    auto commit = [&](auto set, int s) __attribute__((always_inline)) {
+      u32x4_t* const dst = ring + (s & 1) * STAGE;
+      sx.template commit<set.value>(tid, dst);
+      sy.template commit<set.value, LONG>(tid, dst + XU, s * TK, a.ldy, w.K, nullptr, 0);
+    };
+    auto step = [&](auto set, int s) __attribute__((always_inline)) {
+      __syncthreads();  // stage s is there; every wave is done with stage s - 1
+      std::integral_constant<int, (set.value + 1) % SETS> next;
+      if constexpr (!LATE) load(set, s + SETS);
+      compute(ring + (s & 1) * STAGE);
+      if constexpr (LATE) {
+        __builtin_amdgcn_sched_barrier(0);
+        load(set, s + SETS);
+      }
+      commit(next, s + 1);
+    };
+    std::integral_constant<int, 0> s0;
+    std::integral_constant<int, 1> s1;
+    std::integral_constant<int, 2 % SETS> s2;
+    std::integral_constant<int, 3 % SETS> s3;
+    load(s0, 0);
+    load(s1, 1);
+    if constexpr (SETS > 2) {
+      load(s2, 2);
+      load(s3, 3);
     }
-    if (s < n_st) step(even, odd, s);
+    commit(s0, 0);
+    for (int s = 0;;) {
+      step(s0, s);
+      if (++s == n_st) break;
+      step(s1, s);
+      if (++s == n_st) break;
+      if constexpr (SETS > 2) {
+        step(s2, s);
+        if (++s == n_st) break;
+        step(s3, s);
+        if (++s == n_st) break;
+      }
+    }
   }
   store_tile<T, TO, MODE, MODE == kFwd>(a, w, lane, acc, xrow, yrow);
 }
 
-template <typename TO, int MODE, int TM, int TN>
+template <typename TO, int MODE, int TM, int TN, bool LONG = true>
 hipError_t launch_tiles4(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
-  auto* const k = group4_tiles<TO, MODE, TM, TN>;
+  auto* const k = group4_tiles<TO, MODE, TM, TN, (TM > 64 ? 2 : 4), LONG>;
   const int64_t grid = row_tiles * ((a.M + TM - 1) / TM);
   const hipError_t fit = grid_fits(grid, 256);
   if (fit != hipSuccess) return fit;

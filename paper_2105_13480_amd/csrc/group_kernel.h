@@ -125,7 +125,7 @@ template <typename T, bool KC, int R> __device__ __forceinline__ int unit_at(int
 // Stages one operand: R tile rows by TK values of k, 8 R units by NT threads.
 // Rows of the tile past its last read one that is there (their results are not
 // stored; source rows that are not there are stored as zeros).
-template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
+template <typename T, bool KC, int R, int NT, bool GATHER, int SETS = 2> struct Stager {
   static constexpr int CE = 16 / (int)sizeof(T);
   static constexpr int TK = 128 / (int)sizeof(T);
   static constexpr int NU = 8 * R / NT;  // units a thread stages
@@ -137,8 +137,8 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
   int lim[KC ? 1 : NU];  // elements of the row from the unit's first
   bool wide;             // !KC: the row holds a unit; p is at most its last
   int src[GATHER && !KC ? NU : 1];
-  u32x4_t regs[2][NU];
-  uint32_t there[2];     // !KC: whether unit j's row of k is (bit j), of each set
+  u32x4_t regs[SETS][NU];
+  uint32_t there[SETS];    // !KC: whether unit j's row of k is (bit j), of each set
 
   // base: the tensor at its first k; rows [i0, i0 + n) of the tile index are
   // there; ld: elements from row to row; index: source rows of a gathered
@@ -213,9 +213,9 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     }
   }
 
-  // Through registers (one of two sets), at any alignment: loads, and later the
-  // LDS writes.
-  template <int SET = 0>
+  // Through registers (one of SETS sets), at any alignment: loads, and later the
+  // LDS writes.  LONG: K holds a unit, and no branch is around the loads.
+  template <int SET = 0, bool LONG = false>
   __device__ __forceinline__ void load(int k0, int64_t ld, int nk, const int32_t* index, int nsrc) {
     u32x4_t(&reg)[NU] = regs[SET];
     // what is to be cut off or cleared is so when the loads are waited for, and
@@ -223,7 +223,7 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     if constexpr (KC) {
 #pragma unroll
       for (int j = 0; j < NU; ++j) {
-        if (nk >= CE) __builtin_memcpy(&reg[j], p[j] - at[j] + min(k0 + at[j], nk - CE), 16);
+        if (LONG || nk >= CE) __builtin_memcpy(&reg[j], p[j] - at[j] + min(k0 + at[j], nk - CE), 16);
       }
     } else {
       there[SET] = 0;
@@ -236,14 +236,14 @@ template <typename T, bool KC, int R, int NT, bool GATHER> struct Stager {
     }
   }
   // Of the stage at k0, as it was loaded.
-  template <int SET = 0>
+  template <int SET = 0, bool LONG = false>
   __device__ __forceinline__ void commit(int tid, u32x4_t* lds, int k0, int64_t ld, int nk,
                                          const int32_t* index, int nsrc) const {
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
       u32x4_t v = regs[SET][j];
       if constexpr (KC) {
-        if (nk < CE) v = load_unit(p[j] + k0, nk - k0 - at[j]);
+        if (!LONG && nk < CE) v = load_unit(p[j] + k0, nk - k0 - at[j]);
         else if (k0 + TK > nk) v = drop_first<T>(v, max(k0 + at[j] + CE - nk, 0));
       } else {
         if (!wide) {

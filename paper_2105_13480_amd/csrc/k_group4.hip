@@ -49,9 +49,9 @@ int64_t tiles_of(const GroupArgs& a, int tn) { return row_tiles(a.N, a.Ng, true,
 
 // bf16 rows.  Straight from memory: rows on 4-byte boundaries and of whole units, 16 blocks
 // a row at least; the pipelined kernel besides: scales on 4-byte boundaries.
-constexpr Cost4 kFwd4[] = {{64, 32, 0.630, 0.355, 0.00, 4.3, 2.7},  // through registers
-                           {64, 64, 0.821, 0.506, 0.00, 4.0, 2.2},
-                           {128, 128, 1.648, 1.213, 1.43, 3.0, 2.4},
+constexpr Cost4 kFwd4[] = {{64, 32, 0.380, 0.319, 0.00, 5.6, 4.6},  // through registers
+                           {64, 64, 0.580, 0.437, 0.43, 3.8, 4.9},
+                           {128, 128, 1.202, 1.015, 1.37, 3.8, 4.9},
                            {16, 16, 0.028, 0.116, 0.15, 5.9, 3.7},  // straight from memory
                            {64, 16, 0.176, 0.172, 0.16, 5.1, 6.7},
                            {64, 32, 0.166, 0.217, 0.31, 5.0, 5.8},
@@ -60,10 +60,11 @@ constexpr Cost4 kFwd4[] = {{64, 32, 0.630, 0.355, 0.00, 4.3, 2.7},  // through r
 
 template <typename TO> hipError_t launch_fwd4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
   constexpr bool OB = sizeof(TO) == 2;
+  if (a.K < 8) return launch_tiles4<TO, kFwd, 64, 32, false>(a, b, tiles_of(a, 32), 16, stream);
   const bool rows = ((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0 && b.Nb >= 16 && pipe4_fits(a, kFwd) &&
                     a.Nsrc * a.ldy * 2 < kMostBytes;
   const bool pipe = rows && b.Nb % 4 == 0 && ((uintptr_t)b.xs & 3) == 0;
-  const int first = rows ? 3 : 0, last = pipe ? 8 : rows ? 7 : 3;
+  const int first = rows ? 2 : 0, last = pipe ? 8 : rows ? 7 : 3;
   const int pick = cheapest(kFwd4, first, last, a, (a.K + 127) / 128);
   switch (pick) {
     case 0: return launch_tiles4<TO, kFwd, 64, 32>(a, b, tiles_of(a, 32), 16, stream);
@@ -100,12 +101,13 @@ template <typename TO> hipError_t launch_fwd44(const GroupArgs& a, const Group4A
 }
 
 // The gradient of In.  Pipelined: dOut's rows on 4-byte boundaries and of whole units.
-constexpr Cost4 kBwdIn4[] = {{64, 32, 0.470, 0.204, 0.00, 3.0, 2.0},
-                             {64, 64, 0.526, 0.287, 0.00, 3.0, 1.8},
-                             {128, 128, 0.862, 0.641, 0.45, 3.0, 6.9},
+constexpr Cost4 kBwdIn4[] = {{64, 32, 0.269, 0.188, 0.00, 4.5, 2.6},
+                             {64, 64, 0.350, 0.255, 0.19, 3.4, 2.2},
+                             {128, 128, 0.771, 0.557, 1.02, 3.0, 4.5},
                              {256, 256, 0.728, 1.238, 3.70, 3.0, 1.8}};
 
 template <typename TO> hipError_t launch_bwd_in4(const GroupArgs& a, const Group4Args& b, hipStream_t stream) {
+  if (a.K < 8) return launch_tiles4<TO, kBwdIn, 64, 32, false>(a, b, tiles_of(a, 32), 16, stream);
   const bool pipe = ((uintptr_t)a.Y & 3) == 0 && a.K % 8 == 0 && pipe4_fits(a, kBwdIn);
   switch (cheapest(kBwdIn4, 0, pipe ? 4 : 3, a, (a.K + 63) / 64)) {
     case 0: return launch_tiles4<TO, kBwdIn, 64, 32>(a, b, tiles_of(a, 32), 16, stream);
