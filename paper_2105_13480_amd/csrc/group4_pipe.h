@@ -111,7 +111,7 @@ struct PipeKer4 {
     uint32_t t = threadIdx.x;
     asm volatile("" : "+v"(t));  // offsets are made anew each time: registers are short
     const uint32_t row = (t >> 3) * (uint32_t)Nb;
-    code[h] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(codes, (int)(row * 16 + 8 * (t & 7)), k0 * 16 * Nb + 64 * h, 0));
+    code[h] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(codes, (int)(row * 16 + 8 * (t & 7)), (int)((uint32_t)k0 * 16u * (uint32_t)Nb + 64u * h), 0));
     scale[h] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)(row + ((t & 7) >> 1)), k0 * Nb + 4 * h, 0);
 #endif
   }

@@ -203,6 +203,80 @@ def test_no_numbers_stay(sizes, Nc, Nk):
         assert not torch.isfinite(t[1 if i < 2 else 2]).any()
 
 
+@pytest.mark.parametrize("Np", [2, 70, 700])
+def test_ker_past_32_bits(Np):
+    """The last group's Ker begins 4.9 GB into the tensor."""
+    say(f"[group4 past 32 bits] {Np}")
+    Ng, Nk, Nc = 300, 16392, 2048
+    gen = torch.Generator().manual_seed(Np)
+    codes, scales = four_bits.random(gen, 1, Nk, Nc=Nc)
+    Ker = torch.empty((Ng, Nk, Nc // 2), dtype=torch.uint8, device="cuda")
+    KerScales = torch.empty((Ng, Nk, Nc // 32), dtype=torch.uint8, device="cuda")
+    Ker[-1], KerScales[-1] = codes[0].cuda(), scales[0].cuda()
+    offsets = torch.zeros(Ng + 1, dtype=torch.int32)
+    offsets[-1] = Np
+    ker = four_bits.values(codes, scales, Nc)[0]
+    x, d = _whole(gen, Np, Nc), _whole(gen, Np, Nk, top=1)
+    got = routed.group_fwd4(x.cuda(), Ker, KerScales, _out(Np, Nk, torch.float32), offsets.cuda())
+    assert torch.equal(got.cpu().double(), x.double() @ ker.t())
+    xc, xs = four_bits.random(gen, Np, Nc=Nc)
+    got = routed.group_fwd4(xc.cuda(), Ker, KerScales, _out(Np, Nk, torch.float32), offsets.cuda(), InScales=xs.cuda())
+    assert torch.equal(got.cpu().double(), four_bits.values(xc, xs, Nc) @ ker.t())
+    d[:, 2000:] = 0  # sums stay whole numbers in fp32
+    d[:, -300:] = 1
+    got = routed.group_bwd_in4(d.cuda(), Ker, KerScales, _out(Np, Nc, torch.float32), offsets.cuda())
+    assert torch.equal(got.cpu().double(), d.double() @ ker)
+
+
+@pytest.mark.parametrize("both", [False, True])
+@pytest.mark.parametrize("Np", [5, 600])
+def test_rows_past_31_bits(both, Np):
+    """Gathered rows of an In of more than 2^31 bytes."""
+    say(f"[group4 rows past 31 bits] {both} {Np}")
+    Nt, Nc, Nk = ((1 << 22) + 5, 1024, 264) if both else ((1 << 20) + 7, 1040, 264)
+    gen = torch.Generator().manual_seed(Np)
+    codes, scales = four_bits.random(gen, 2, Nk, Nc=Nc)
+    rows = torch.randperm(Nt, generator=gen)[:Np]
+    rows[0], rows[1], rows[2] = Nt - 1, 0, Nt - 2
+    if both:
+        xc, xs = four_bits.random(gen, Np, Nc=Nc)
+        x = four_bits.values(xc, xs, Nc)
+        In = torch.empty((Nt, Nc // 2), dtype=torch.uint8, device="cuda")
+        InScales = torch.empty((Nt, Nc // 32), dtype=torch.uint8, device="cuda")
+        In[rows.cuda()], InScales[rows.cuda()] = xc.cuda(), xs.cuda()
+        assert In.numel() > 1 << 31
+    else:
+        x, InScales = _whole(gen, Np, Nc), None
+        In = torch.empty((Nt, Nc), dtype=torch.bfloat16, device="cuda")
+        In[rows.cuda()] = x.cuda()
+        assert In.numel() * 2 > 1 << 31
+    offsets = torch.tensor([0, Np // 2, Np], dtype=torch.int32)
+    got = routed.group_fwd4(In, codes.cuda(), scales.cuda(), _out(Np, Nk, torch.float32), offsets.cuda(),
+                            rows.int().cuda(), InScales=InScales)
+    assert torch.equal(got.cpu().double(), _product(x.double(), four_bits.values(codes, scales, Nc), offsets))
+
+
+def test_one_ker_past_31_bits():
+    """One group's Ker has more than 2^31 bytes of codes: zeros but for its ends."""
+    say("[group4 one Ker past 31 bits]")
+    Np, Nk, Nc, n = 5, (1 << 21) + 24, 2048, 50
+    gen = torch.Generator().manual_seed(1)
+    ends = [four_bits.random(gen, 1, n, Nc=Nc) for _ in range(2)]
+    Ker = torch.zeros((1, Nk, Nc // 2), dtype=torch.uint8, device="cuda")
+    KerScales = torch.full((1, Nk, Nc // 32), 127, dtype=torch.uint8, device="cuda")
+    for (c, s), at in zip(ends, (slice(0, n), slice(Nk - n, Nk))):
+        Ker[:, at], KerScales[:, at] = c.cuda(), s.cuda()
+    ker = torch.cat([four_bits.values(c, s, Nc)[0] for c, s in ends])
+    offsets = torch.tensor([0, Np], dtype=torch.int32)
+    x, d = _whole(gen, Np, Nc), _whole(gen, Np, Nk)
+    got = routed.group_fwd4(x.cuda(), Ker, KerScales, _out(Np, Nk, torch.float32), offsets.cuda())
+    want = x.double() @ ker.t()
+    assert torch.equal(got[:, :n].cpu().double(), want[:, :n]) and torch.equal(got[:, -n:].cpu().double(), want[:, n:])
+    assert not got[:, n:-n].any()
+    got = routed.group_bwd_in4(d.cuda(), Ker, KerScales, _out(Np, Nc, torch.float32), offsets.cuda())
+    assert torch.equal(got.cpu().double(), torch.cat([d[:, :n], d[:, -n:]], 1).double() @ ker)
+
+
 def test_rows_that_are_not_there():
     """Rows outside In read as zeros; offsets that are no order write nothing outside."""
     gen = torch.Generator().manual_seed(2)
