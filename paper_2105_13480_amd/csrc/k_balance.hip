@@ -419,14 +419,12 @@ __global__ __launch_bounds__(256) void balance_bwd(BalanceArgs a) {
 #pragma unroll
   for (int i = 0; i < E; ++i) sum += f[i];
   const float rows = (float)max(a.tokens[s], 1);
-  const float inv = 1.f / fmaxf(row_sum<LT>(sum), 1.f);
+  // f stays the whole number n until the end: f - sum p f = (n - sum p n) / sum n
+  const float choices = fmaxf(row_sum<LT>(sum), 1.f);
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    f[i] *= inv;
-    pf += p[i] * f[i];
-  }
+  for (int i = 0; i < E; ++i) pf += p[i] * f[i];
   pf = row_sum<LT>(pf);
-  const float db = d0 * (float)a.Ng / ((float)max(live, 1) * rows);
+  const float db = d0 * (float)a.Ng / ((float)max(live, 1) * rows * choices);
   const float dz = d1 * 2.f / (float)max(total, 1) * lse;
   if (!ok) return;
   TO* const out = reinterpret_cast<TO*>(a.dlogits) + row * a.Ng + E * li;
