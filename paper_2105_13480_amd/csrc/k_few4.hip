@@ -148,14 +148,11 @@ __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
     const int c8 = 8 * ((tid & 15) ^ (tid >> 4));
     const __amdgpu_buffer_rsrc_t yr = rsrc_of(a.Y, (int64_t)a.Nsrc * 2 * a.ldy);
     uint32_t src[RB];
+    int from[RB];  // the rows' numbers are asked for first, then codes, which need none
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
-      int64_t r = t.n0 + min(16 * i + (tid >> 4), n_valid - 1);
-      if (a.rows) {
-        r = a.rows[r];
-        if (r < 0 || r >= a.Nsrc) r = 0;
-      }
-      src[i] = (uint32_t)((r * a.ldy + c8) * 2);
+      from[i] = t.n0 + min(16 * i + (tid >> 4), n_valid - 1);
+      if (a.rows) from[i] = a.rows[from[i]];
     }
     const int n_run = (Nb + 3) / 4;
     Blocks4<SB> x[2][FB];
@@ -206,6 +203,11 @@ __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
       }
     };
     load(std::integral_constant<int, 0>{}, 0);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const int64_t r = from[i] < 0 || from[i] >= a.Nsrc ? 0 : from[i];
+      src[i] = (uint32_t)((r * a.ldy + c8) * 2);
+    }
     copy_y(0);
     copy_y(1);
     copy_y(2);
