@@ -1,9 +1,20 @@
 // The pipelined 256 x 256 tile kernels of products with a Ker in 4 bits, in the
-// phases of group_pipe (which see): eight waves of 128 x 64 results, a stage in four
-// phases of one quarter, waves 4 to 7 a slot behind.  Operands come by buffer
-// instructions: one offset register a row (or one in all, where rows follow one
-// another), scalar offsets for the rest, and zeros past the end, since the
-// accumulators, two quarters of X and three of Y leave no registers to spare.
+// phases of group_pipe (which see): eight waves, a stage in four phases of one quarter,
+// waves 4 to 7 a slot behind.  Operands come by buffer instructions: one offset register
+// a row (or one in all, where rows follow one another), scalar offsets for the rest, and
+// zeros past the end (both offsets' sum is what is compared with it), since accumulators
+// and operands leave no registers to spare, and a spill in the loop is a wait for
+// everything in flight.
+//
+// Bound by the matrix unit and by a tile's start and results, 8 to 10 us in which the CU
+// that it fills alone multiplies nothing (16384 x 2 rows of 16 groups of 4096 x 2048):
+//   bf16 rows    465 us, 1180 TFLOP/s; one group of 8192 x 8192 1445, the library's bf16
+//                product of that size 1330 to 1480
+//   gradient     425 us, 1295 TFLOP/s; 1400
+//   both 4 bits  209 us, 2630 TFLOP/s; 4330: a stage of 1.7 us (0.9 at the matrix unit's
+//                rate, 1.0 of reads from LDS)
+// Workgroups that stay for several tiles (results are in the same order of waits as the
+// next tile's copies) and stores past the caches gained nothing.
 #pragma once
 
 #include "group4_kernel.h"

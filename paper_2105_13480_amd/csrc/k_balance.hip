@@ -15,6 +15,13 @@
 // sequence, adds a sequence's places in order and the last of them to finish adds
 // up the sequences, in order too.  One workgroup and one sequence: one launch.
 // Rows are held by 16 lanes (64 past 256 experts), as in the router.
+//
+// Bound by launches and by what waits for what within them (bounds, logits, sums), not by
+// the 9 MB: 16384 rows of 128 experts in 37 sequences, bf16, rows 8.4 to 10.1 us, sums 5.6
+// to 5.9, gradient 6.4 to 7.0 (a launch with nothing to do 2.5); 256 rows of 32 experts in
+// fp32, one launch of 6.0 us (the two would be 8) and 3.8.  Sums of each workgroup are
+// places of their own in the workspace, added up in order: atomic
+// sums of floats would change from run to run.
 #include "common.h"
 #include "routed.h"
 

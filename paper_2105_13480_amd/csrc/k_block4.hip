@@ -10,8 +10,11 @@
 // values, scale or results are subnormal.  A block that holds an infinity or NaN has
 // s = 255 and reads back as NaN.
 //
-// A lane has 8 values, four lanes a block.  Bound by memory: each value is read and
-// each code written once.
+// A lane has 8 values, four lanes a block: 32 or 16 bytes of each in one load, and the
+// largest magnitude by two moves among the four.  Bound by memory, each value being read
+// and each code written once: 32768 x 2048 from fp32 62 us, 4.9 TB/s, and to bf16 26 us,
+// 6.5 TB/s (what was just written is still in the caches); 16384 x 2048 from bf16 18 us,
+// 4.7 TB/s; 1001 x 2048 2.7 us each, a launch.
 #include "common.h"
 #include "routed.h"
 

@@ -112,8 +112,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void group4_few(GroupArgs a, Group4
 // its features at a time, 64 SB bytes of each row in loads that follow one another, and
 // for the next ones while it multiplies (a run at a time, 64 bytes of a row, half a
 // line: 256 rows of two of 28 groups of 4096 x 1024 27.5 us in 64 x 32 tiles, this way
-// 20.9, 3.2 TB/s; 8 rows of four of 20 of 1024 x 2048 in 64 x 16 13.1 and 9.0).  The
-// rows come through a ring of four runs.
+// 20.4, 3.3 TB/s; 8 rows of four of 20 of 1024 x 2048 in 64 x 16 13.1 and 9.0, half of it
+// the start).  Four sets of codes in flight were slower (27.3 and 11.2): fewer waves fit,
+// and a wait for the rows' copies is one for all older loads.  The rows come through a
+// ring of four runs.
 template <typename TO, int FB, int RB, int SB>
 __global__ __launch_bounds__(256) void group4_rows(GroupArgs a, Group4Args b) {
   constexpr int TM = 64 * FB, TN = 16 * RB, D = 4;

@@ -12,8 +12,8 @@ using namespace group;
 // What a kernel's tile of tm features by tn rows costs (microseconds, fitted to 155
 // products on MI355X: 1 to 32 groups of 1 to 3000 rows, 512 to 4096 features each way,
 // Ker cold): of s stages and n tiles a CU, once + max(s max(alone, n share), Ker's bytes
-// at bw TB/s) + n ends.  The least is within 1 to 4 % of the best kernel's time on
-// average, 1.4 times it at worst.
+// at bw TB/s) + n ends.  The least is within 1 to 3 % of the best kernel's time on
+// average, 1.35 times it at worst.
 struct Cost4 {
   int tm, tn;
   double alone, share, ends, once, bw;

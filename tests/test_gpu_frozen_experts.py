@@ -108,7 +108,7 @@ def test_against_64_bits(case, four):
             total = total + experts * (f / f.sum() * p[rows_s].mean(0)).sum()
             squares = squares + (torch.logsumexp(l[rows_s], 1) ** 2).sum()
             used, n = used + 1, n + len(rows_s)
-    total, squares = total / max(used, 1), squares / max(n, 1)  # nothing to judge: zero
+    total, squares = total / max(used, 1), squares / max(n, 1)  # no row takes part: zero
     assert abs(float(losses[0]) - float(total)) <= 1e-4 * float(total)
     assert abs(float(losses[1]) - float(squares)) <= 1e-4 * float(squares)
     (score + float(dl[0]) * total + float(dl[1]) * squares + 0 * torch.nan_to_num(l).sum()).backward()
