@@ -320,25 +320,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
   if (w.K > 0) {
     const int Nb = b.Nb;
     const int64_t x0 = g * a.M + w.m0;
-    // the row of Y of a row of the tile
-    auto source = [&](int n) __attribute__((always_inline)) -> int64_t {
-      int64_t r = w.n0 + min(n, w.n_valid - 1);
-      if (w.rows) {
-        r = w.rows[r];
-        if (r < 0 || r >= a.Nsrc) r = 0;
-      }
-      return r;
-    };
     // this thread's unit column, and its rows NT / 8 by NT / 8
     const int r0 = tid >> 3, c8 = 8 * ((tid & 7) ^ ((r0 >> 1) & 7));
     static_assert((NT / 8) % 16 == 0, "one unit column in all rows");
+    // Y's rows of this thread's copies and of its lane's scales: their numbers are asked
+    // for first, then X, which needs none
+    int yrow_of[NY], srow_of[NJ];
+    auto number = [&](int n) __attribute__((always_inline)) {
+      const int r = w.n0 + min(n, w.n_valid - 1);
+      return w.rows ? w.rows[r] : r;
+    };
+    auto source = [&](int r) __attribute__((always_inline)) -> int64_t { return r < 0 || r >= a.Nsrc ? 0 : r; };
+#pragma unroll
+    for (int j = 0; j < NY; ++j) yrow_of[j] = number(r0 + j * (NT / 8));
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) srow_of[j] = number(yrow(j) + l16);
     const T* const X = reinterpret_cast<const T*>(a.X) + x0 * a.ldx + c8;
     const T* const Y = reinterpret_cast<const T*>(a.Y) + c8;
     __amdgpu_buffer_rsrc_t xr, yr;
     int64_t yat[NY];
     uint32_t xoff = 0;
-#pragma unroll
-    for (int j = 0; j < NY; ++j) yat[j] = source(r0 + j * (NT / 8)) * a.ldy;
     Scales4<NI, BUF> px;
     Scales4<NJ, BUF> py;
     if constexpr (BUF) {
@@ -354,15 +355,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
       if constexpr (BUF) px.off[i] = (uint32_t)(m * Nb);
       else px.p[i] = b.xs + (x0 + m) * Nb;
     }
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int64_t r = source(yrow(j) + l16);
-      if constexpr (BUF) py.off[j] = (uint32_t)(r * Nb);
-      else py.p[j] = b.ys + r * Nb;
-    }
     const int n_st = (w.K + TK - 1) / TK;
     // past K zeros, so that every wait counts the same
-    auto copy = [&](int s) __attribute__((always_inline)) {
+    auto copy_x = [&](int s) __attribute__((always_inline)) {
       u32x4_t* const dst = ring + (s % DEPTH) * STAGE + 64 * wave;
       const bool ok = s * TK + c8 < w.K;
 #pragma unroll
@@ -371,10 +366,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
         if constexpr (BUF) buffer_lds(xr, dst + j * NT, ok ? xoff : kNowhere, (uint32_t)((row * a.ldx + s * TK) * 2));
         else copy16_lds(ok ? (const void*)(X + (int64_t)min(row + r0, w.m_valid - 1) * a.ldx + s * TK) : (const void*)zero_unit, dst + j * NT);
       }
+    };
+    auto copy_y = [&](int s) __attribute__((always_inline)) {
+      u32x4_t* const dst = ring + (s % DEPTH) * STAGE + 64 * wave + XU;
+      const bool ok = s * TK + c8 < w.K;
 #pragma unroll
       for (int j = 0; j < NY; ++j) {
-        if constexpr (BUF) buffer_lds(yr, dst + XU + j * NT, ok ? (uint32_t)((yat[j] + c8) * 2) : kNowhere, (uint32_t)(2 * s * TK));
-        else copy16_lds(ok ? (const void*)(Y + yat[j] + s * TK) : (const void*)zero_unit, dst + XU + j * NT);
+        if constexpr (BUF) buffer_lds(yr, dst + j * NT, ok ? (uint32_t)((yat[j] + c8) * 2) : kNowhere, (uint32_t)(2 * s * TK));
+        else copy16_lds(ok ? (const void*)(Y + yat[j] + s * TK) : (const void*)zero_unit, dst + j * NT);
       }
     };
     uint32_t at[2][2];  // LDS bytes of this lane's units, by sub-step
@@ -385,17 +384,32 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
     }
     uint32_t fx[2][NI], fy[2][NJ];  // scales of this stage and the next
     px.load(2 * G, Nb, fx[0]);
+#pragma unroll
+    for (int s = 0; s < DEPTH - 1; ++s) copy_x(s);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t r = source(srow_of[j]);
+      if constexpr (BUF) py.off[j] = (uint32_t)(r * Nb);
+      else py.p[j] = b.ys + r * Nb;
+    }
+#pragma unroll
+    for (int j = 0; j < NY; ++j) yat[j] = source(yrow_of[j]) * a.ldy;
     py.load(2 * G, Nb, fy[0]);
 #pragma unroll
-    for (int s = 0; s < DEPTH - 1; ++s) copy(s);
-    auto step = [&](auto set, auto first, int s) __attribute__((always_inline)) {
+    for (int s = 0; s < DEPTH - 1; ++s) copy_y(s);
+    // Stage s has landed and every wave is done with stage s - 1.  What may be in flight: the
+    // copies of the stages between and, but for the second stage, the scales asked for with
+    // them; of the first, Y's alone, since X's were all asked for before.
+    constexpr int kFirst = (DEPTH - 2) * NY;
+    constexpr int kSecond = DEPTH == 4 ? 2 * NY + NX : (DEPTH - 2) * (NX + NY);
+    constexpr int kLater = (DEPTH - 2) * (NX + NY + (BUF ? NI + NJ : 0));
+    auto step = [&](auto set, auto in_flight, int s) __attribute__((always_inline)) {
       constexpr int S = set.value;
-      // stage s has landed (the later ones' copies, and the scales that were asked for
-      // with them but for the first, may be in flight); every wave is done with stage s - 1
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((DEPTH - 2) * (NX + NY + (BUF && !first.value ? NI + NJ : 0))) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(in_flight.value) : "memory");
       px.load(8 * s + 8 + 2 * G, Nb, fx[1 - S]);
       py.load(8 * s + 8 + 2 * G, Nb, fy[1 - S]);
-      copy(s + DEPTH - 1);
+      copy_x(s + DEPTH - 1);
+      copy_y(s + DEPTH - 1);
       const char* const buf = reinterpret_cast<const char*>(ring + (s % DEPTH) * STAGE);
       u32x4_t xf[NI][2], yf[NJ][2];
 #pragma unroll
@@ -418,10 +432,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group44_tiles(GroupArgs a, Gr
     static_assert(DEPTH <= 4, "two first stages");
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
-    constexpr std::integral_constant<bool, true> first;
-    constexpr std::integral_constant<bool, false> later;
+    constexpr std::integral_constant<int, kFirst> first;
+    constexpr std::integral_constant<int, kSecond> second;
+    constexpr std::integral_constant<int, kLater> later;
     step(even, first, 0);
-    if (n_st > 1) step(odd, first, 1);
+    if (n_st > 1) step(odd, second, 1);
     int s = 2;
     for (; s + 2 <= n_st; s += 2) {
       step(even, later, s);
