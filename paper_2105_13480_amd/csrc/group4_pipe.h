@@ -536,28 +536,32 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
         std::integral_constant<int, 1 - P> other;
-        X.read(2 * P * kHalfBytes, xf);
+        // scales first: reads come back in order, and the first product needs them
 #pragma unroll
         for (int i = 0; i < 4; ++i) sx[i] = scales(chk, s, xrow(i));
 #pragma unroll
         for (int j = 0; j < 2; ++j) sy[j] = scales(chk, s, 256 + yrow(j));
+        __builtin_amdgcn_sched_barrier(0);
+        X.read(2 * P * kHalfBytes, xf);
         if constexpr (P == 0) copy_scales((s >> 1) + 1);
         copy_x(other, chk, s + 1, 1);
         pipe_landed<10>();
         products(0, 0, y0);
         pipe_done();
         if constexpr (!HALF) {
-          Y.read((2 * P + 1) * kHalfBytes, y1);
 #pragma unroll
           for (int j = 2; j < 4; ++j) sy[j] = scales(chk, s, 256 + yrow(j));
+          __builtin_amdgcn_sched_barrier(0);
+          Y.read((2 * P + 1) * kHalfBytes, y1);
         }
         copy_y(par, chk, s + 2, 0);
         pipe_landed<10>();
         if constexpr (!HALF) products(0, 1, y1);
         pipe_done();
-        X.read((2 * P + 1) * kHalfBytes, xf);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sx[i] = scales(chk, s, xrow(4 + i));
+        __builtin_amdgcn_sched_barrier(0);
+        X.read((2 * P + 1) * kHalfBytes, xf);
         copy_x(par, chk, s + 2, 0);
         pipe_landed<10>();
         if constexpr (!HALF) products(1, 1, y1);
