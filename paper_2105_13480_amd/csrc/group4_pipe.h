@@ -13,6 +13,10 @@
 //   gradient     425 us, 1295 TFLOP/s; 1400
 //   both 4 bits  209 us, 2630 TFLOP/s; 4330: a stage of 1.7 us (0.9 at the matrix unit's
 //                rate, 1.0 of reads from LDS)
+// A last round of at most 128 tiles is halved by features (15550 rows of 8 groups of
+// 2048 x 2048, 520 tiles: 141 us, now 131; one group of 1100 rows of 4096 x 4096 with both
+// in 4 bits 32.1 and 24.5), and a tile without its second half of features does without
+// its products (8000 rows of 2056 x 2048: 96 us, now 87).
 // Workgroups that stay for several tiles (results are in the same order of waits as the
 // next tile's copies) and stores past the caches gained nothing.
 #pragma once
@@ -164,6 +168,26 @@ template <typename F> __device__ __forceinline__ void pipe_stages(int K, F stage
   }
 }
 
+// run(X, Y): of that operand half 1 is not there, and its phases only keep the step (such
+// a tile takes 0.73 to 0.77 of a whole one's time).
+template <typename F> __device__ __forceinline__ void pipe_halves(int m_valid, int n_valid, F run) {
+  constexpr std::integral_constant<bool, true> half;
+  constexpr std::integral_constant<bool, false> whole;
+  if (m_valid <= 128) {
+    if (n_valid <= 128) run(half, half);
+    else run(half, whole);
+  } else {
+    if (n_valid <= 128) run(whole, half);
+    else run(whole, whole);
+  }
+}
+// The launch's arguments with the tile's end for features.
+__device__ __forceinline__ GroupArgs up_to(const GroupArgs& a, int end) {
+  GroupArgs e = a;
+  e.M = end;
+  return e;
+}
+
 // bf16 rows, forward.  Ker stays in 4 bits in LDS and each wave turns what it reads into
 // bf16 in its registers, in the slot in which the other waves multiply, so that X takes a
 // quarter of the copies and reads: with bf16 in LDS these and the writes were as long as
@@ -196,7 +220,7 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
   auto yrow = [&](int j) { return (j >> 2) * 128 + wn * 64 + 16 * (j & 3); };
 
   Tile<T, TO> w;
-  if (!setup_tile<T, TO, kFwd, 256, 256>(a, band, &w)) return;
+  if (!setup_tile<T, TO, kFwd, 256, 256, true>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
 
   f32x4_t acc[4][8];
@@ -274,29 +298,28 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
     read_x(0, 0);
     pipe_done();
     if (late) pipe_done();
-    // HALF: no row of Y half 1 is there, its phases only keep the step
-    auto run = [&](auto half) __attribute__((always_inline)) {
-      constexpr bool HALF = half.value;
+    auto run = [&](auto one_x, auto one_y) __attribute__((always_inline)) {
+      constexpr bool XHALF = one_x.value, HALF = one_y.value;
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
         std::integral_constant<int, 1 - P> other;
         Y.read(2 * P * kHalfBytes, yf);
         turn_x(0);
-        read_x(s, 1);
+        if constexpr (!XHALF) read_x(s, 1);
         copy_y(other, chk, s + 1, 1);
         pipe_landed<kPipe4Waits[4 * P]>();
         products(0, 0);
         pipe_done();
-        turn_x(1);
+        if constexpr (!XHALF) turn_x(1);
         copy_x(chk, s + 2);
         if constexpr (P == 0) copy_scales((s >> 1) + 1);
         pipe_landed<kPipe4Waits[4 * P + 1]>();
-        products(1, 0);
+        if constexpr (!XHALF) products(1, 0);
         pipe_done();
         if constexpr (!HALF) Y.read((2 * P + 1) * kHalfBytes, yf);
         copy_y(par, chk, s + 2, 0);
         pipe_landed<kPipe4Waits[4 * P + 2]>();
-        if constexpr (!HALF) products(1, 1);
+        if constexpr (!HALF && !XHALF) products(1, 1);
         pipe_done();
         read_x(s + 1, 0);
         pipe_landed<kPipe4Waits[4 * P + 3]>();
@@ -304,12 +327,11 @@ __global__ __launch_bounds__(512, 2) void group4_pipe(GroupArgs a, Group4Args b,
         pipe_done();
       });
     };
-    if (w.n_valid <= 128) run(std::integral_constant<bool, true>{});
-    else run(std::integral_constant<bool, false>{});
+    pipe_halves(w.m_valid, w.n_valid, run);
     if (!late) pipe_done();
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the trailing copies
   }
-  store_tile<T, TO, kFwd, true>(a, w, lane, acc, xrow, yrow);
+  store_tile<T, TO, kFwd, true>(up_to(a, w.m0 + w.m_valid), w, lane, acc, xrow, yrow);
 }
 
 // The gradient of In.  Ker's part of a stage is 16 values a thread and half: codes and
@@ -335,7 +357,7 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
   auto yrow = [&](int j) { return (j >> 2) * 128 + wn * 64 + 16 * (j & 3); };
 
   Tile<T, TO> w;
-  if (!setup_tile<T, TO, kBwdIn, 256, 256>(a, band, &w)) return;
+  if (!setup_tile<T, TO, kBwdIn, 256, 256, true>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
 
   f32x4_t acc[4][8];
@@ -391,9 +413,8 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     if (late) pipe_done();
-    // HALF: no row of Y half 1 is there, its phases only keep the step
-    auto run = [&](auto half) __attribute__((always_inline)) {
-      constexpr bool HALF = half.value;
+    auto run = [&](auto one_x, auto one_y) __attribute__((always_inline)) {
+      constexpr bool XHALF = one_x.value, HALF = one_y.value;
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
         std::integral_constant<int, 1 - P> other;
@@ -403,15 +424,15 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
         pipe_landed<10>();
         products(0, 0, x0);
         pipe_done();
-        X.template read<0>(half_of(P, 1), x1);
+        if constexpr (!XHALF) X.template read<0>(half_of(P, 1), x1);
         put_x(other, s + 1, 1);
         pipe_landed<10>();
-        products(1, 0, x1);
+        if constexpr (!XHALF) products(1, 0, x1);
         pipe_done();
         if constexpr (!HALF) Y.read((2 * P + 1) * kHalfBytes, yf);
         copy_y(par, chk, s + 2, 0);
         pipe_landed<10>();
-        if constexpr (!HALF) products(1, 1, x1);
+        if constexpr (!HALF && !XHALF) products(1, 1, x1);
         pipe_done();
         put_x(par, s + 2, 0);
         pipe_landed<10>();
@@ -419,12 +440,11 @@ __global__ __launch_bounds__(512, 2) void group4_pipe_bwd_in(GroupArgs a, Group4
         pipe_done();
       });
     };
-    if (w.n_valid <= 128) run(std::integral_constant<bool, true>{});
-    else run(std::integral_constant<bool, false>{});
+    pipe_halves(w.m_valid, w.n_valid, run);
     if (!late) pipe_done();
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the trailing copies
   }
-  store_tile<T, TO, kBwdIn, false>(a, w, lane, acc, xrow, yrow);
+  store_tile<T, TO, kBwdIn, false>(up_to(a, w.m0 + w.m_valid), w, lane, acc, xrow, yrow);
 }
 
 // Both operands in 4 bits: the same bytes a stage, 256 values of k, and so the same
@@ -446,7 +466,7 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
   auto yrow = [&](int j) { return (j >> 1) * 128 + wn * 32 + 16 * (j & 1); };
 
   Tile<T, TO> w;
-  if (!setup_tile<T, TO, kFwd, 256, 256>(a, band, &w)) return;
+  if (!setup_tile<T, TO, kFwd, 256, 256, true>(a, band, &w)) return;
   const int64_t g = w.g < a.Ng ? w.g : 0;
 
   f32x4_t acc[8][4];
@@ -531,8 +551,8 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
     Y.read(0, y0);
     pipe_done();
     if (late) pipe_done();
-    auto run = [&](auto half) __attribute__((always_inline)) {
-      constexpr bool HALF = half.value;
+    auto run = [&](auto one_x, auto one_y) __attribute__((always_inline)) {
+      constexpr bool XHALF = one_x.value, HALF = one_y.value;
       pipe_stages(K, [&](auto par, auto chk, int s) __attribute__((always_inline)) {
         constexpr int P = par.value;
         std::integral_constant<int, 1 - P> other;
@@ -558,19 +578,21 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
         pipe_landed<10>();
         if constexpr (!HALF) products(0, 1, y1);
         pipe_done();
+        if constexpr (!XHALF) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sx[i] = scales(chk, s, xrow(4 + i));
-        __builtin_amdgcn_sched_barrier(0);
-        X.read((2 * P + 1) * kHalfBytes, xf);
+          for (int i = 0; i < 4; ++i) sx[i] = scales(chk, s, xrow(4 + i));
+          __builtin_amdgcn_sched_barrier(0);
+          X.read((2 * P + 1) * kHalfBytes, xf);
+        }
         copy_x(par, chk, s + 2, 0);
         pipe_landed<10>();
-        if constexpr (!HALF) products(1, 1, y1);
+        if constexpr (!HALF && !XHALF) products(1, 1, y1);
         pipe_done();
         u32x4_t next[2][2];
         Y.read(2 * (1 - P) * kHalfBytes, next);
         copy_y(par, chk, s + 2, 1);
         pipe_landed<10>();
-        products(1, 0, y0);
+        if constexpr (!XHALF) products(1, 0, y0);
         pipe_done();
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -578,12 +600,11 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
           for (int ks = 0; ks < 2; ++ks) y0[j][ks] = next[j][ks];
       });
     };
-    if (w.n_valid <= 128) run(std::integral_constant<bool, true>{});
-    else run(std::integral_constant<bool, false>{});
+    pipe_halves(w.m_valid, w.n_valid, run);
     if (!late) pipe_done();
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the trailing (empty) copies
   }
-  store_tile<T, TO, kFwd, true>(a, w, lane, acc, xrow, yrow);
+  store_tile<T, TO, kFwd, true>(up_to(a, w.m0 + w.m_valid), w, lane, acc, xrow, yrow);
 }
 
 // Whether the byte offsets of a tile's rows, of any row that may be gathered and (the
@@ -597,7 +618,7 @@ inline bool pipe4_fits(const GroupArgs& a, int mode) {
 template <typename TO, int MODE>
 hipError_t launch_pipe4(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
   auto* const k = MODE == kFwd ? group4_pipe<TO> : group4_pipe_bwd_in<TO>;
-  const int64_t grid = row_tiles * ((a.M + 255) / 256);
+  const int64_t grid = row_tiles * ((a.M + 255) / 256) + kRound / 2;
   hipError_t e = grid_fits(grid, 512);
   if (e == hipSuccess) e = allow_max_lds(reinterpret_cast<const void*>(k));
   if (e != hipSuccess) return e;
@@ -608,7 +629,7 @@ hipError_t launch_pipe4(const GroupArgs& a, const Group4Args& b, int64_t row_til
 template <typename TO>
 hipError_t launch_pipe44(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
   auto* const k = group44_pipe<TO>;
-  const int64_t grid = row_tiles * ((a.M + 255) / 256);
+  const int64_t grid = row_tiles * ((a.M + 255) / 256) + kRound / 2;
   hipError_t e = grid_fits(grid, 512);
   if (e == hipSuccess) e = allow_max_lds(reinterpret_cast<const void*>(k));
   if (e != hipSuccess) return e;

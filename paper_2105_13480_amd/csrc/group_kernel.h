@@ -447,7 +447,10 @@ __device__ __forceinline__ void store4(TO* row, int m, int M, f32x4_t v) {
 // [n0, n1) of the group from the tile's first on, and its tile of m.
 struct RowTile {
   int g, n0, n1, mt;
+  int part;  // of a tile halved by features, 1 or 2; else 0
 };
+// Workgroups of a round of tiles that fill a CU each.
+constexpr int kRound = 256;
 
 // Rows of group g; group Ng is the rows past the last.
 __device__ __forceinline__ void group_rows(const int32_t* off, int Ng, int Np, int g, int* lo,
@@ -494,13 +497,16 @@ __device__ __forceinline__ int row16_min(int v) {
 // tiles an XCD runs at a time share their rows of X and Y in its L2.  Offsets
 // that are not an order (documented as the caller's duty) are found out by the
 // wave that adds them up: no tile is then run.
-template <int TN, bool SPLIT = false>
+// HALVES: a last round of few tiles has each of them twice, halved by features (the
+// launch has kRound / 2 workgroups more).
+template <int TN, bool SPLIT = false, bool HALVES = false>
 __device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, int MT, int bid,
                                           int band, RowTile* t) {
   const int lane = threadIdx.x & 63;
   int nt, j0, lo_g = 0, hi_g = Np;  // row tiles of the group, tile within it, its rows
   int first = 0;                    // the first of those row tiles
   t->g = 0;
+  t->part = 0;
   if (!off) {
     nt = (Np + TN - 1) / TN;
     if (bid >= nt * MT) return false;
@@ -527,6 +533,13 @@ __device__ __forceinline__ bool find_tile(const int32_t* off, int Ng, int Np, in
       const int both = __builtin_amdgcn_readlane(parts, 63);
       n_of[1] += both & 0xffff;
       n_of[2] += both >> 16;
+    }
+    if constexpr (HALVES) {
+      const int all = (n_of[0] + n_of[1] + n_of[2]) * MT, left = all % kRound, at = bid - (all - left);
+      if (left <= kRound / 2 && at >= 0) {
+        if (at < 2 * left) t->part = 1 + (at & 1);
+        bid -= t->part ? at - (at >> 1) : left;
+      }
     }
     int kind = 0;
     while (kind < (SPLIT ? 3 : 1) && bid >= n_of[kind] * MT) bid -= n_of[kind++] * MT;
@@ -620,14 +633,14 @@ template <typename T, typename TO> struct Tile {
   int K, m0, m_valid, n0, n_valid, g;
 };
 
-template <typename T, typename TO, int MODE, int TM, int TN>
+template <typename T, typename TO, int MODE, int TM, int TN, bool HALVES = false>
 __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T, TO>* w) {
   const int MT = (a.M + TM - 1) / TM;
   w->X = reinterpret_cast<const T*>(a.X);
   w->Y = reinterpret_cast<const T*>(a.Y);
   w->D = reinterpret_cast<TO*>(a.D);
   w->rows = a.rows;
-  int mt;
+  int mt, part = 0;
   if constexpr (MODE == kBwdKer) {
     const int NTL = (a.N + TN - 1) / TN;
     const int g = group_by_rows(a.off, a.Ng, a.K, blockIdx.x, MT * NTL);
@@ -647,7 +660,8 @@ __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T,
     w->D += g * a.dgroup + (int64_t)w->n0 * a.ldd;
   } else {
     RowTile t;
-    if (!find_tile<TN, TN == 256>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return false;
+    if (!find_tile<TN, TN == 256, HALVES>(a.off, a.Ng, a.N, MT, blockIdx.x, band, &t)) return false;
+    part = t.part;
     w->K = t.g < a.Ng ? a.K : 0;  // the rows past the last group: no products
     w->n0 = t.n0;
     w->g = t.g;
@@ -657,9 +671,9 @@ __device__ __forceinline__ bool setup_tile(const GroupArgs& a, int band, Tile<T,
     if constexpr (MODE < kAdapt) w->D += (int64_t)t.n0 * a.ldd;
     mt = t.mt;
   }
-  w->m0 = mt * TM;
-  w->m_valid = min(a.M - w->m0, TM);
-  return true;
+  w->m0 = mt * TM + (part == 2 ? TM / 2 : 0);
+  w->m_valid = min(a.M - w->m0, part ? TM / 2 : TM);
+  return !HALVES || w->m_valid > 0;
 }
 
 // Eight consecutive bf16 results from `m` of one row, as many as lie below M.
