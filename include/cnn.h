@@ -653,8 +653,9 @@ int cnn_dequantize4(const uint8_t* Codes, const uint8_t* Scales, void* Out, int6
  * cnn_group_fwd of a Ker in 4 bits along c: Ker [Ng][Nk][blocks][16], KerScales
  * [Ng][Nk][blocks].  InScales NULL: In[Nt][Nc] is bf16; else In is in 4 bits too,
  * codes [Nt][blocks][16] and InScales [Nt][blocks], as cnn_quantize4 makes them of
- * the rows.  Products are of the exact values, sums fp32.  dtype: CNN_BF16 (fp32
- * Out) or CNN_BF16_OBF16 (CNN_F32: CNN_E_UNSUPPORTED).
+ * the rows.  Products are of the exact values (with bf16 rows, Ker's of 2^128 and more
+ * are infinite), sums fp32.  dtype: CNN_BF16 (fp32 Out) or CNN_BF16_OBF16 (CNN_F32:
+ * CNN_E_UNSUPPORTED).
  */
 int cnn_group_fwd4(const void* In, const uint8_t* InScales, const uint8_t* Ker, const uint8_t* KerScales,
                    void* Out, const int32_t* Offsets, const int32_t* Rows, int64_t Nt, int64_t Np,
