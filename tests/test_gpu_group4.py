@@ -19,7 +19,7 @@ pytestmark = pytest.mark.gpu
 OUT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 # (Nt, Ng, active, Kt, drop, Nc, Nk): one row and one value, few rows a group, whole and
-# ragged tiles of each size, rows that end inside a block, idle groups, more than 64 of
+# ragged tiles of each size, last rounds that are halved, rows that end inside a block, idle groups, more than 64 of
 # them, rows without a group
 CASES = [(1, 1, 1, 1, 0.0, 1, 1), (1, 4, 2, 1, 0.0, 64, 32), (2, 3, 3, 2, 0.0, 130, 33),
          (5, 8, 6, 2, 0.0, 256, 128), (9, 2, 2, 1, 0.3, 2048, 48), (16, 4, 3, 2, 0.2, 520, 100),
@@ -30,7 +30,8 @@ CASES = [(1, 1, 1, 1, 0.0, 1, 1), (1, 4, 2, 1, 0.0, 64, 32), (2, 3, 3, 2, 0.0, 1
          (640, 28, 26, 1, 0.0, 1056, 2048), (1300, 3, 3, 2, 0.1, 1152, 2112), (2600, 2, 2, 2, 0.05, 640, 3000),
          (3000, 1, 1, 1, 0.0, 1280, 2304), (4100, 5, 5, 1, 0.02, 2304, 1290), (20, 2, 2, 1, 0.0, 3008, 250),
          (6001, 1, 1, 1, 0.0, 267, 2071), (4800, 16, 15, 1, 0.1, 1536, 1544), (8000, 5, 5, 1, 0.05, 1000, 2056),
-         (400, 40, 30, 1, 0.0, 2112, 500), (5000, 3, 3, 1, 0.05, 2056, 2056)]
+         (400, 40, 30, 1, 0.0, 2112, 500), (5000, 3, 3, 1, 0.05, 2056, 2056),
+         (8200, 3, 3, 1, 0.05, 2304, 2056), (8000, 2, 2, 1, 0.02, 2056, 1544)]
 
 
 def _order(gen, Nt, Ng, active, Kt, drop):
