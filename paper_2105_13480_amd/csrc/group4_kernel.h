@@ -51,6 +51,13 @@ __device__ __forceinline__ void buffer_lds(__amdgpu_buffer_rsrc_t r, u32x4_t* ld
 #endif
 }
 
+// Half blocks of 16 values, of which a stage of 64 of k takes q = 0..3 of a row of Nb
+// blocks: in the stage at k0, half block q reads the 16 values from half_base(q, Nb) +
+// half_step(16 q, k0, 32 Nb) on.  What is not the row's reads its first half block or that
+// of the first stage (a row of one block has two, and the bytes past it may be past the tensor).
+__host__ __device__ constexpr int half_base(int q, int Nb) { return q < 2 * Nb ? 16 * q : 0; }
+__host__ __device__ constexpr int half_step(int at, int k0, int nk) { return k0 + at < nk ? k0 : 0; }
+
 // Stages R rows of features by 64 of k (KC) or 64 rows of k by R of c of a Ker in
 // 4 bits as bf16: a thread takes half blocks (8 bytes, 16 values).
 template <bool KC, int R, int NT, int SETS> struct Stager4 {
@@ -72,8 +79,8 @@ template <bool KC, int R, int NT, int SETS> struct Stager4 {
       if constexpr (KC) {
         const int64_t row = i0 + min(r, n - 1);
         at[j] = 16 * q;
-        codes[j] = c4 + row * 16 * Nb + 8 * q;
-        scales[j] = s4 + row * Nb + (q >> 1);
+        codes[j] = c4 + row * 16 * Nb + half_base(q, Nb) / 2;
+        scales[j] = s4 + row * Nb + half_base(q, Nb) / 32;
         there[j] = true;
       } else {
         at[j] = r;
@@ -92,7 +99,7 @@ template <bool KC, int R, int NT, int SETS> struct Stager4 {
       const bool in = k0 + at[j] < nk;
       gone[SET] |= (in && there[j] ? 0u : 1u) << j;
       if constexpr (KC) {
-        const int k = in ? k0 : 0;
+        const int k = half_step(at[j], k0, nk);
         __builtin_memcpy(&code[SET][j], codes[j] + (k >> 1), 8);
         scale[SET][j] = scales[j][k >> 5];
       } else {
