@@ -607,14 +607,6 @@ __global__ __launch_bounds__(512, 2) void group44_pipe(GroupArgs a, Group4Args b
   store_tile<T, TO, kFwd, true>(up_to(a, w.m0 + w.m_valid), w, lane, acc, xrow, yrow);
 }
 
-// Whether the byte offsets of a tile's rows, of any row that may be gathered and (the
-// gradient's) of a group's Ker fit a buffer of 2^31.
-constexpr int64_t kMostBytes = (1LL << 31) - 65536;
-inline bool pipe4_fits(const GroupArgs& a, int mode) {
-  return a.ldx < (1 << 22) && a.ldy < (1 << 22) && (!a.rows || a.Nsrc * a.ldy * 2 < kMostBytes) &&
-         (mode == kFwd || a.K * a.ldx * 2 < kMostBytes);
-}
-
 template <typename TO, int MODE>
 hipError_t launch_pipe4(const GroupArgs& a, const Group4Args& b, int64_t row_tiles, int band, hipStream_t stream) {
   auto* const k = MODE == kFwd ? group4_pipe<TO> : group4_pipe_bwd_in<TO>;

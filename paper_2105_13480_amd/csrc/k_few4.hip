@@ -8,6 +8,7 @@
 // by group4_rows 11.8), where no CU has enough workgroups otherwise.
 // group4_rows: 64 features by 16 or 32 rows, or 128 by 64; each wave has its own features
 // over all of k, and the rows come through a ring in LDS that the waves share.
+#include "group4_choice.h"
 #include "group4_kernel.h"
 
 namespace cnnlib {
@@ -241,8 +242,7 @@ template <typename TO> hipError_t launch_few(const GroupArgs& a, const Group4Arg
   const int64_t blocks = row_tiles(a.N, a.Ng, true, 16) * ((a.M + 15) / 16);
   const hipError_t e = grid_fits(blocks, 64 * kFewWaves);
   if (e != hipSuccess) return e;
-  // some runs for each wave
-  auto* const k = b.Nb >= 64 ? group4_few<TO, 4> : group4_few<TO, 2>;
+  auto* const k = few4_runs(b.Nb) == 4 ? group4_few<TO, 4> : group4_few<TO, 2>;
   k<<<dim3((uint32_t)blocks), dim3(64 * kFewWaves), 0, stream>>>(a, b);
   return hipGetLastError();
 }
