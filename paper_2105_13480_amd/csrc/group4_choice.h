@@ -16,8 +16,13 @@ constexpr int kShort4 = -1;
 // What a kernel's tile of tm features by tn rows costs (microseconds, fitted to 155
 // products on MI355X: 1 to 32 groups of 1 to 3000 rows, 512 to 4096 features each way,
 // Ker cold): of s stages and n tiles a CU, once + max(s max(alone, n share), Ker's bytes
-// at bw TB/s) + n ends.  The least is within 1 to 3 % of the best kernel's time on
-// average, 1.35 times it at worst.
+// at bw TB/s) + n ends.  The fit is older than the kernels: those of few rows, both kinds of
+// tiles with both in 4 bits and the pipelined ones have become faster since, and a last round
+// that is halved, or a tile of half the features, counts as a whole one here.  Of the
+// present kernels, launched from a graph, the pick is 5 % (bf16 rows), 2 % (both in 4 bits)
+// and 2 % (gradient) above the best one's time on average over the same sizes, and at worst
+// 1.48, 1.39 and 1.36 times it (8 rows of 8 groups of 1024 x 2048: 7.0 and 4.7 us; 512 rows
+// of 8 groups of 4096 x 4096: 31 and 23; the gradient of 320 of them: 63 and 46).
 struct Cost4 {
   int tm, tn;
   double alone, share, ends, once, bw;

@@ -131,7 +131,8 @@ template <bool KC, int R, int NT, int SETS> struct Stager4 {
 // writes of LDS, conversions and products, which a barrier a stage keeps from overlapping
 // within a workgroup (400 rows of 32 groups of 2048 x 2048 in 128 x 128 tiles: 147 us,
 // 730 TFLOP/s).  128 x 128 tiles have registers for two stages.  By 8 waves these are 8 to
-// 20 % faster where a CU has one tile, and a quarter slower where it has more.
+// 20 % faster where a CU has one tile, and a quarter slower where it has more: not built as
+// a tile of its own beside this one, between which the choice could tell.
 template <typename TO, int MODE, int TM, int TN, int SETS, bool LONG>
 __global__ __launch_bounds__(256, 2) void group4_tiles(GroupArgs a, Group4Args b, int band) {
   typedef bf16_t T;

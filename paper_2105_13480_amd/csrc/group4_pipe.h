@@ -12,7 +12,9 @@
 //                product of that size 1330 to 1480
 //   gradient     425 us, 1295 TFLOP/s; 1400
 //   both 4 bits  209 us, 2630 TFLOP/s; 4330: a stage of 1.7 us (0.9 at the matrix unit's
-//                rate, 1.0 of reads from LDS)
+//                rate).  Neither that nor LDS bounds the loop: both are busy for a
+//                quarter of the kernel, some 42 % of the loop, one after the other as it
+//                seems; why they do not overlap is not known.
 // A last round of at most 128 tiles is halved by features (15550 rows of 8 groups of
 // 2048 x 2048, 520 tiles: 141 us, now 131; one group of 1100 rows of 4096 x 4096 with both
 // in 4 bits 32.1 and 24.5), and a tile without its second half of features does without

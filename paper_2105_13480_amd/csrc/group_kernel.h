@@ -449,7 +449,9 @@ struct RowTile {
   int g, n0, n1, mt;
   int part;  // of a tile halved by features, 1 or 2; else 0
 };
-// Workgroups of a round of tiles that fill a CU each.
+// Workgroups of a round of tiles that fill a CU each: MI355X's CUs.  Where a part of the
+// GPU has fewer, tiles of other rounds than the last are halved: the same results, but
+// later, since a half takes three quarters of a tile's time.
 constexpr int kRound = 256;
 
 // Rows of group g; group Ng is the rows past the last.
